@@ -112,6 +112,90 @@ FEATFIX_API featfix_status featfix_op_attention(int dtype, const void* dev_qkv, 
                                     int batch, int n_txt, int n_img, int heads, int head_dim,
                                     void* stream);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit transformer layers: a root-mean-square norm, a product and a
+ * quantiser on e4m3 values with a scale for each block of 128 along the
+ * reduction dimension, and rotary positions with several axes.  They serve
+ * pre-norm transformer layers beside the denoiser's own adaLN blocks; the paper
+ * has no counterpart.
+ *
+ * 8-bit tensors are e4m3 bytes (largest value 448), row-major with a row stride
+ * ld of at least the width and a multiple of 16.  A block's scale is
+ *   s = max(largest |x| of the block / 448, 2^-100),   q = e4m3(x / s)
+ * rounded to nearest even; a block stands for q * s.  A NaN in a block makes its
+ * scale NaN, an infinity makes it infinite: what is computed from the block is
+ * NaN, never a finite number.  Activations have one scale per row and 128
+ * columns, stored block by block: the scale of row r and column c is
+ * scale[(c / 128) * ld_scale + r], ld_scale >= rows.  Weights have one per
+ * 128 x 128 block: scale[(r / 128) * ld_scale + c / 128],
+ * ld_scale >= ceil(cols / 128).
+ *
+ * Pointers to 8-bit tensors are 16-byte aligned, all others need only their
+ * element's alignment (16-byte aligned rows are faster); dtypes are
+ * FEATFIX_DTYPE_F32 / _BF16; row strides are in elements.  Sizes of zero rows
+ * are allowed and do nothing.  No call allocates or keeps anything.
+ * ------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of rows of C columns (C <= 32768) with the residual's
+ * addition in front of it:
+ *   h = x + resid   (x alone where dev_resid is NULL),
+ *   y = h / sqrt(mean(h^2) + eps) * weight   (weight 1 where dev_weight is NULL).
+ * h is kept in fp32 for the norm; dev_sum (NULL: not wanted) receives it rounded
+ * to dtype and may be dev_x or dev_resid.  Exactly one of dev_out (y in dtype)
+ * and dev_q (y in 8 bits, with dev_scale) is given.                          */
+FEATFIX_API featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void* dev_x, long long ld_x,
+                                   const void* dev_resid, long long ld_resid, void* dev_sum, long long ld_sum,
+                                   const void* dev_weight, float eps, void* dev_out, long long ld_out, void* dev_q,
+                                   long long ld_q, float* dev_scale, long long ld_scale, void* stream);
+
+/* x [rows, cols] in 8 bits: tile 1 for activations, 128 for weights (the
+ * scales' layouts above).                                                    */
+FEATFIX_API featfix_status featfix_op_quant8(int dtype, int tile, long long rows, int cols, const void* dev_x,
+                                 long long ld_x, void* dev_q, long long ld_q, float* dev_scale, long long ld_scale,
+                                 void* stream);
+
+/* Linear layer on 8-bit activations A [M, K] and weights W [N, K]:
+ *   acc[m, n] = sum_b a_scale[b, m] w_scale[n / 128, b] sum_{k in block b} A[m, k] W[n, k],
+ *   y = act(acc + bias),   act 0 = identity, 1 = GELU (tanh),
+ * with fp32 accumulation.  Exactly one of the results is given:
+ *   dev_out: resid + gate[m / rows_per_batch, :] * y in dtype [M, N] (gate float
+ *            rows of stride gate_stride, without it y; resid in dtype; both
+ *            nullable);
+ *   dev_q:   y in 8 bits with dev_q_scale, for the next layer (no gate, no resid).
+ * bias [N] is in dtype.  dev_out may be dev_resid where both have one row stride.
+ * A scale product a_scale * w_scale past fp32's range makes the result infinite
+ * or zero.  tcgen05 tensor cores (kind::f8f6f4), fed by TMA.                 */
+FEATFIX_API featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, const void* dev_a, long long ld_a,
+                                const float* dev_a_scale, long long ld_a_scale, const void* dev_w, long long ld_w,
+                                const float* dev_w_scale, long long ld_w_scale, const void* dev_bias, int act,
+                                const float* dev_gate, long long gate_stride, int rows_per_batch, const void* dev_resid,
+                                long long ld_resid, void* dev_out, long long ld_out, void* dev_q, long long ld_q,
+                                float* dev_q_scale, long long ld_q_scale, void* stream);
+
+/* Rotary positions on the heads of q [rows, q_heads * head_dim] and k [rows,
+ * k_heads * head_dim] (shared key heads: k_heads below q_heads; either may be
+ * absent with 0 heads).  axis_dims (host, n_axes even numbers, n_axes <= 8) are the
+ * widths of a head that each axis turns, one after the other; their sum rot <=
+ * head_dim, the columns past it are only copied.  Pair p, the i-th of axis a, of
+ * row r turns by
+ *   pos[a * ld_pos + r] * theta^(-2 i / axis_dims[a]),
+ * or theta^(-2 p / rot) with FEATFIX_ROPE_ONE_LADDER; the angle is within fp32
+ * rounding of a turn up to positions of 2^20, and within 3e-5 at any int32.  Pairs are columns (2p, 2p + 1), or (p, p + rot / 2) with
+ * FEATFIX_ROPE_HALVES.  FEATFIX_ROPE_INVERSE turns the other way: the inverse and
+ * so the gradient of the rotation.  q_weight / k_weight ([head_dim] in dtype,
+ * nullable) put the root-mean-square norm of each head, times the weight, in front
+ * of the rotation (not with INVERSE).  Outputs may be their inputs.  head_dim is
+ * even and at most 256.                                                      */
+#define FEATFIX_ROPE_HALVES 1u
+#define FEATFIX_ROPE_ONE_LADDER 2u
+#define FEATFIX_ROPE_INVERSE 4u
+FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_axes, const int* axis_dims,
+                               const int* dev_pos, long long ld_pos, double theta, unsigned flags, const void* dev_q,
+                               long long ld_q, int q_heads, const void* dev_q_weight, void* dev_q_out,
+                               long long ld_q_out, const void* dev_k, long long ld_k, int k_heads,
+                               const void* dev_k_weight, void* dev_k_out, long long ld_k_out, float eps,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

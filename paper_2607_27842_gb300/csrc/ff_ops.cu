@@ -2,12 +2,27 @@
 #include "featfix_ops.h"
 #include "ff_common.cuh"
 
+#include <math.h>
+
+#include <initializer_list>
+
 using namespace ff;
 
 namespace {
 
 bool dt_ok(int dt) { return dt == FEATFIX_DTYPE_F32 || dt == FEATFIX_DTYPE_BF16; }
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// every given pointer on its element's boundary
+bool el_al(int dt, std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if ((uintptr_t)p & (dt == FEATFIX_DTYPE_F32 ? 3 : 1)) return false;
+  return true;
+}
+// an 8-bit tensor of `width` columns with at least `scales` scales to a row of them
+bool q8_ok(const Quant8Out& t, long long width, long long scales) {
+  return t.q && t.scale && al16(t.q) && t.ldq >= width && t.ldq % 16 == 0 && !((uintptr_t)t.scale & 3) &&
+         t.lds >= scales;
+}
 featfix_status st(cudaError_t e) {
   if (e == cudaSuccess) return FEATFIX_OK;
   if (e == cudaErrorInvalidValue) return FEATFIX_ERR_INVALID_ARG;
@@ -109,6 +124,110 @@ featfix_status featfix_op_attention(int dtype, const void* dev_qkv, int ld_qkv, 
   a.H = heads;
   a.hd = head_dim;
   return st(attention((DType)dtype, a, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void* dev_x, long long ld_x,
+                                   const void* dev_resid, long long ld_resid, void* dev_sum, long long ld_sum,
+                                   const void* dev_weight, float eps, void* dev_out, long long ld_out, void* dev_q,
+                                   long long ld_q, float* dev_scale, long long ld_scale, void* stream) {
+  if (!dt_ok(dtype) || rows < 0 || rows > 0x7fffffff || C <= 0 || C > 32768 || !(eps >= 0.f))
+    return FEATFIX_ERR_INVALID_ARG;
+  if (rows == 0) return FEATFIX_OK;
+  if (!dev_x || ld_x < C || (dev_out != nullptr) == (dev_q != nullptr)) return FEATFIX_ERR_INVALID_ARG;
+  if ((dev_resid && ld_resid < C) || (dev_sum && ld_sum < C) || (dev_out && ld_out < C)) return FEATFIX_ERR_INVALID_ARG;
+  if (!el_al(dtype, {dev_x, dev_resid, dev_sum, dev_weight, dev_out})) return FEATFIX_ERR_INVALID_ARG;
+  const Quant8Out q8 = {dev_q, ld_q, dev_scale, ld_scale};
+  if (dev_q && !q8_ok(q8, C, rows)) return FEATFIX_ERR_INVALID_ARG;
+  const RmsArgs a = {dev_x, ld_x, dev_resid, ld_resid, dev_sum, ld_sum, dev_weight, eps, dev_out, ld_out, q8};
+  return st(launch_rms_norm((DType)dtype, rows, C, a, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_quant8(int dtype, int tile, long long rows, int cols, const void* dev_x, long long ld_x,
+                                 void* dev_q, long long ld_q, float* dev_scale, long long ld_scale, void* stream) {
+  if (!dt_ok(dtype) || (tile != 1 && tile != 128) || rows < 0 || rows > 0x7fffffff || cols <= 0)
+    return FEATFIX_ERR_INVALID_ARG;
+  if (rows == 0) return FEATFIX_OK;
+  if (!dev_x || ld_x < cols) return FEATFIX_ERR_INVALID_ARG;
+  const Quant8Out q8 = {dev_q, ld_q, dev_scale, ld_scale};
+  if (!el_al(dtype, {dev_x}) || !q8_ok(q8, cols, tile == 1 ? rows : (cols + 127) / 128)) return FEATFIX_ERR_INVALID_ARG;
+  return st(launch_quant8((DType)dtype, tile, rows, cols, dev_x, ld_x, q8, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, const void* dev_a, long long ld_a,
+                                const float* dev_a_scale, long long ld_a_scale, const void* dev_w, long long ld_w,
+                                const float* dev_w_scale, long long ld_w_scale, const void* dev_bias, int act,
+                                const float* dev_gate, long long gate_stride, int rows_per_batch, const void* dev_resid,
+                                long long ld_resid, void* dev_out, long long ld_out, void* dev_q, long long ld_q,
+                                float* dev_q_scale, long long ld_q_scale, void* stream) {
+  if (!dt_ok(dtype) || M < 0 || N <= 0 || K <= 0 || (act != 0 && act != 1)) return FEATFIX_ERR_INVALID_ARG;
+  if (M == 0) return FEATFIX_OK;
+  if ((dev_out != nullptr) == (dev_q != nullptr)) return FEATFIX_ERR_INVALID_ARG;
+  // (the operands' scales are only read: q8_ok asks for the same of inputs and outputs)
+  const Quant8Out a8 = {const_cast<void*>(dev_a), ld_a, const_cast<float*>(dev_a_scale), ld_a_scale};
+  const Quant8Out w8 = {const_cast<void*>(dev_w), ld_w, const_cast<float*>(dev_w_scale), ld_w_scale};
+  const Quant8Out q8 = {dev_q, ld_q, dev_q_scale, ld_q_scale};
+  if (!q8_ok(a8, K, M) || !q8_ok(w8, K, ((long long)K + 127) / 128) || (dev_q && !q8_ok(q8, N, M)))
+    return FEATFIX_ERR_INVALID_ARG;
+  if (dev_q && (dev_gate || dev_resid)) return FEATFIX_ERR_INVALID_ARG;
+  if (dev_gate && (rows_per_batch <= 0 || gate_stride < N || ((uintptr_t)dev_gate & 3))) return FEATFIX_ERR_INVALID_ARG;
+  if ((dev_resid && ld_resid < N) || (dev_out && ld_out < N) || !el_al(dtype, {dev_bias, dev_resid, dev_out}))
+    return FEATFIX_ERR_INVALID_ARG;
+  const Gemm8Args g = {dev_a, ld_a, dev_a_scale, ld_a_scale, dev_w, ld_w, dev_w_scale, ld_w_scale, dev_bias, act,
+                       dev_gate, gate_stride, rows_per_batch > 0 ? rows_per_batch : 1, dev_resid, ld_resid, dev_out,
+                       ld_out, q8};
+  return st(gemm8((DType)dtype, M, N, K, g, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_axes, const int* axis_dims,
+                               const int* dev_pos, long long ld_pos, double theta, unsigned flags, const void* dev_q,
+                               long long ld_q, int q_heads, const void* dev_q_weight, void* dev_q_out,
+                               long long ld_q_out, const void* dev_k, long long ld_k, int k_heads,
+                               const void* dev_k_weight, void* dev_k_out, long long ld_k_out, float eps,
+                               void* stream) {
+  if (!dt_ok(dtype) || rows < 0 || rows > 0x7fffffff || head_dim <= 0 || head_dim % 2 || head_dim > 2 * ROPE_PAIRS ||
+      n_axes < 1 || n_axes > 8 || !axis_dims ||
+      !(theta > 0.0) || isinf(theta) || (flags & ~7u) || q_heads < 0 || k_heads < 0 || q_heads + (long long)k_heads < 1 ||
+      !(eps >= 0.f))
+    return FEATFIX_ERR_INVALID_ARG;
+  int rot = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (axis_dims[a] <= 0 || axis_dims[a] % 2 || axis_dims[a] > head_dim - rot) return FEATFIX_ERR_INVALID_ARG;
+    rot += axis_dims[a];
+  }
+  if (rows == 0) return FEATFIX_OK;
+  if (!dev_pos || ((uintptr_t)dev_pos & 3) || ld_pos < rows) return FEATFIX_ERR_INVALID_ARG;
+  RopeArgs r = {};
+  r.side[0] = {dev_q, ld_q, dev_q_out, ld_q_out, dev_q_weight, q_heads};
+  r.side[1] = {dev_k, ld_k, dev_k_out, ld_k_out, dev_k_weight, k_heads};
+  for (const RopeSide& sd : r.side) {
+    const long long width = (long long)sd.heads * head_dim;
+    if (sd.heads == 0) continue;
+    if (!sd.x || !sd.out || width > 0x7fffffff || sd.ldx < width || sd.ldo < width ||
+        !el_al(dtype, {sd.x, sd.out, sd.weight}) || (sd.weight && (flags & FEATFIX_ROPE_INVERSE)))
+      return FEATFIX_ERR_INVALID_ARG;
+  }
+  r.pos = dev_pos;
+  r.ld_pos = ld_pos;
+  r.hd = head_dim;
+  r.rot = rot;
+  r.halves = (flags & FEATFIX_ROPE_HALVES) ? 1 : 0;
+  r.eps = eps;
+  // turns per position: theta^(-2 i / width) / 2 pi, each step of a ladder one product
+  const double turn = ((flags & FEATFIX_ROPE_INVERSE) ? -0.5 : 0.5) / M_PI;
+  const bool one = (flags & FEATFIX_ROPE_ONE_LADDER) != 0;
+  double f = turn, step = one ? pow(theta, -2.0 / rot) : 1.0;
+  for (int a = 0, p = 0; a < n_axes; ++a) {
+    if (!one) {
+      f = turn;
+      step = pow(theta, -2.0 / axis_dims[a]);
+    }
+    for (int i = 0; i < axis_dims[a] / 2; ++i, ++p, f *= step) {
+      const float hi = (float)f;
+      r.freq[p] = make_float2(hi, (float)(f - (double)hi));
+      r.axis[p] = (unsigned char)a;
+    }
+  }
+  return st(launch_rope((DType)dtype, rows, r, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -94,6 +94,13 @@ SIGNATURES = {
     "featfix_op_ln_modulate": (_I, [_I, _VP, _VP, _LL, _I, _VP, _VP, _I, _I, _VP]),
     "featfix_op_gemm": (_I, [_I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _I, _I, _VP, _VP, _VP, _VP, _VP]),
     "featfix_op_attention": (_I, [_I, _VP, _I, _VP, _I, _I, _I, _I, _I, _I, _VP]),
+    "featfix_op_rms_norm": (_I, [_I, _LL, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP, ctypes.c_float, _VP, _LL, _VP, _LL,
+                                 _VP, _LL, _VP]),
+    "featfix_op_quant8": (_I, [_I, _I, _LL, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP]),
+    "featfix_op_gemm8": (_I, [_I, _I, _I, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _I, _VP, _LL, _I, _VP, _LL,
+                              _VP, _LL, _VP, _LL, _VP, _LL, _VP]),
+    "featfix_op_rope": (_I, [_I, _LL, _I, _I, _P(_I), _VP, _LL, _D, ctypes.c_uint, _VP, _LL, _I, _VP, _VP, _LL, _VP,
+                             _LL, _I, _VP, _VP, _LL, ctypes.c_float, _VP]),
 }
 
 # argument arrays of the draft and the paid check (at most four history terms)
@@ -431,6 +438,129 @@ def featfix_op_gemm(dtype, a, w, out, bias=None, act=0, gate=None, gate_stride=0
 def featfix_op_attention(dtype, qkv, out, batch, n_txt, n_img, heads, head_dim, stream=None):
     _check(lib().featfix_op_attention(_dt(dtype), _ptr(qkv), qkv.shape[-1], _ptr(out), out.shape[-1], int(batch),
                                       int(n_txt), int(n_img), int(heads), int(head_dim), _stream_ptr(stream)))
+
+
+# ----------------------------------------------------------------------------
+# 8-bit layers (featfix_ops.h): tensors are 2-D with unit column stride, any row
+# stride; 8-bit ones have an element of one byte and rows of whole 16 bytes
+# ----------------------------------------------------------------------------
+
+ROPE_HALVES, ROPE_ONE_LADDER, ROPE_INVERSE = 1, 2, 4
+
+
+def _bad(msg):
+    raise FeatFixError(ERR_INVALID_ARG, msg)
+
+
+# element types: those of the C ABI, then 8-bit values and positions
+_F32, _BF16, _Q8, _I32 = range(4)
+_torch_types = None
+
+
+def _typed(t, name, dtype):
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        _torch_types = ((torch.float32,), (torch.bfloat16,), (torch.float8_e4m3fn, torch.uint8), (torch.int32,))
+    if t.dtype not in _torch_types[dtype]:
+        _bad("%s: %s where %s is expected" % (name, t.dtype, _torch_types[dtype][0]))
+    if not t.is_cuda:
+        _bad("%s is not on the GPU" % name)
+
+
+def _dims(t, name):
+    if len(t.shape) != 2:
+        _bad("%s: expected two dimensions, got %s" % (name, list(t.shape)))
+    return t.shape
+
+
+def _mat(t, name, dtype, rows, cols):
+    """(address, row stride) of a 2-D tensor of the given size; None -> NULL."""
+    if t is None:
+        return None, 0
+    sh, st = t.shape, t.stride()
+    if len(sh) != 2 or sh[0] != rows or sh[1] != cols:
+        _bad("%s: expected a tensor [%d, %d], got %s" % (name, rows, cols, list(sh)))
+    if cols > 1 and st[1] != 1:
+        _bad("%s: columns must be adjacent" % name)
+    _typed(t, name, dtype)
+    # (the stride of a single row says nothing)
+    return t.data_ptr(), st[0] if rows > 1 else cols if dtype != _Q8 else (cols + 15) // 16 * 16
+
+
+def _vec(t, name, dtype, n):
+    """Address of n adjacent elements; None -> NULL."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous():
+        _bad("%s: expected %d adjacent elements" % (name, n))
+    _typed(t, name, dtype)
+    return t.data_ptr()
+
+
+def _quant8(q, scale, rows, cols, tile=1):
+    """(q address, ld, scale address, ld) of an 8-bit tensor and its scales."""
+    if (q is None) != (scale is None):
+        _bad("8-bit values and their scales come together")
+    nb = (cols + 127) // 128
+    return _mat(q, "8-bit values", _Q8, rows, cols) + (
+        _mat(scale, "scales", _F32, nb, rows) if tile == 1 else _mat(scale, "scales", _F32, (rows + 127) // 128, nb))
+
+
+def featfix_op_rms_norm(dtype, x, weight, eps, resid=None, sum_out=None, out=None, q=None, q_scale=None, stream=None):
+    """y = rms_norm(x + resid) * weight into ``out``, or in 8 bits into ``q`` and
+    ``q_scale`` [ceil(C / 128), rows]; x + resid into ``sum_out``."""
+    dt = _dt(dtype)
+    rows, C = _dims(x, "x")
+    _check(lib().featfix_op_rms_norm(dt, rows, C, *_mat(x, "x", dt, rows, C), *_mat(resid, "resid", dt, rows, C),
+                                     *_mat(sum_out, "sum_out", dt, rows, C), _vec(weight, "weight", dt, C), eps,
+                                     *_mat(out, "out", dt, rows, C), *_quant8(q, q_scale, rows, C),
+                                     _stream_ptr(stream)))
+
+
+def featfix_op_quant8(dtype, x, q, q_scale, tile=1, stream=None):
+    """x in 8 bits: ``tile`` 1 for activations (q_scale [ceil(cols / 128), rows]),
+    128 for weights (q_scale [ceil(rows / 128), ceil(cols / 128)])."""
+    dt = _dt(dtype)
+    rows, cols = _dims(x, "x")
+    _check(lib().featfix_op_quant8(dt, int(tile), rows, cols, *_mat(x, "x", dt, rows, cols),
+                                   *_quant8(q, q_scale, rows, cols, tile), _stream_ptr(stream)))
+
+
+def featfix_op_gemm8(dtype, a, a_scale, w, w_scale, out=None, bias=None, act=0, gate=None, rows_per_batch=0, resid=None,
+                     q=None, q_scale=None, stream=None):
+    """act(a w^T + bias) of 8-bit a and w into ``out`` (resid + gate * it, where
+    given), or in 8 bits into ``q`` and ``q_scale``."""
+    dt = _dt(dtype)
+    M, K = _dims(a, "a")
+    N = _dims(w, "w")[0]
+    gp, gs = (None, 0) if gate is None else _mat(gate, "gate", _F32, -(-M // max(1, rows_per_batch)), N)
+    _check(lib().featfix_op_gemm8(dt, M, N, K, *_quant8(a, a_scale, M, K), *_quant8(w, w_scale, N, K, 128),
+                                  _vec(bias, "bias", dt, N), act, gp, gs, rows_per_batch,
+                                  *_mat(resid, "resid", dt, M, N), *_mat(out, "out", dt, M, N),
+                                  *_quant8(q, q_scale, M, N), _stream_ptr(stream)))
+
+
+def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None, k_out=None, theta=10000.0, halves=False,
+                    one_ladder=False, inverse=False, q_weight=None, k_weight=None, eps=1e-6, stream=None):
+    """Rotary positions on q [rows, heads * head_dim] and k: ``pos`` int32 [axes,
+    rows], ``axis_dims`` the columns of a head that each axis turns."""
+    dt = _dt(dtype)
+    n = len(axis_dims)
+    rows = _dims(pos, "pos")[1]
+    side = []
+    for name, x, o, w in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
+        if x is None:
+            side += [None, 0, 0, None, None, 0]
+            continue
+        width = _dims(x, name)[1]
+        if width % head_dim:
+            _bad("%s: %d columns are no whole number of heads" % (name, width))
+        side += [*_mat(x, name, dt, rows, width), width // head_dim, _vec(w, name + "_weight", dt, head_dim),
+                 *_mat(o, name + "_out", dt, rows, width)]
+    flags = (ROPE_HALVES if halves else 0) | (ROPE_ONE_LADDER if one_ladder else 0) | (ROPE_INVERSE if inverse else 0)
+    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_I * n)(*axis_dims), *_mat(pos, "pos", _I32, n, rows), theta,
+                                 flags, *side, eps, _stream_ptr(stream)))
 
 
 class FeatFix:
