@@ -1,89 +1,526 @@
-// 8-bit dense layers with a scale for each block of 128.
+// 8-bit dense layers with a scale for each block of 128 (formula: featfix_op_gemm8),
+// on the tensor cores (tcgen05.mma kind::f8f6f4, fp32 accumulators in TMEM).
+//
+// The scales change every 128 columns of K, so TMEM only ever holds the sum over one
+// such block: the MMA warp fills an accumulator buffer with four K = 32 products and
+// starts the next buffer, while the epilogue warps read the buffer back, multiply it
+// by its two scales and add it to fp32 sums in their registers.  A row of a thread
+// covers 128 columns, one scale block of W and of an 8-bit result, so a thread needs
+// a single product of scales per block and finds the largest magnitude of an 8-bit
+// result's block by itself.
 #include "ff_common.cuh"
 #include "ff_q8.cuh"
+#include "ff_tc.cuh"
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <mutex>
 
 namespace ff {
 
 namespace {
 
-__device__ __forceinline__ float from_e4m3(uint8_t q) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3)));
+using namespace tc;
+
+__device__ unsigned int g_watchdog8;
+
+constexpr int BK = 128;   // one scale block, one 128-byte swizzled row of a stage
+
+__device__ __forceinline__ bool wait_poll(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  return mbar_wait<true>(b, parity, abort_flag, &g_watchdog8);
+}
+// every lane waits, the vote keeps the loop around it warp-uniform
+__device__ __forceinline__ bool wait_warp(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  const bool ok = mbar_test(b, parity) || wait_poll(b, parity, abort_flag);
+  return __all_sync(0xffffffffu, ok);
 }
 
-// 32 rows x 128 columns to a block, 4 x 4 results to a thread.
-template <class T>
-__global__ void __launch_bounds__(256) k_gemm8(int M, int N, int K, const __grid_constant__ Gemm8Args g) {
-  __shared__ float sa[32][33], sw[128][33];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int m0 = blockIdx.y * 32, n0 = blockIdx.x * 128;
-  float acc[4][4] = {};
-  for (int b = 0; b * 128 < K; ++b) {
-    float part[4][4] = {};
-    for (int k0 = b * 128; k0 < min(K, b * 128 + 128); k0 += 32) {
-      __syncthreads();
-      for (int i = ty; i < 32; i += 8)
-        sa[i][tx] = m0 + i < M && k0 + tx < K
-                        ? from_e4m3(reinterpret_cast<const uint8_t*>(g.a)[(m0 + i) * g.lda + k0 + tx]) : 0.f;
-      for (int i = ty; i < 128; i += 8)
-        sw[i][tx] = n0 + i < N && k0 + tx < K
-                        ? from_e4m3(reinterpret_cast<const uint8_t*>(g.w)[(n0 + i) * g.ldw + k0 + tx]) : 0.f;
-      __syncthreads();
-      for (int k = 0; k < 32; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) part[i][j] = fmaf(sa[ty * 4 + i][k], sw[tx + 32 * j][k], part[i][j]);
-    }
-    const float fw = g.sw[blockIdx.x * g.ldsw + b];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int m = m0 + ty * 4 + i;
-      const float f = m < M ? g.sa[b * g.ldsa + m] * fw : 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(f, part[i][j], acc[i][j]);
+// the same without a call: the epilogue warps hold 128 sums in registers meanwhile
+__device__ __forceinline__ bool wait_inline(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
+  const unsigned long long t0 = gtimer();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
+    const bool late = *abort_flag || gtimer() - t0 > WAIT_LIMIT_NS;
+    if (__any_sync(0xffffffffu, late)) {
+      *abort_flag = 1;
+      atomicOr(&g_watchdog8, 1u);
+      return false;
     }
   }
+}
+
+// instruction descriptor, kind::f8f6f4: D fp32 (bit 4), A and B e4m3 (0 at bits 7
+// and 10), both K-major, N >> 3 at bit 17, M >> 4 at bit 24
+constexpr uint32_t idesc8(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+__device__ __forceinline__ void umma8_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(
+          d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(accum));
+}
+
+// GELU (tanh form) of four values: x (1 + tanh u) / 2 = x / (1 + 2^t), t = -2 u
+// log2(e).  One reciprocal for the four (16 a clock and SM against 32 for the
+// exponential): each denominator is capped at 2^30, past which the result is below
+// 2^-26 of x, the rounding of the tanh form.  Within 1e-6 of the exact value; the
+// hardware tanh (2^-11) would show in an 8-bit result's scales.
+__device__ __forceinline__ void gelu4(float& a, float& b, float& c, float& d) {
+  constexpr float K0 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, K1 = K0 * 0.044715f;
+  float v[4] = {a, b, c, d}, e[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const long long m = m0 + ty * 4 + i;
-    if (m >= M) return;
+    const float t = fminf(v[i] * __fmaf_rn(v[i] * v[i], K1, K0), 30.f);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(t));
+    e[i] += 1.f;
+  }
+  const float ab = e[0] * e[1], cd = e[2] * e[3];
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(ab * cd));
+  const float rab = r * cd, rcd = r * ab;
+  a *= rab * e[1];
+  b *= rab * e[0];
+  c *= rcd * e[3];
+  d *= rcd * e[2];
+}
+
+// ---------------------------------------------------------------------------
+// CTA pairs: 256 x 256 tiles of the result, persistent.  Each CTA stages its own
+// 128 rows of A and 128 of the tile's rows of W (32 KB a block of K) and
+// holds 128 x 256 of the accumulator.
+//   warp 0     TMA producer, a ring of STAGES blocks of K
+//   warp 1     MMA issuer (even CTA): tcgen05.mma.cta_group::2, M = N = 256
+//   warps 4-11 epilogue: TMEM lane quarter warp % 4, column half (warp - 4) / 4
+// 168 registers a thread at launch; the first four warps hand theirs on down to
+// 40, the epilogue's two warpgroups take 232 (40 + 2 * 232 = 3 * 168), 128 of
+// which hold sums.
+// ---------------------------------------------------------------------------
+constexpr int P_THREADS = 384;
+constexpr int P_STAGES = 5;
+constexpr uint32_t P_STAGE_BYTES = 2 * 128 * BK;
+constexpr uint32_t P_EPI_BYTES = 8 * 8192;   // 8 KB of output blocks to an epilogue warp
+constexpr size_t P_SMEM = 1024 + (size_t)P_STAGES * P_STAGE_BYTES + P_EPI_BYTES + 256;
+
+// 128-byte-swizzled block of 32 rows: 16-byte chunk k of row r
+__device__ __forceinline__ uint32_t sw128_off(int r, int k) { return (uint32_t)(r * 128 + ((k ^ (r & 7)) << 4)); }
+
+enum { STAGED = 1, RESID_TMA = 2 };
+
+// bias, gate and residual of 32 adjacent columns n0.. of row m, or 8-bit output: y in
+// place of the sums.  Columns past N: y of a zero sum, never stored.
+template <class T>
+__device__ __forceinline__ void finish32(const Gemm8Args& g, int m, int n0, int N, float (&y)[32]) {
+  const T* bias = reinterpret_cast<const T*>(g.bias);
+  if (bias) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (n0 + j < N) y[j] += to_f(bias[n0 + j]);
+  }
+  if (g.act) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) gelu4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+  }
+  if (g.gate) {
+    const float* gp = g.gate + (long long)(m / g.rpb) * g.gate_stride + n0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (n0 + j < N) y[j] *= gp[j];
+  }
+}
+
+// A warp's block of 32 rows of 128 bytes between shared memory and row-major global
+// memory, coalesced, element by element: for rows that TMA cannot take.
+template <class T>
+__device__ __forceinline__ void block_in(uint8_t* b, const T* src, long long ld, int rows, int cols, int lane) {
+#pragma unroll 4
+  for (int r = 0; r < min(rows, 32); ++r)
+#pragma unroll
+    for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
+      if (j < cols)
+        *reinterpret_cast<T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16) = src[r * ld + j];
+}
+template <class T>
+__device__ __forceinline__ void block_out(const uint8_t* b, T* dst, long long ld, int rows, int cols, int lane) {
+#pragma unroll 4
+  for (int r = 0; r < min(rows, 32); ++r)
+#pragma unroll
+    for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
+      if (j < cols)
+        dst[r * ld + j] = *reinterpret_cast<const T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16);
+}
+
+// Sums of a thread's row over 128 columns -> result, through the warp's two 4 KB
+// blocks.  A TMA store writes whole 16 bytes, past the last column too: rows that
+// do not end on 16 bytes leave their last tile through block_out.
+template <class T, bool Q8>
+__device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const CUtensorMap* tmO, float (&acc)[128], int row0,
+                                           int lane, int n0, int M, int N, uint8_t* blk, uint64_t* rbar, uint32_t rph,
+                                           volatile int* abort_flag) {
+  const int m = min(row0 + lane, M - 1);   // (rows past M repeat the last one and are not stored)
+  const int es = Q8 ? 1 : (int)sizeof(T);
+  const bool tma = (flags & STAGED) && (n0 + 128 <= N || (long long)N * es % 16 == 0);
+  if constexpr (Q8) {
     uint32_t mx = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + tx + 32 * j;
-      float y = acc[i][j];
-      if (n < N) {
-        if (g.bias) y += to_f(reinterpret_cast<const T*>(g.bias)[n]);
-        if (g.act) y = gelu_tanh(y);
-        if (g.gate) y *= g.gate[m / g.rpb * g.gate_stride + n];
-        if (g.resid) y += to_f(reinterpret_cast<const T*>(g.resid)[m * g.ldr + n]);
-        if (g.out) reinterpret_cast<T*>(g.out)[m * g.ldo + n] = from_f<T>(y);
-        mx = max(mx, abs_bits(y));
-      }
-      acc[i][j] = y;
-    }
-    if (!g.out) {
-      const float s = q8_scale(__reduce_max_sync(0xffffffffu, mx)), inv = 1.f / s;
+    for (int c = 0; c < 128; c += 32) {
+      float y[32];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (n0 + tx + 32 * j < N)
-          reinterpret_cast<uint8_t*>(g.q8.q)[m * g.q8.ldq + n0 + tx + 32 * j] = (uint8_t)to_e4m3x2(acc[i][j] * inv, 0.f);
-      if (tx == 0) g.q8.scale[blockIdx.x * g.q8.lds + m] = s;
+      for (int j = 0; j < 32; ++j) y[j] = acc[c + j];
+      finish32<T>(g, m, n0 + c, N, y);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        mx = max(mx, abs_bits(y[j]));
+        acc[c + j] = y[j];
+      }
+    }
+    const float s = q8_scale(mx), inv = 1.f / s;
+    if (row0 + lane < M) g.q8.scale[(n0 >> 7) * g.q8.lds + m] = s;
+    if (lane == 0) bulk_wait_read<0>();
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = to_e4m3x4(acc[16 * k + 4 * i] * inv, acc[16 * k + 4 * i + 1] * inv, acc[16 * k + 4 * i + 2] * inv,
+                         acc[16 * k + 4 * i + 3] * inv);
+      *reinterpret_cast<uint4*>(blk + sw128_off(lane, k)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    if (tma) fence_async_smem();
+    __syncwarp();
+    if (!tma) {
+      block_out<uint8_t>(blk, reinterpret_cast<uint8_t*>(g.q8.q) + row0 * g.q8.ldq + n0, g.q8.ldq, M - row0, N - n0, lane);
+      __syncwarp();
+    } else if (lane == 0) {
+      tma_store(tmO, blk, n0, row0);
+      bulk_commit();
+    }
+    return true;
+  }
+  constexpr int PER = 128 / (int)sizeof(T);   // columns of a block
+  constexpr int V = 16 / (int)sizeof(T);
+  if ((flags & RESID_TMA) && !wait_inline(rbar, rph, abort_flag)) return false;
+#pragma unroll
+  for (int c = 0; c < 128; c += PER) {
+    if (n0 + c >= N) break;
+    uint8_t* b = blk + (c / PER & 1) * 4096;
+    if (!(flags & RESID_TMA)) {
+      // the last tile's stores, or this tile's before last, have left the block (with
+      // the residual by TMA: before that came)
+      if (lane == 0) {
+        if (c == 0) bulk_wait_read<0>(); else bulk_wait_read<1>();
+      }
+      __syncwarp();
+      if (g.resid) {
+        block_in<T>(b, reinterpret_cast<const T*>(g.resid) + row0 * g.ldr + n0 + c, g.ldr, M - row0, N - n0 - c, lane);
+        __syncwarp();
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < PER; d += 32) {
+      float y[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) y[j] = acc[c + d + j];
+      finish32<T>(g, m, n0 + c + d, N, y);
+#pragma unroll
+      for (int k = 0; k < 32 / V; ++k) {
+        T* p = reinterpret_cast<T*>(b + sw128_off(lane, d / V + k));
+        float o[V], r[V];
+        if (g.resid) ld16(p, r);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = g.resid ? y[V * k + i] + r[i] : y[V * k + i];
+        st16(p, o);
+      }
+    }
+    if (tma) fence_async_smem();
+    __syncwarp();
+    if (!tma) {
+      block_out<T>(b, reinterpret_cast<T*>(g.out) + row0 * g.ldo + n0 + c, g.ldo, M - row0, N - n0 - c, lane);
+      __syncwarp();
+    } else if (lane == 0) {
+      tma_store(tmO, b, n0 + c, row0);
+      bulk_commit();
     }
   }
+  return true;
+}
+
+// Tile order: groups of 8 row blocks, each swept over all column blocks with its
+// rows fastest (ff_gemm_tc.cu has the measurement).
+__device__ __forceinline__ void tile_at8(int tile, int num_m, int num_n, int& m, int& n) {
+  const int g = tile / (8 * num_n), r = tile - g * 8 * num_n;
+  const int gm = min(8, num_m - g * 8);
+  n = r / gm;
+  m = g * 8 + r - n * gm;
+}
+
+template <class T, bool Q8>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+    k_gemm8_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                 const __grid_constant__ CUtensorMap tmO, const __grid_constant__ CUtensorMap tmR, int M, int N, int K,
+                 int flags, const __grid_constant__ Gemm8Args g) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* epi = smem + P_STAGES * P_STAGE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(epi + P_EPI_BYTES);
+  uint64_t* empty = full + P_STAGES;
+  uint64_t* tfull = empty + P_STAGES;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* rbar = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(rbar + 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int num_m = (M + 255) / 256, num_n = (N + 255) / 256, num_tiles = num_m * num_n;
+  const int num_kb = (K + BK - 1) / BK;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P_STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 16);   // the epilogue warps of both CTAs
+    }
+    for (int w = 0; w < 8; ++w) mbar_init(&rbar[w], 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tmA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tmW) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_trigger();
+  pdl_wait();
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 0 && lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+        int mb, nb;
+        tile_at8(tile, num_m, num_n, mb, nb);
+        for (int kb = 0; kb < num_kb; ++kb, ++it) {
+          const int s = it % P_STAGES;
+          if (!wait_poll(&empty[s], ((it / P_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(&full[s], 2 * P_STAGE_BYTES);
+          const uint32_t fb = map_to(&full[s], 0);
+          uint8_t* st = smem + s * P_STAGE_BYTES;
+          tma_load_pair(&tmA, fb, st, kb * BK, mb * 256 + (int)rank * 128);
+          tma_load_pair(&tmW, fb, st + 128 * BK, kb * BK, nb * 256 + (int)rank * 128);
+        }
+      }
+      if (rank == 0) {   // no copy may land after the CTAs exit
+        for (uint32_t k = 0; k < (uint32_t)P_STAGES && k < it; ++k) {
+          const uint32_t j = it - 1 - k;
+          const unsigned long long t0 = gtimer();
+          while (!mbar_try(&full[j % P_STAGES], (j / P_STAGES) & 1))
+            if (gtimer() - t0 > WAIT_LIMIT_NS) { atomicOr(&g_watchdog8, 2u); break; }
+        }
+      }
+    }
+    if (warp == 1 && rank == 0) {
+      uint32_t it = 0;   // blocks of K over all tiles: ring stage it % STAGES, TMEM buffer it % 2
+      bool ok = true;
+      for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+        for (int kb = 0; kb < num_kb; ++kb, ++it) {
+          const int s = it % P_STAGES;
+          const uint32_t buf = it & 1;
+          if (!wait_warp(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag) ||
+              !wait_warp(&full[s], (it / P_STAGES) & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t st = saddr(smem + s * P_STAGE_BYTES);
+          const uint64_t ad = sw128_desc(st), wd = sw128_desc(st + 128 * BK);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // 32 bytes along K inside the swizzle atom
+              umma8_pair(tmem_base + buf * 256, ad + 2 * k, wd + 2 * k, idesc8(256, 256), k != 0);
+            umma_commit_pair(&tfull[buf]);
+            umma_commit_pair(&empty[s]);
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int q = warp & 3, h = (warp - 4) >> 2;
+    uint8_t* blk = epi + (warp - 4) * 8192;
+    const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 128);
+    uint32_t it = 0, rph = 0;
+    for (int tile = pair; tile < num_tiles; tile += npairs) {
+      int mb, nb;
+      tile_at8(tile, num_m, num_n, mb, nb);
+      const int row0 = mb * 256 + (int)rank * 128 + q * 32, n0 = nb * 256 + h * 128;
+      const bool live = n0 < N && row0 < M;   // (warp-uniform)
+      if (live && (flags & RESID_TMA) && lane == 0) {
+        bulk_wait_read<0>();   // the last tile's stores have left the blocks
+        fence_async_smem();    // (and so have block_out's reads)
+        mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
+        tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
+        if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+      }
+      // scales of this row and of W's block of rows, two blocks of K ahead
+      const bool in = live && row0 + lane < M;
+      const float* sa = g.sa + row0 + lane;
+      const float* sw = g.sw + (n0 >> 7) * g.ldsw;
+      float a0 = in ? sa[0] : 0.f, w0 = in ? sw[0] : 0.f;
+      float a1 = in && num_kb > 1 ? sa[g.ldsa] : 0.f, w1 = in && num_kb > 1 ? sw[1] : 0.f;
+      f32x2 acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = 0;
+      bool ok = true;
+      for (int kb = 0; kb < num_kb; ++kb, ++it) {
+        const uint32_t buf = it & 1;
+        const float f = a0 * w0;
+        a0 = a1;
+        w0 = w1;
+        if (in && kb + 2 < num_kb) {
+          a1 = sa[(kb + 2) * g.ldsa];
+          w1 = sw[kb + 2];
+        }
+        if (!wait_inline(&tfull[buf], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        if (live) {
+          const f32x2 ff = f2u(f, f);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float p[32];
+            tmem_ld32(tq + buf * 256 + c * 32, p);
+            if (c == 3) {   // the buffer is read: the MMA warp may fill it again
+              tc_fence_before();
+              if (lane == 0) mbar_arrive_cluster(map_to(&tempty[buf], 0));
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c * 16 + i] = ffma2(f2u(p[2 * i], p[2 * i + 1]), ff, acc[c * 16 + i]);
+          }
+        } else {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to(&tempty[buf], 0));
+        }
+      }
+      if (live) {
+        float y[128];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+          y[2 * i] = lo_f(acc[i]);
+          y[2 * i + 1] = hi_f(acc[i]);
+        }
+        if (ok) {
+          ok = finish_row<T, Q8>(g, flags, &tmO, y, row0, lane, n0, M, N, blk, &rbar[warp - 4], rph, abort_flag);
+        } else if ((flags & RESID_TMA) && lane == 0) {   // its copies still land before the CTA exits
+          const unsigned long long t0 = gtimer();
+          while (!mbar_try(&rbar[warp - 4], rph))
+            if (gtimer() - t0 > WAIT_LIMIT_NS) { atomicOr(&g_watchdog8, 2u); break; }
+        }
+        rph ^= 1;
+      }
+      if (!ok) break;
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();   // no CTA leaves while its peer may still address its TMEM or barriers
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+std::once_flag g_once;
+int g_sms = 0;
+
+bool init_driver() {
+  std::call_once(g_once, [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&g_sms, cudaDevAttrMultiProcessorCount, dev);
+    if (g_sms <= 0) g_sms = 148;
+    auto smem = [](const void* fn, size_t bytes) {
+      cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    };
+    smem((const void*)k_gemm8_pair<float, false>, P_SMEM);
+    smem((const void*)k_gemm8_pair<float, true>, P_SMEM);
+    smem((const void*)k_gemm8_pair<bf16, false>, P_SMEM);
+    smem((const void*)k_gemm8_pair<bf16, true>, P_SMEM);
+  });
+  return g_encode != nullptr;
+}
+
+// Row-major [rows, cols] of `es`-byte elements in boxes of box_rows rows of 128
+// bytes, 128-byte swizzle, zero fill out of bounds.
+bool make_map8(CUtensorMap* m, const void* base, int es, long long rows, long long cols, long long ld, int box_rows) {
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * es};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType t = es == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                : es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                          : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  return g_encode(m, t, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class T>
+cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
+  constexpr int es = (int)sizeof(T);
+  CUtensorMap ma, mw, mo, mr;
+  if (!make_map8(&ma, g.a, 1, M, K, g.lda, 128) || !make_map8(&mw, g.w, 1, N, K, g.ldw, 128))
+    return cudaErrorInvalidValue;
+  mo = mr = ma;
+  int flags = 0;
+  if (!g.out) {
+    if (!make_map8(&mo, g.q8.q, 1, M, N, g.q8.ldq, 32)) return cudaErrorInvalidValue;
+    flags = STAGED;
+  } else if (!((uintptr_t)g.out & 15) && g.ldo * es % 16 == 0 && make_map8(&mo, g.out, es, M, N, g.ldo, 32)) {
+    flags = STAGED;
+    if (es == 2 && g.resid && !((uintptr_t)g.resid & 15) && g.ldr * es % 16 == 0 &&
+        make_map8(&mr, g.resid, es, M, N, g.ldr, 32))
+      flags |= RESID_TMA;
+  }
+  const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
+  if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
+  const int pairs = g_sms / 2, grid = 2 * (int)(tiles < pairs ? tiles : pairs);
+  if (g.out)
+    launch_pdl(k_gemm8_pair<T, false>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
+  else
+    launch_pdl(k_gemm8_pair<T, true>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
+  return launched();
 }
 
 }  // namespace
 
 cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
   if (M <= 0) return cudaSuccess;
-  const dim3 grid((N + 127) / 128, (M + 31) / 32);
-  if (grid.y > 65535) return cudaErrorInvalidValue;
-  if (dt == F32)
-    k_gemm8<float><<<grid, 256, 0, s>>>(M, N, K, g);
-  else
-    k_gemm8<bf16><<<grid, 256, 0, s>>>(M, N, K, g);
-  return launched();
+  if (!init_driver()) return cudaErrorNotSupported;
+  return dt == F32 ? gemm8_t<float>(M, N, K, g, s) : gemm8_t<bf16>(M, N, K, g, s);
 }
 
 }  // namespace ff
