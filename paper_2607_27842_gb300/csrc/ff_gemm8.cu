@@ -16,6 +16,7 @@
 #include <cudaTypedefs.h>
 
 #include <mutex>
+#include <type_traits>
 
 namespace ff {
 
@@ -27,30 +28,46 @@ __device__ unsigned int g_watchdog8;
 
 constexpr int BK = 128;   // one scale block, one 128-byte swizzled row of a stage
 
+// Bounded wait: polls, and looks at the clock and the abort flag once in 256 polls
+// only (reading the global timer takes long).  Written out at each use: a call would
+// spill the epilogue's sums.
 __device__ __forceinline__ bool wait_poll(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
-  return mbar_wait<true>(b, parity, abort_flag, &g_watchdog8);
-}
-// every lane waits, the vote keeps the loop around it warp-uniform
-__device__ __forceinline__ bool wait_warp(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
-  const bool ok = mbar_test(b, parity) || wait_poll(b, parity, abort_flag);
-  return __all_sync(0xffffffffu, ok);
-}
-
-// the same without a call: the epilogue warps hold 128 sums in registers meanwhile
-__device__ __forceinline__ bool wait_inline(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
-  if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
-  const unsigned long long t0 = gtimer();
-  for (;;) {
+  unsigned long long t0 = 0;
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
-    const bool late = *abort_flag || gtimer() - t0 > WAIT_LIMIT_NS;
-    if (__any_sync(0xffffffffu, late)) {
-      *abort_flag = 1;
-      atomicOr(&g_watchdog8, 1u);
-      return false;
+  for (uint32_t i = 1;; ++i) {
+    if (mbar_test(b, parity)) return true;
+    if ((i & 255) == 0) {
+      if (i == 256) t0 = gtimer();
+      if (*abort_flag || gtimer() - t0 > WAIT_LIMIT_NS) {
+        *abort_flag = 1;
+        atomicOr(&g_watchdog8, 1u);
+        return false;
+      }
     }
   }
+}
+// every lane waits, the vote keeps the code around it warp-uniform
+__device__ __forceinline__ bool wait_warp(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait_poll(b, parity, abort_flag));
+}
+// the same, suspended in hardware between looks, for waits that the polls of others
+// would slow down (both hand-overs of TMEM: 8192 x 8192 x 8192 474 us polled, 454)
+__device__ __forceinline__ bool wait_try(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  unsigned long long t0 = 0;
+  bool ok = mbar_try(b, parity);
+#pragma unroll 1
+  for (uint32_t i = 1; !ok; ++i) {
+    ok = mbar_try(b, parity);
+    if (!ok && (i & 15) == 0) {
+      if (i == 16) t0 = gtimer();
+      if (*abort_flag || gtimer() - t0 > WAIT_LIMIT_NS) {
+        *abort_flag = 1;
+        atomicOr(&g_watchdog8, 1u);
+        break;
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
 }
 
 // instruction descriptor, kind::f8f6f4: D fp32 (bit 4), A and B e4m3 (0 at bits 7
@@ -62,6 +79,34 @@ __device__ __forceinline__ void umma8_pair(uint32_t d_tmem, uint64_t a, uint64_t
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(
           d_tmem),
       "l"(a), "l"(b), "r"(idesc), "r"(accum));
+}
+
+// 64 consecutive TMEM columns of this warp's lanes, read when it returns
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, "
+      "%38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, "
+      "%60, %61, %62, %63}, [%64];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
+        "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
+        "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+        "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
+        "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+}
+
+// Arrival on an mbarrier of either CTA of a pair that only says that TMEM has been
+// read (tcgen05.wait::ld and the tcgen05 fence are behind it): nothing in memory is
+// handed over, so it is relaxed.  A release at cluster scope waited for the
+// thread's stores every time: 8192 x 8192 x 8192 1133 us with it, 595 without.
+__device__ __forceinline__ void arrive_read(uint32_t bar_cluster) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
 }
 
 // GELU (tanh form) of four values: x (1 + tanh u) / 2 = x / (1 + 2^t), t = -2 u
@@ -86,6 +131,12 @@ __device__ __forceinline__ void gelu4(float& a, float& b, float& c, float& d) {
   b *= rab * e[0];
   c *= rcd * e[3];
   d *= rcd * e[2];
+}
+
+__device__ __forceinline__ float gelu1(float x) {
+  float y = x, z[3] = {0.f, 0.f, 0.f};
+  gelu4(y, z[0], z[1], z[2]);
+  return y;
 }
 
 // ---------------------------------------------------------------------------
@@ -203,7 +254,7 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
   }
   constexpr int PER = 128 / (int)sizeof(T);   // columns of a block
   constexpr int V = 16 / (int)sizeof(T);
-  if ((flags & RESID_TMA) && !wait_inline(rbar, rph, abort_flag)) return false;
+  if ((flags & RESID_TMA) && !wait_warp(rbar, rph, abort_flag)) return false;
 #pragma unroll
   for (int c = 0; c < 128; c += PER) {
     if (n0 + c >= N) break;
@@ -342,11 +393,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
         for (int kb = 0; kb < num_kb; ++kb, ++it) {
           const int s = it % P_STAGES;
           const uint32_t buf = it & 1;
-          if (!wait_warp(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag) ||
-              !wait_warp(&full[s], (it / P_STAGES) & 1, abort_flag)) { ok = false; break; }
-          tc_fence_after();
+          // the buffer comes last: it is what the next products wait for
           const uint32_t st = saddr(smem + s * P_STAGE_BYTES);
           const uint64_t ad = sw128_desc(st), wd = sw128_desc(st + 128 * BK);
+          if (!wait_warp(&full[s], (it / P_STAGES) & 1, abort_flag) ||
+              !wait_try(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // 32 bytes along K inside the swizzle atom
@@ -362,6 +414,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
     const int q = warp & 3, h = (warp - 4) >> 2;
     uint8_t* blk = epi + (warp - 4) * 8192;
     const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 128);
+    const uint32_t tempty0 = map_to(tempty, 0);
     uint32_t it = 0, rph = 0;
     for (int tile = pair; tile < num_tiles; tile += npairs) {
       int mb, nb;
@@ -394,25 +447,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
           a1 = sa[(kb + 2) * g.ldsa];
           w1 = sw[kb + 2];
         }
-        if (!wait_inline(&tfull[buf], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+        if (!wait_try(&tfull[buf], (it >> 1) & 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
         if (live) {
           const f32x2 ff = f2u(f, f);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float p[32];
-            tmem_ld32(tq + buf * 256 + c * 32, p);
-            if (c == 3) {   // the buffer is read: the MMA warp may fill it again
+          for (int c = 0; c < 2; ++c) {
+            uint32_t p[64];
+            tmem_ld64(tq + buf * 256 + c * 64, p);
+            if (c == 1) {   // the buffer is read: the MMA warp may fill it again
               tc_fence_before();
-              if (lane == 0) mbar_arrive_cluster(map_to(&tempty[buf], 0));
+              if (lane == 0) arrive_read(tempty0 + 8 * buf);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c * 16 + i] = ffma2(f2u(p[2 * i], p[2 * i + 1]), ff, acc[c * 16 + i]);
+            for (int i = 0; i < 32; ++i)
+              acc[c * 32 + i] = ffma2((f32x2)p[2 * i] | (f32x2)p[2 * i + 1] << 32, ff, acc[c * 32 + i]);
           }
         } else {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to(&tempty[buf], 0));
+          if (lane == 0) arrive_read(tempty0 + 8 * buf);
         }
       }
       if (live) {
@@ -445,6 +499,252 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
 }
 
 // ---------------------------------------------------------------------------
+// Few rows of A: the product transposed.  128 rows of W are the M side of the
+// products, BT rows of A (16 to 128) their N side, and the blocks of K are shared out
+// to the S CTAs of a cluster, so that a handful of rows still reads W on every SM.
+// A thread holds one row of W for BT / 2 rows of A; the scales' products are the same
+// for all of them and come from shared memory.  The cluster's partial sums meet in
+// shared memory: CTA r adds up and finishes the r-th share of the tile's rows of A, in
+// the order of the CTAs (the same bits every time).
+//   warp 0 TMA producer, warp 1 MMA issuer, warps 2-9 epilogue: TMEM lane quarter
+//   warp % 4, half of the BT columns (warp - 2) / 4
+// ---------------------------------------------------------------------------
+constexpr int S_THREADS = 320;
+constexpr int S_TABLE = 32;   // blocks of K whose scales are in shared memory at a time
+template <int BT> struct SCfg {
+  static constexpr int STAGES = BT == 16 ? 5 : 4;
+  static constexpr uint32_t STAGE_BYTES = (128 + BT) * BK;
+  static constexpr uint32_t PART_BYTES = BT * 512;   // the tile in fp32
+  // up to 32 rows the partial sums have a place of their own, above it they take the
+  // ring's (with a cluster barrier more, until all are done with theirs)
+  static constexpr bool OWN = BT <= 32;
+  static constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + (OWN ? PART_BYTES : 0) + S_TABLE * BT * 4 + 8 * BT * 4 + 256;
+};
+
+__device__ __forceinline__ void umma8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(
+          d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(accum));
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+}
+template <int C> __device__ __forceinline__ void tmem_read(uint32_t taddr, uint32_t (&r)[C]) {
+  if constexpr (C == 64) tmem_ld64(taddr, r);
+  else if constexpr (C == 8) tmem_ld8(taddr, r);
+  else {
+    float v[C];
+    if constexpr (C == 32) tmem_ld32(taddr, v); else tmem_ld16(taddr, v);
+#pragma unroll
+    for (int i = 0; i < C; ++i) r[i] = __float_as_uint(v[i]);
+  }
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <class T, bool Q8, int BT>
+__global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
+    k_gemm8_split(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, int M, int N, int K,
+                  int S, const __grid_constant__ Gemm8Args g) {
+  using C = SCfg<BT>;
+  constexpr int CT = BT / 2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  float* table = reinterpret_cast<float*>(smem + C::STAGES * C::STAGE_BYTES);   // [S_TABLE][BT]
+  uint32_t* red = reinterpret_cast<uint32_t*>(table + S_TABLE * BT);             // [warp][row of A]
+  uint64_t* full = reinterpret_cast<uint64_t*>(red + 8 * BT);
+  uint64_t* empty = full + C::STAGES;
+  uint64_t* tfull = empty + C::STAGES;
+  uint64_t* tempty = tfull + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* part = C::OWN ? reinterpret_cast<float*>(tmem_slot + 4) : reinterpret_cast<float*>(smem);   // [S][BT / S][128]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = S > 1 ? (int)cluster_rank() : 0;
+  const int tile = blockIdx.x / S, num_a = (M + BT - 1) / BT;
+  const int n0 = tile / num_a * 128, m0 = tile % num_a * BT;
+  const int num_kb = (K + BK - 1) / BK;
+  const int kb0 = (int)((long long)num_kb * rank / S), kb1 = (int)((long long)num_kb * (rank + 1) / S);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int b = 0; b < 4; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 8);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tmA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tmW) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(tmem_slot)), "r"(4 * BT)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  if (C::OWN && S > 1) cluster_arrive();
+  pdl_trigger();
+  pdl_wait();
+
+  const int q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane;
+  f32x2 acc[CT / 2];
+#pragma unroll
+  for (int i = 0; i < CT / 2; ++i) acc[i] = 0;
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int s = it % C::STAGES;
+        if (!wait_poll(&empty[s], ((it / C::STAGES) & 1) ^ 1, abort_flag)) break;
+        mbar_expect_tx(&full[s], C::STAGE_BYTES);
+        uint8_t* st = smem + s * C::STAGE_BYTES;
+        tma_load(&tmW, &full[s], st, kb * BK, n0);
+        tma_load(&tmA, &full[s], st + 128 * BK, kb * BK, m0);
+      }
+      for (uint32_t k = 0; k < (uint32_t)C::STAGES && k < it; ++k) {   // no copy may land after the CTA exits
+        const uint32_t j = it - 1 - k;
+        const unsigned long long t0 = gtimer();
+        while (!mbar_try(&full[j % C::STAGES], (j / C::STAGES) & 1))
+          if (gtimer() - t0 > WAIT_LIMIT_NS) { atomicOr(&g_watchdog8, 2u); break; }
+      }
+    }
+  } else if (warp == 1) {
+    uint32_t it = 0;
+    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+      const int s = it % C::STAGES;
+      const uint32_t buf = it & 3, st = saddr(smem + s * C::STAGE_BYTES);
+      const uint64_t wd = sw128_desc(st), ad = sw128_desc(st + 128 * BK);
+      if (!wait_warp(&tempty[buf], ((it >> 2) & 1) ^ 1, abort_flag) ||
+          !wait_warp(&full[s], (it / C::STAGES) & 1, abort_flag)) break;
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma8(tmem_base + buf * BT, wd + 2 * k, ad + 2 * k, idesc8(128, BT), k != 0);
+        umma_commit(&tfull[buf]);
+        umma_commit(&empty[s]);
+      }
+    }
+  } else {
+    const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * CT);
+    const float* sw = g.sw + (n0 >> 7) * g.ldsw;
+    uint32_t it = 0;
+    bool ok = true;   // (after a wait that gave up the loop still meets the others at its barriers)
+    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+      if (it % S_TABLE == 0) {   // the scales' products of the next blocks of K
+        if (it) epi_barrier();
+        for (int i = threadIdx.x - 64; i < min(S_TABLE, kb1 - kb) * BT; i += 256) {
+          const int b = kb + i / BT, m = m0 + i % BT;
+          table[i] = m < M ? g.sa[b * g.ldsa + m] * sw[b] : 0.f;
+        }
+        epi_barrier();
+      }
+      const uint32_t buf = it & 3;
+      ok = ok && wait_warp(&tfull[buf], (it >> 2) & 1, abort_flag);
+      if (!ok) continue;
+      tc_fence_after();
+      uint32_t p[CT];
+      tmem_read<CT>(tq + buf * BT, p);
+      tc_fence_before();
+      if (lane == 0) mbar_arrive(&tempty[buf]);
+      const float* f = table + it % S_TABLE * BT + h * CT;
+#pragma unroll
+      for (int i = 0; i < CT; i += 4) {
+        const ulonglong2 f2 = *reinterpret_cast<const ulonglong2*>(f + i);
+        acc[i / 2] = ffma2((f32x2)p[i] | (f32x2)p[i + 1] << 32, f2.x, acc[i / 2]);
+        acc[i / 2 + 1] = ffma2((f32x2)p[i + 2] | (f32x2)p[i + 3] << 32, f2.y, acc[i / 2 + 1]);
+      }
+    }
+  }
+  // partial sums to the CTA that finishes their rows of A: part[CTA][row of A][row of W]
+  const int share = BT / S;
+  __syncwarp();
+  if (S == 1) {
+    __syncthreads();
+  } else {
+    if (!C::OWN) cluster_arrive();   // (with OWN: every CTA of the cluster has started, above)
+    cluster_wait();
+  }
+  if (warp >= 2) {
+    const uint32_t at = saddr(part);
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+      const int t = h * CT + i, to = t / share;
+      const float v = i & 1 ? hi_f(acc[i / 2]) : lo_f(acc[i / 2]);
+      const int off = (rank * share + t - to * share) * 128 + row;
+      if (S == 1) {
+        part[off] = v;
+      } else {
+        uint32_t a;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at + 4 * off), "r"(to));
+        st_cluster(a, v);
+      }
+    }
+  }
+  __syncwarp();
+  if (S > 1) cluster_sync_all(); else __syncthreads();
+  if (warp >= 2) {
+    const int n = n0 + row, mine = share / 2, t0 = h * mine;   // this half's rows of A: t0 .. t0 + mine - 1 of the share
+    const int mb = m0 + rank * share + t0;
+    const float bias = g.bias && n < N ? to_f(reinterpret_cast<const T*>(g.bias)[n]) : 0.f;
+#pragma unroll 4
+    for (int t = 0; t < mine; ++t) {
+      const int m = mb + t;
+      float* const p = part + (t0 + t) * 128 + row;
+      float y = p[0];
+      for (int s = 1; s < S; ++s) y += p[s * share * 128];
+      y += bias;
+      if (g.act) y = gelu1(y);
+      if constexpr (Q8) {
+        if (n >= N) y = 0.f;
+        p[0] = y;
+        const uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(y));
+        if (lane == 0) red[(t0 + t) * 4 + q] = mx;
+      } else if (m < M && n < N) {
+        if (g.gate) y *= g.gate[(long long)(m / g.rpb) * g.gate_stride + n];
+        if (g.resid) y += to_f(reinterpret_cast<const T*>(g.resid)[m * g.ldr + n]);
+        reinterpret_cast<T*>(g.out)[m * g.ldo + n] = from_f<T>(y);
+      }
+    }
+    if constexpr (Q8) {
+      epi_barrier();
+#pragma unroll 4
+      for (int t = 0; t < mine; ++t) {
+        const int m = mb + t;
+        const uint4 r = *reinterpret_cast<const uint4*>(red + (t0 + t) * 4);
+        const float sc = q8_scale(max(max(r.x, r.y), max(r.z, r.w)));
+        if (m < M && n < N) {
+          reinterpret_cast<uint8_t*>(g.q8.q)[m * g.q8.ldq + n] = (uint8_t)to_e4m3x2(part[(t0 + t) * 128 + row] * (1.f / sc), 0.f);
+          if (row == 0) g.q8.scale[(n0 >> 7) * g.q8.lds + m] = sc;
+        }
+      }
+    }
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(4 * BT) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
@@ -465,10 +765,19 @@ bool init_driver() {
     auto smem = [](const void* fn, size_t bytes) {
       cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     };
-    smem((const void*)k_gemm8_pair<float, false>, P_SMEM);
-    smem((const void*)k_gemm8_pair<float, true>, P_SMEM);
-    smem((const void*)k_gemm8_pair<bf16, false>, P_SMEM);
-    smem((const void*)k_gemm8_pair<bf16, true>, P_SMEM);
+    auto both = [&](auto t, auto q8) {
+      using T = decltype(t);
+      constexpr bool Q8 = decltype(q8)::value;
+      smem((const void*)k_gemm8_pair<T, Q8>, P_SMEM);
+      smem((const void*)k_gemm8_split<T, Q8, 16>, SCfg<16>::SMEM);
+      smem((const void*)k_gemm8_split<T, Q8, 32>, SCfg<32>::SMEM);
+      smem((const void*)k_gemm8_split<T, Q8, 64>, SCfg<64>::SMEM);
+      smem((const void*)k_gemm8_split<T, Q8, 128>, SCfg<128>::SMEM);
+    };
+    both(0.f, std::false_type());
+    both(0.f, std::true_type());
+    both(bf16(), std::false_type());
+    both(bf16(), std::true_type());
   });
   return g_encode != nullptr;
 }
@@ -488,15 +797,38 @@ bool make_map8(CUtensorMap* m, const void* base, int es, long long rows, long lo
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T>
-cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
+template <class T, bool Q8, int BT>
+cudaError_t launch_split(int M, int N, int K, int S, const Gemm8Args& g, cudaStream_t s) {
+  CUtensorMap ma, mw;
+  if (!make_map8(&ma, g.a, 1, M, K, g.lda, BT) || !make_map8(&mw, g.w, 1, N, K, g.ldw, 128)) return cudaErrorInvalidValue;
+  const long long grid = (long long)S * ((N + 127) / 128) * ((M + BT - 1) / BT);
+  if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(S_THREADS);
+  cfg.dynamicSmemBytes = SCfg<BT>::SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)S;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_gemm8_split<T, Q8, BT>, ma, mw, M, N, K, S, g);
+  return e != cudaSuccess ? e : launched();
+}
+
+template <class T, bool Q8>
+cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
   constexpr int es = (int)sizeof(T);
   CUtensorMap ma, mw, mo, mr;
   if (!make_map8(&ma, g.a, 1, M, K, g.lda, 128) || !make_map8(&mw, g.w, 1, N, K, g.ldw, 128))
     return cudaErrorInvalidValue;
   mo = mr = ma;
   int flags = 0;
-  if (!g.out) {
+  if (Q8) {
     if (!make_map8(&mo, g.q8.q, 1, M, N, g.q8.ldq, 32)) return cudaErrorInvalidValue;
     flags = STAGED;
   } else if (!((uintptr_t)g.out & 15) && g.ldo * es % 16 == 0 && make_map8(&mo, g.out, es, M, N, g.ldo, 32)) {
@@ -508,11 +840,48 @@ cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
   const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
   if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
   const int pairs = g_sms / 2, grid = 2 * (int)(tiles < pairs ? tiles : pairs);
-  if (g.out)
-    launch_pdl(k_gemm8_pair<T, false>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
-  else
-    launch_pdl(k_gemm8_pair<T, true>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
-  return launched();
+  const cudaError_t e = launch_pdl(k_gemm8_pair<T, Q8>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
+  return e != cudaSuccess ? e : launched();
+}
+
+// The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster, by
+// the estimated time in clocks (CTAs in waves over the SMs; a block of K, then what a
+// tile costs beside them).
+struct Plan {
+  int bt, s;   // bt 0: CTA pairs
+};
+Plan plan8(int M, int N, int K) {
+  const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
+  const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
+  Plan best = {0, 1};
+  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (900.0 * kb + 3500) + 3000;
+  const int bts[4] = {16, 32, 64, 128};
+  const double per_kb[4] = {330, 360, 450, 650}, fixed[4] = {2500, 2700, 3000, 4000};
+  for (int i = 0; i < 4; ++i) {
+    if (i > 0 && bts[i - 1] >= M) break;
+    const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
+    for (int s = 1; s <= 8 && s <= kb; s *= 2) {
+      const double waves = (double)((tiles * s + g_sms - 1) / g_sms);
+      const double t = waves * (per_kb[i] * ((kb + s - 1) / s) + fixed[i]) + 3000 + (s > 1 ? 800 : 0);
+      if (t < least) {
+        least = t;
+        best = {bts[i], s};
+      }
+    }
+  }
+  return best;
+}
+
+template <class T, bool Q8>
+cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
+  const Plan p = plan8(M, N, K);
+  switch (p.bt) {
+    case 16: return launch_split<T, Q8, 16>(M, N, K, p.s, g, s);
+    case 32: return launch_split<T, Q8, 32>(M, N, K, p.s, g, s);
+    case 64: return launch_split<T, Q8, 64>(M, N, K, p.s, g, s);
+    case 128: return launch_split<T, Q8, 128>(M, N, K, p.s, g, s);
+    default: return launch_pair<T, Q8>(M, N, K, g, s);
+  }
 }
 
 }  // namespace
@@ -520,7 +889,8 @@ cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
 cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
   if (M <= 0) return cudaSuccess;
   if (!init_driver()) return cudaErrorNotSupported;
-  return dt == F32 ? gemm8_t<float>(M, N, K, g, s) : gemm8_t<bf16>(M, N, K, g, s);
+  if (dt == F32) return g.out ? gemm8_t<float, false>(M, N, K, g, s) : gemm8_t<float, true>(M, N, K, g, s);
+  return g.out ? gemm8_t<bf16, false>(M, N, K, g, s) : gemm8_t<bf16, true>(M, N, K, g, s);
 }
 
 }  // namespace ff
