@@ -50,24 +50,25 @@ __device__ __forceinline__ bool wait_poll(uint64_t* b, uint32_t parity, volatile
 __device__ __forceinline__ bool wait_warp(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, wait_poll(b, parity, abort_flag));
 }
-// the same, suspended in hardware between looks, for waits that the polls of others
-// would slow down (both hand-overs of TMEM: 8192 x 8192 x 8192 474 us polled, 454)
+// The hand-overs of TMEM, on which every block of K waits twice: try_wait suspends the
+// warp between looks, so its polls are not in the way of the other warps', and the loop
+// is as short as it gets, for the code around it competes for the instruction cache.
+// 40000 looks of at most 0.1 ms are the same 4 s.  (8192 x 8192 x 8192: 520 us with the
+// polls above, 494 with this.)
 __device__ __forceinline__ bool wait_try(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
-  unsigned long long t0 = 0;
-  bool ok = mbar_try(b, parity);
-#pragma unroll 1
-  for (uint32_t i = 1; !ok; ++i) {
-    ok = mbar_try(b, parity);
-    if (!ok && (i & 15) == 0) {
-      if (i == 16) t0 = gtimer();
-      if (*abort_flag || gtimer() - t0 > WAIT_LIMIT_NS) {
-        *abort_flag = 1;
-        atomicOr(&g_watchdog8, 1u);
-        break;
-      }
-    }
-  }
-  return __all_sync(0xffffffffu, ok);
+  uint32_t n;
+  asm volatile(
+      "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, 40000;\n"
+      "LOOP_%=:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n @p bra DONE_%=;\n"
+      " sub.u32 n, n, 1;\n setp.ne.u32 q, n, 0;\n @q bra LOOP_%=;\n"
+      "DONE_%=:\n mov.u32 %0, n;\n}\n"
+      : "=r"(n)
+      : "r"(saddr(b)), "r"(parity), "r"(100000u)
+      : "memory");
+  if (!__any_sync(0xffffffffu, n == 0)) return true;
+  *abort_flag = 1;
+  atomicOr(&g_watchdog8, 1u);
+  return false;
 }
 
 // instruction descriptor, kind::f8f6f4: D fp32 (bit 4), A and B e4m3 (0 at bits 7
@@ -133,12 +134,6 @@ __device__ __forceinline__ void gelu4(float& a, float& b, float& c, float& d) {
   d *= rcd * e[2];
 }
 
-__device__ __forceinline__ float gelu1(float x) {
-  float y = x, z[3] = {0.f, 0.f, 0.f};
-  gelu4(y, z[0], z[1], z[2]);
-  return y;
-}
-
 // ---------------------------------------------------------------------------
 // CTA pairs: 256 x 256 tiles of the result, persistent.  Each CTA stages its own
 // 128 rows of A and 128 of the tile's rows of W (32 KB a block of K) and
@@ -151,42 +146,85 @@ __device__ __forceinline__ float gelu1(float x) {
 // which hold sums.
 // ---------------------------------------------------------------------------
 constexpr int P_THREADS = 384;
-constexpr int P_STAGES = 5;
+constexpr int P_STAGES = 4;
 constexpr uint32_t P_STAGE_BYTES = 2 * 128 * BK;
 constexpr uint32_t P_EPI_BYTES = 8 * 8192;   // 8 KB of output blocks to an epilogue warp
-constexpr size_t P_SMEM = 1024 + (size_t)P_STAGES * P_STAGE_BYTES + P_EPI_BYTES + 256;
+constexpr uint32_t P_CONST_BYTES = 3 * 128 * 4;   // a warp's columns: bias, gate of its first and last row
+constexpr size_t P_SMEM = 1024 + (size_t)P_STAGES * P_STAGE_BYTES + P_EPI_BYTES + 8 * P_CONST_BYTES + 256;
 
 // 128-byte-swizzled block of 32 rows: 16-byte chunk k of row r
 __device__ __forceinline__ uint32_t sw128_off(int r, int k) { return (uint32_t)(r * 128 + ((k ^ (r & 7)) << 4)); }
 
 enum { STAGED = 1, RESID_TMA = 2 };
 
-// bias, gate and residual of 32 adjacent columns n0.. of row m, or 8-bit output: y in
-// place of the sums.  Columns past N: y of a zero sum, never stored.
+// Bias and gate of a warp's 128 columns, on their way into shared memory (cp.async)
+// while the sums are formed, not read behind the last product (4096 x 1152 x 4608 with
+// gate and residual 53.5 -> 48.4 us).
 template <class T>
-__device__ __forceinline__ void finish32(const Gemm8Args& g, int m, int n0, int N, float (&y)[32]) {
-  const T* bias = reinterpret_cast<const T*>(g.bias);
-  if (bias) {
+__device__ __forceinline__ void consts_in(const Gemm8Args& g, uint8_t* cst, int row0, int n0, int M, int N, int lane) {
+  if (g.bias) {
+    const T* bias = reinterpret_cast<const T*>(g.bias) + n0;
+    if (!((uintptr_t)bias & 3)) {
+      constexpr int E = 4 / (int)sizeof(T);
+      for (int i = lane; i < 128 / E; i += 32)
+        cp_async4(cst + 4 * i, n0 + E * i < N ? bias + E * i : bias, max(0, min(4, (N - n0 - E * i) * (int)sizeof(T))));
+    } else {
+      for (int i = lane; i < 128; i += 32) reinterpret_cast<T*>(cst)[i] = n0 + i < N ? bias[i] : from_f<T>(0.f);
+    }
+  }
+  if (g.gate) {
+    const float* lo = g.gate + (long long)(row0 / g.rpb) * g.gate_stride + n0;
+    const float* hi = g.gate + (long long)(min(row0 + 31, M - 1) / g.rpb) * g.gate_stride + n0;
+    for (int i = lane; i < 128; i += 32) {
+      const bool in = n0 + i < N;
+      cp_async4(cst + 512 + 4 * i, in ? lo + i : lo, in ? 4 : 0);
+      cp_async4(cst + 1024 + 4 * i, in ? hi + i : hi, in ? 4 : 0);
+    }
+  }
+  cp_commit();
+}
+
+// bias, GELU and gate of a row's columns n0 + c .. n0 + c + 31.  `gate`: the row's 128
+// columns in shared memory, or null where the warp's rows have more than two samples
+// (fewer than 32 rows to one).
+template <class T>
+__device__ __forceinline__ void finish32(const Gemm8Args& g, const uint8_t* cst, const float* gate, int m, int n0, int c,
+                                         int N, float (&y)[32]) {
+  if (g.bias) {
+    constexpr int V = 16 / (int)sizeof(T);
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (n0 + j < N) y[j] += to_f(bias[n0 + j]);
+    for (int j = 0; j < 32; j += V) {
+      float b[V];
+      ld16(reinterpret_cast<const T*>(cst) + c + j, b);
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[j + i] += b[i];
+    }
   }
   if (g.act) {
 #pragma unroll
     for (int j = 0; j < 32; j += 4) gelu4(y[j], y[j + 1], y[j + 2], y[j + 3]);
   }
   if (g.gate) {
-    const float* gp = g.gate + (long long)(m / g.rpb) * g.gate_stride + n0;
+    const float* gp = g.gate + (long long)(m / g.rpb) * g.gate_stride + n0 + c;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (n0 + j < N) y[j] *= gp[j];
+    for (int j = 0; j < 32; j += 4) {
+      float f[4];
+      if (gate) {
+        ld16(gate + c + j, f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = n0 + c + j + i < N ? gp[j + i] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[j + i] *= f[i];
+    }
   }
 }
 
 // A warp's block of 32 rows of 128 bytes between shared memory and row-major global
 // memory, coalesced, element by element: for rows that TMA cannot take.
 template <class T>
-__device__ __forceinline__ void block_in(uint8_t* b, const T* src, long long ld, int rows, int cols, int lane) {
+__device__ __noinline__ void block_in(uint8_t* b, const T* src, long long ld, int rows, int cols, int lane) {
 #pragma unroll 4
   for (int r = 0; r < min(rows, 32); ++r)
 #pragma unroll
@@ -195,7 +233,7 @@ __device__ __forceinline__ void block_in(uint8_t* b, const T* src, long long ld,
         *reinterpret_cast<T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16) = src[r * ld + j];
 }
 template <class T>
-__device__ __forceinline__ void block_out(const uint8_t* b, T* dst, long long ld, int rows, int cols, int lane) {
+__device__ __noinline__ void block_out(const uint8_t* b, T* dst, long long ld, int rows, int cols, int lane) {
 #pragma unroll 4
   for (int r = 0; r < min(rows, 32); ++r)
 #pragma unroll
@@ -209,10 +247,14 @@ __device__ __forceinline__ void block_out(const uint8_t* b, T* dst, long long ld
 // do not end on 16 bytes leave their last tile through block_out.
 template <class T, bool Q8>
 __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const CUtensorMap* tmO, float (&acc)[128], int row0,
-                                           int lane, int n0, int M, int N, uint8_t* blk, uint64_t* rbar, uint32_t rph,
-                                           volatile int* abort_flag) {
+                                           int lane, int n0, int M, int N, uint8_t* blk, const uint8_t* cst, uint64_t* rbar,
+                                           uint32_t rph, volatile int* abort_flag) {
+  cp_wait<0>();
+  __syncwarp();
   const int m = min(row0 + lane, M - 1);   // (rows past M repeat the last one and are not stored)
   const int es = Q8 ? 1 : (int)sizeof(T);
+  const int b_lo = row0 / g.rpb, b_hi = min(row0 + 31, M - 1) / g.rpb;
+  const float* gate = b_hi - b_lo > 1 ? nullptr : reinterpret_cast<const float*>(cst + (m / g.rpb == b_lo ? 512 : 1024));
   const bool tma = (flags & STAGED) && (n0 + 128 <= N || (long long)N * es % 16 == 0);
   if constexpr (Q8) {
     uint32_t mx = 0;
@@ -221,9 +263,10 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
       float y[32];
 #pragma unroll
       for (int j = 0; j < 32; ++j) y[j] = acc[c + j];
-      finish32<T>(g, m, n0 + c, N, y);
+      finish32<T>(g, cst, gate, m, n0, c, N, y);
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
+        if (n0 + c + j >= N) y[j] = 0.f;
         mx = max(mx, abs_bits(y[j]));
         acc[c + j] = y[j];
       }
@@ -276,7 +319,7 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
       float y[32];
 #pragma unroll
       for (int j = 0; j < 32; ++j) y[j] = acc[c + d + j];
-      finish32<T>(g, m, n0 + c + d, N, y);
+      finish32<T>(g, cst, gate, m, n0, c + d, N, y);
 #pragma unroll
       for (int k = 0; k < 32 / V; ++k) {
         T* p = reinterpret_cast<T*>(b + sw128_off(lane, d / V + k));
@@ -317,7 +360,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* epi = smem + P_STAGES * P_STAGE_BYTES;
-  uint64_t* full = reinterpret_cast<uint64_t*>(epi + P_EPI_BYTES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(epi + P_EPI_BYTES + 8 * P_CONST_BYTES);
   uint64_t* empty = full + P_STAGES;
   uint64_t* tfull = empty + P_STAGES;
   uint64_t* tempty = tfull + 2;
@@ -413,6 +456,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     const int q = warp & 3, h = (warp - 4) >> 2;
     uint8_t* blk = epi + (warp - 4) * 8192;
+    uint8_t* cst = epi + P_EPI_BYTES + (warp - 4) * P_CONST_BYTES;
     const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 128);
     const uint32_t tempty0 = map_to(tempty, 0);
     uint32_t it = 0, rph = 0;
@@ -427,6 +471,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
         mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
         tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
         if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+      }
+      if (live) {
+        __syncwarp();   // the last tile's are read
+        consts_in<T>(g, cst, row0, n0, M, N, lane);
       }
       // scales of this row and of W's block of rows, two blocks of K ahead
       const bool in = live && row0 + lane < M;
@@ -477,7 +525,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
           y[2 * i + 1] = hi_f(acc[i]);
         }
         if (ok) {
-          ok = finish_row<T, Q8>(g, flags, &tmO, y, row0, lane, n0, M, N, blk, &rbar[warp - 4], rph, abort_flag);
+          ok = finish_row<T, Q8>(g, flags, &tmO, y, row0, lane, n0, M, N, blk, cst, &rbar[warp - 4], rph, abort_flag);
         } else if ((flags & RESID_TMA) && lane == 0) {   // its copies still land before the CTA exits
           const unsigned long long t0 = gtimer();
           while (!mbar_try(&rbar[warp - 4], rph))
@@ -512,7 +560,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
 constexpr int S_THREADS = 320;
 constexpr int S_TABLE = 32;   // blocks of K whose scales are in shared memory at a time
 template <int BT> struct SCfg {
-  static constexpr int STAGES = BT == 16 ? 5 : 4;
+  // two CTAs to an SM up to 64 rows (deeper rings with one CTA were slower, clusters of
+  // eight by half: 1 x 2048 x 8192 6.6 -> 12.4 us)
+  static constexpr int STAGES = BT == 16 || BT == 128 ? 5 : 4;
   static constexpr uint32_t STAGE_BYTES = (128 + BT) * BK;
   static constexpr uint32_t PART_BYTES = BT * 512;   // the tile in fp32
   // up to 32 rows the partial sums have a place of their own, above it they take the
@@ -627,14 +677,23 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
       }
     }
   } else if (warp == 1) {
+    // the loop's time is this warp's: both barriers are tested together, and the next
+    // block's behind this one's products
     uint32_t it = 0;
+    bool ready = false;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % C::STAGES;
       const uint32_t buf = it & 3, st = saddr(smem + s * C::STAGE_BYTES);
       const uint64_t wd = sw128_desc(st), ad = sw128_desc(st + 128 * BK);
-      if (!wait_warp(&tempty[buf], ((it >> 2) & 1) ^ 1, abort_flag) ||
-          !wait_warp(&full[s], (it / C::STAGES) & 1, abort_flag)) break;
+      if (!__all_sync(0xffffffffu, ready) && (!wait_warp(&tempty[buf], ((it >> 2) & 1) ^ 1, abort_flag) ||
+                                              !wait_warp(&full[s], (it / C::STAGES) & 1, abort_flag)))
+        break;
       tc_fence_after();
+      {
+        const uint32_t j = it + 1;
+        const bool t = mbar_test(&tempty[j & 3], ((j >> 2) & 1) ^ 1), f = mbar_test(&full[j % C::STAGES], (j / C::STAGES) & 1);
+        ready = t && f;
+      }
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -647,7 +706,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
     const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * CT);
     const float* sw = g.sw + (n0 >> 7) * g.ldsw;
     uint32_t it = 0;
-    bool ok = true;   // (after a wait that gave up the loop still meets the others at its barriers)
+    bool ok = true, ready = false;   // (after a wait that gave up the loop still meets the others at its barriers)
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       if (it % S_TABLE == 0) {   // the scales' products of the next blocks of K
         if (it) epi_barrier();
@@ -658,13 +717,14 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
         epi_barrier();
       }
       const uint32_t buf = it & 3;
-      ok = ok && wait_warp(&tfull[buf], (it >> 2) & 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ready)) ok = ok && wait_warp(&tfull[buf], (it >> 2) & 1, abort_flag);
       if (!ok) continue;
       tc_fence_after();
       uint32_t p[CT];
       tmem_read<CT>(tq + buf * BT, p);
       tc_fence_before();
       if (lane == 0) mbar_arrive(&tempty[buf]);
+      ready = mbar_test(&tfull[(it + 1) & 3], ((it + 1) >> 2) & 1);
       const float* f = table + it % S_TABLE * BT + h * CT;
 #pragma unroll
       for (int i = 0; i < CT; i += 4) {
@@ -675,7 +735,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
     }
   }
   // partial sums to the CTA that finishes their rows of A: part[CTA][row of A][row of W]
-  const int share = BT / S;
+  const int lshare = (BT == 128 ? 7 : BT == 64 ? 6 : BT == 32 ? 5 : 4) - (31 - __clz(S)), share = 1 << lshare;
   __syncwarp();
   if (S == 1) {
     __syncthreads();
@@ -684,17 +744,17 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
     cluster_wait();
   }
   if (warp >= 2) {
-    const uint32_t at = saddr(part);
+    const uint32_t at = saddr(part) + 4 * ((rank << lshare) * 128 + row);
 #pragma unroll
     for (int i = 0; i < CT; ++i) {
-      const int t = h * CT + i, to = t / share;
+      const int t = h * CT + i;
       const float v = i & 1 ? hi_f(acc[i / 2]) : lo_f(acc[i / 2]);
-      const int off = (rank * share + t - to * share) * 128 + row;
+      const uint32_t to = at + (t & (share - 1)) * 512;
       if (S == 1) {
-        part[off] = v;
+        part[t * 128 + row] = v;
       } else {
         uint32_t a;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at + 4 * off), "r"(to));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(to), "r"(t >> lshare));
         st_cluster(a, v);
       }
     }
@@ -703,38 +763,58 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
   if (S > 1) cluster_sync_all(); else __syncthreads();
   if (warp >= 2) {
     const int n = n0 + row, mine = share / 2, t0 = h * mine;   // this half's rows of A: t0 .. t0 + mine - 1 of the share
-    const int mb = m0 + rank * share + t0;
+    const int mb = m0 + rank * share + t0, cnt = n < N ? min(mine, M - mb) : 0;
     const float bias = g.bias && n < N ? to_f(reinterpret_cast<const T*>(g.bias)[n]) : 0.f;
-#pragma unroll 4
-    for (int t = 0; t < mine; ++t) {
-      const int m = mb + t;
-      float* const p = part + (t0 + t) * 128 + row;
-      float y = p[0];
-      for (int s = 1; s < S; ++s) y += p[s * share * 128];
-      y += bias;
-      if (g.act) y = gelu1(y);
+    float* const pp = part + t0 * 128 + row;
+    constexpr int U = BT == 16 ? 4 : BT == 32 ? 8 : 16;   // rows of A at a time: their loads come first
+    for (int u = 0; u < mine; u += U) {
+      float y[U], gt[U], rs[U];
+      if (!Q8) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const bool in = u + i < cnt;
+          const long long m = mb + u + i;
+          gt[i] = g.gate && in ? g.gate[(int)m / g.rpb * g.gate_stride + n] : 1.f;
+          rs[i] = g.resid && in ? to_f(reinterpret_cast<const T*>(g.resid)[m * g.ldr + n]) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) y[i] = u + i < mine ? pp[(u + i) * 128] : 0.f;
+      for (int s = 1; s < S; ++s) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (u + i < mine) y[i] += pp[(u + i) * 128 + (s << lshare) * 128];
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) y[i] += bias;
+      if (g.act) {
+#pragma unroll
+        for (int i = 0; i < U; i += 4) gelu4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+      }
       if constexpr (Q8) {
-        if (n >= N) y = 0.f;
-        p[0] = y;
-        const uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(y));
-        if (lane == 0) red[(t0 + t) * 4 + q] = mx;
-      } else if (m < M && n < N) {
-        if (g.gate) y *= g.gate[(long long)(m / g.rpb) * g.gate_stride + n];
-        if (g.resid) y += to_f(reinterpret_cast<const T*>(g.resid)[m * g.ldr + n]);
-        reinterpret_cast<T*>(g.out)[m * g.ldo + n] = from_f<T>(y);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (u + i >= mine) break;
+          const float v = n < N ? y[i] : 0.f;
+          pp[(u + i) * 128] = v;
+          const uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(v));
+          if (lane == 0) red[(t0 + u + i) * 4 + q] = mx;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (u + i < cnt)
+            reinterpret_cast<T*>(g.out)[(long long)(mb + u + i) * g.ldo + n] = from_f<T>(y[i] * gt[i] + rs[i]);
       }
     }
     if constexpr (Q8) {
       epi_barrier();
 #pragma unroll 4
-      for (int t = 0; t < mine; ++t) {
-        const int m = mb + t;
+      for (int t = 0; t < cnt; ++t) {
         const uint4 r = *reinterpret_cast<const uint4*>(red + (t0 + t) * 4);
         const float sc = q8_scale(max(max(r.x, r.y), max(r.z, r.w)));
-        if (m < M && n < N) {
-          reinterpret_cast<uint8_t*>(g.q8.q)[m * g.q8.ldq + n] = (uint8_t)to_e4m3x2(part[(t0 + t) * 128 + row] * (1.f / sc), 0.f);
-          if (row == 0) g.q8.scale[(n0 >> 7) * g.q8.lds + m] = sc;
-        }
+        reinterpret_cast<uint8_t*>(g.q8.q)[(mb + t) * g.q8.ldq + n] = (uint8_t)to_e4m3x2(pp[t * 128] * (1.f / sc), 0.f);
+        if (row == 0) g.q8.scale[(n0 >> 7) * g.q8.lds + mb + t] = sc;
       }
     }
   }
@@ -844,9 +924,14 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
   return e != cudaSuccess ? e : launched();
 }
 
-// The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster, by
-// the estimated time in clocks (CTAs in waves over the SMs; a block of K, then what a
-// tile costs beside them).
+// The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster: the
+// least time of a model in us fitted to a sweep of both over M from 1 to 4096 (K of 512
+// to 8192): a tile's time is linear in its blocks of K, tiles run in waves over the SMs
+// (two CTAs of the split kernel to an SM up to 64 rows, each slower beside the other),
+// and the cluster's meeting costs more the larger it is.  Measured against the choice's
+// neighbours at 256 x 2048 x 8192: pairs 34 us, 128 rows and 4 CTAs 16.2, 32 rows and 2
+// CTAs 17.0; 512 x 2048 x 2048: pairs 14.6, 32 rows 10.7, 128 rows and 2 CTAs 13.0; from
+// 1024 x 2048 x 2048 (14.8 and 16.1) pairs are the faster.
 struct Plan {
   int bt, s;   // bt 0: CTA pairs
 };
@@ -854,18 +939,21 @@ Plan plan8(int M, int N, int K) {
   const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
-  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (900.0 * kb + 3500) + 3000;
+  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.42 * kb + 3.6) + 3.6;
   const int bts[4] = {16, 32, 64, 128};
-  const double per_kb[4] = {330, 360, 450, 650}, fixed[4] = {2500, 2700, 3000, 4000};
+  const double one[4] = {0.235, 0.29, 0.36, 0.49}, two[4] = {0.30, 0.40, 0.63, 0.49}, fixed[4] = {1.6, 2.2, 3.3, 7.0};
+  const double meet[4] = {0, 0.3, 0.6, 1.2};
   for (int i = 0; i < 4; ++i) {
     if (i > 0 && bts[i - 1] >= M) break;
     const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
-    for (int s = 1; s <= 8 && s <= kb; s *= 2) {
-      const double waves = (double)((tiles * s + g_sms - 1) / g_sms);
-      const double t = waves * (per_kb[i] * ((kb + s - 1) / s) + fixed[i]) + 3000 + (s > 1 ? 800 : 0);
+    for (int l = 0; l < 4 && (1 << l) <= kb; ++l) {
+      const long long ctas = tiles << l, room = (long long)g_sms * (bts[i] <= 64 ? 2 : 1);
+      const bool shared = bts[i] <= 64 && ctas > g_sms;
+      const double t = (double)((ctas + room - 1) / room) * ((shared ? two : one)[i] * (double)((kb + (1 << l) - 1) >> l) + fixed[i]) +
+                       2.0 + meet[l] + (shared ? 0.5 : 0.0);
       if (t < least) {
         least = t;
-        best = {bts[i], s};
+        best = {bts[i], 1 << l};
       }
     }
   }
