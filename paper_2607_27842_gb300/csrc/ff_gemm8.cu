@@ -271,7 +271,7 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
         acc[c + j] = y[j];
       }
     }
-    const float s = q8_scale(mx), inv = 1.f / s;
+    const float s = q8_scale(mx), inv = q8_inv(s);
     if (row0 + lane < M) g.q8.scale[(n0 >> 7) * g.q8.lds + m] = s;
     if (lane == 0) bulk_wait_read<0>();
     __syncwarp();
@@ -813,7 +813,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
       for (int t = 0; t < cnt; ++t) {
         const uint4 r = *reinterpret_cast<const uint4*>(red + (t0 + t) * 4);
         const float sc = q8_scale(max(max(r.x, r.y), max(r.z, r.w)));
-        reinterpret_cast<uint8_t*>(g.q8.q)[(mb + t) * g.q8.ldq + n] = (uint8_t)to_e4m3x2(pp[t * 128] * (1.f / sc), 0.f);
+        reinterpret_cast<uint8_t*>(g.q8.q)[(mb + t) * g.q8.ldq + n] = (uint8_t)to_e4m3x2(pp[t * 128] * q8_inv(sc), 0.f);
         if (row == 0) g.q8.scale[(n0 >> 7) * g.q8.lds + mb + t] = sc;
       }
     }

@@ -17,6 +17,18 @@ __device__ __forceinline__ float q8_scale(uint32_t amax_bits) {
   return s < 0x1p-100f ? 0x1p-100f : s;
 }
 
+// The larger magnitude, NaN where either is (one instruction, the magnitudes are
+// operand modifiers); its bits are ordered as above.
+__device__ __forceinline__ float max_abs(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return r;
+}
+
+// 1 / scale within an ulp: it only decides codes that lie within 2^-23 of a tie
+// (scales are 2^-100 to 2^120, infinite or NaN, so no result is denormal).
+__device__ __forceinline__ float q8_inv(float s) { return __fdividef(1.f, s); }
+
 // Two values in e4m3, rounded to nearest even, past 448 saturated (a rounded
 // 1 / scale can lift a block's largest value a half step above 448), a in the low byte.
 __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {

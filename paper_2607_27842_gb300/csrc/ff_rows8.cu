@@ -11,117 +11,114 @@ namespace ff {
 
 namespace {
 
-// Four elements of a lane's share of a 128-column block: adjacent columns 4 lane ..
-// in one vector where rows allow it, columns lane, lane + 32, .. otherwise.
+// Four elements of a lane's share of a 128-column block, as two fp32 pairs: adjacent
+// columns 4 lane .. in one vector where rows allow it, columns lane, lane + 32, ..
+// otherwise.  Pointers are to the lane's first column (at()), n the columns from
+// there to the row's end.
 template <class T, bool VEC> struct Four;
+template <bool VEC> __device__ __forceinline__ int at(int lane) { return VEC ? 4 * lane : lane; }
 template <> struct Four<float, true> {
-  float4 r;
-  __device__ __forceinline__ void load(const float* p, int lane, int) { r = *reinterpret_cast<const float4*>(p + 4 * lane); }
-  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
-  static __device__ __forceinline__ void store(float* p, int lane, int, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
+  ulonglong2 r;
+  __device__ __forceinline__ void load(const float* p, int) { r = *reinterpret_cast<const ulonglong2*>(p); }
+  __device__ __forceinline__ void get(f32x2 (&v)[2]) const { v[0] = r.x; v[1] = r.y; }
+  static __device__ __forceinline__ void store(float* p, int, const f32x2 (&v)[2]) {
+    *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(v[0], v[1]);
   }
 };
 template <> struct Four<bf16, true> {
   uint2 r;
-  __device__ __forceinline__ void load(const bf16* p, int lane, int) { r = *reinterpret_cast<const uint2*>(p + 4 * lane); }
-  __device__ __forceinline__ void get(float (&v)[4]) const {
-    const f32x2 a = bf2u(r.x), b = bf2u(r.y);
-    v[0] = lo_f(a); v[1] = hi_f(a); v[2] = lo_f(b); v[3] = hi_f(b);
-  }
-  static __device__ __forceinline__ void store(bf16* p, int lane, int, const float (&v)[4]) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-    *reinterpret_cast<uint2*>(p + 4 * lane) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  __device__ __forceinline__ void load(const bf16* p, int) { r = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(f32x2 (&v)[2]) const { v[0] = bf2u(r.x); v[1] = bf2u(r.y); }
+  static __device__ __forceinline__ void store(bf16* p, int, const f32x2 (&v)[2]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(lo_f(v[0]), hi_f(v[0])), b = __floats2bfloat162_rn(lo_f(v[1]), hi_f(v[1]));
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
   }
 };
 template <class T> struct Four<T, false> {
   T r[4];
-  __device__ __forceinline__ void load(const T* p, int lane, int n) {
+  __device__ __forceinline__ void load(const T* p, int n) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = lane + 32 * k < n ? p[lane + 32 * k] : from_f<T>(0.f);
+    for (int k = 0; k < 4; ++k) r[k] = 32 * k < n ? p[32 * k] : from_f<T>(0.f);
   }
-  __device__ __forceinline__ void get(float (&v)[4]) const {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = to_f(r[k]);
+  __device__ __forceinline__ void get(f32x2 (&v)[2]) const {
+    v[0] = f2u(to_f(r[0]), to_f(r[1]));
+    v[1] = f2u(to_f(r[2]), to_f(r[3]));
   }
-  static __device__ __forceinline__ void store(T* p, int lane, int n, const float (&v)[4]) {
+  static __device__ __forceinline__ void store(T* p, int n, const f32x2 (&v)[2]) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (lane + 32 * k < n) p[lane + 32 * k] = from_f<T>(v[k]);
+      if (32 * k < n) p[32 * k] = from_f<T>(k & 1 ? hi_f(v[k / 2]) : lo_f(v[k / 2]));
   }
 };
-// the four as e4m3 (p: the block's first byte, 16-byte aligned rows of bytes)
+// the four as e4m3
 template <bool VEC>
-__device__ __forceinline__ void store8(uint8_t* p, int lane, int n, const float (&v)[4], float inv) {
-  const uint32_t c = to_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+__device__ __forceinline__ void store8(uint8_t* p, int n, const f32x2 (&v)[2], float inv) {
+  const f32x2 i2 = f2u(inv, inv), a = fmul2(v[0], i2), b = fmul2(v[1], i2);
+  const uint32_t c = to_e4m3x4(lo_f(a), hi_f(a), lo_f(b), hi_f(b));
   if (VEC) {
-    *reinterpret_cast<uint32_t*>(p + 4 * lane) = c;
+    *reinterpret_cast<uint32_t*>(p) = c;
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (lane + 32 * k < n) p[lane + 32 * k] = (uint8_t)(c >> (8 * k));
+      if (32 * k < n) p[32 * k] = (uint8_t)(c >> (8 * k));
   }
 }
-__device__ __forceinline__ uint32_t amax4(const float (&v)[4]) {
-  return __reduce_max_sync(0xffffffffu, max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3]))));
+__device__ __forceinline__ float amax4(const f32x2 (&v)[2]) {
+  return max_abs(max_abs(lo_f(v[0]), hi_f(v[0])), max_abs(lo_f(v[1]), hi_f(v[1])));
 }
 
-// W warps to a row (1, 2, 4 or 8; eight warps to a block), NB 128-column blocks to a
-// warp: block i of warp w is w + W i.  A lane has four columns of each, so one warp
-// instruction finds a block's largest magnitude.  With VEC, C is a multiple of 4: a
-// lane's four columns are all in the row or none is.
+// W warps to a row (1, 2, 4 or 8; eight warps to a block), NB adjacent 128-column
+// blocks to a warp.  A lane has four columns of each, so one warp instruction finds a
+// block's largest magnitude.  With VEC, C is a multiple of 4: a lane's four columns
+// are all in the row or none is.  Bound by instruction issue before it was by memory:
+// hence the adjacent blocks (one address, constant offsets), packed pairs and
+// approximate reciprocals (14566 x 2048 with residual and 8-bit output 45 us without
+// them).
 template <class T, int NB, bool VEC, bool NORM, bool Q8>
 __global__ void __launch_bounds__(256) k_rows8(long long rows, int C, int W, const __grid_constant__ RmsArgs a) {
   __shared__ float red[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int w = warp & (W - 1);
   const long long r = (long long)blockIdx.x * (8 / W) + warp / W;
-  const bool on = r < rows;
-  const T* x = reinterpret_cast<const T*>(a.x) + r * a.ldx;
+  const int c0 = w * NB * 128 + at<VEC>(lane), left = r < rows ? C - c0 : 0;   // columns from the lane's first on
   Four<T, VEC> f[NB], g[NB];
   pdl_trigger();
   pdl_wait();
-  auto in = [&](int i) { return on && (w + W * i) * 128 + (VEC ? 4 * lane : lane) < C; };
+  const T* x = reinterpret_cast<const T*>(a.x) + r * a.ldx + c0;
 #pragma unroll
   for (int i = 0; i < NB; ++i)
-    if (in(i)) f[i].load(x + (w + W * i) * 128, lane, C - (w + W * i) * 128);
+    if (128 * i < left) f[i].load(x + 128 * i, left - 128 * i);
   if (NORM && a.resid) {
-    const T* rs = reinterpret_cast<const T*>(a.resid) + r * a.ldr;
+    const T* rs = reinterpret_cast<const T*>(a.resid) + r * a.ldr + c0;
 #pragma unroll
     for (int i = 0; i < NB; ++i)
-      if (in(i)) g[i].load(rs + (w + W * i) * 128, lane, C - (w + W * i) * 128);
+      if (128 * i < left) g[i].load(rs + 128 * i, left - 128 * i);
   }
-  float h[NB][4], ss = 0.f;
+  f32x2 h[NB][2], s2 = 0;
+  T* sm = reinterpret_cast<T*>(a.sum) + r * a.ldsum + c0;
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
-    if (in(i)) {
+    h[i][0] = h[i][1] = 0;
+    if (128 * i < left) {
       f[i].get(h[i]);
       if (NORM && a.resid) {
-        float u[4];
+        f32x2 u[2];
         g[i].get(u);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) h[i][k] += u[k];
+        h[i][0] = fadd2(h[i][0], u[0]);
+        h[i][1] = fadd2(h[i][1], u[1]);
       }
-      if (NORM) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) ss = fmaf(h[i][k], h[i][k], ss);
-        if (a.sum)
-          Four<T, VEC>::store(reinterpret_cast<T*>(a.sum) + r * a.ldsum + (w + W * i) * 128, lane, C - (w + W * i) * 128, h[i]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) h[i][k] = 0.f;
+      if (NORM && a.sum) Four<T, VEC>::store(sm + 128 * i, left - 128 * i, h[i]);
     }
+    if (NORM) s2 = ffma2(h[i][1], h[i][1], ffma2(h[i][0], h[i][0], s2));
   }
-  float rstd = 1.f;
-  if (NORM) {
-    const T* wt = reinterpret_cast<const T*>(a.weight);
-    if (wt) {   // (its loads are under way during the sum)
+  if constexpr (NORM) {
+    const T* wt = reinterpret_cast<const T*>(a.weight) + c0;
+    if (a.weight) {   // (its loads are under way during the sum)
 #pragma unroll
       for (int i = 0; i < NB; ++i)
-        if (in(i)) f[i].load(wt + (w + W * i) * 128, lane, C - (w + W * i) * 128);
+        if (128 * i < left) f[i].load(wt + 128 * i, left - 128 * i);
     }
+    float ss = lo_f(s2) + hi_f(s2);
 #pragma unroll
     for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if (W > 1) {
@@ -130,32 +127,42 @@ __global__ void __launch_bounds__(256) k_rows8(long long rows, int C, int W, con
       ss = 0.f;
       for (int k = 0; k < W; ++k) ss += red[warp - w + k];
     }
-    rstd = rsqrtf(ss / (float)C + a.eps);
+    const float rstd = rsqrtf(ss / (float)C + a.eps);
+    const f32x2 r2 = f2u(rstd, rstd);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      float u[4] = {1.f, 1.f, 1.f, 1.f};
-      if (wt && in(i)) f[i].get(u);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) h[i][k] = h[i][k] * rstd * u[k];
+      h[i][0] = fmul2(h[i][0], r2);
+      h[i][1] = fmul2(h[i][1], r2);
+      if (a.weight && 128 * i < left) {
+        f32x2 u[2];
+        f[i].get(u);
+        h[i][0] = fmul2(h[i][0], u[0]);
+        h[i][1] = fmul2(h[i][1], u[1]);
+      }
     }
   }
   if constexpr (!Q8) {
+    T* o = reinterpret_cast<T*>(a.out) + r * a.ldo + c0;
 #pragma unroll
     for (int i = 0; i < NB; ++i)
-      if (in(i))
-        Four<T, VEC>::store(reinterpret_cast<T*>(a.out) + r * a.ldo + (w + W * i) * 128, lane, C - (w + W * i) * 128, h[i]);
+      if (128 * i < left) Four<T, VEC>::store(o + 128 * i, left - 128 * i, h[i]);
   } else {
+    uint8_t* q = reinterpret_cast<uint8_t*>(a.q8.q) + r * a.q8.ldq + c0;
+    float* sp = a.q8.scale + (long long)(w * NB) * a.q8.lds + r;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int b = w + W * i;
-      if (!on || b * 128 >= C) continue;   // (warp-uniform)
       // columns past the row's end hold no magnitude, not even a NaN's
+      float m = VEC ? amax4(h[i]) : 0.f;
+      if (VEC) {
+        if (128 * i >= left) m = 0.f;
+      } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (b * 128 + (VEC ? 4 * lane : lane + 32 * k) >= C) h[i][k] = 0.f;
-      const float s = q8_scale(amax4(h[i]));
-      if (in(i)) store8<VEC>(reinterpret_cast<uint8_t*>(a.q8.q) + r * a.q8.ldq + b * 128, lane, C - b * 128, h[i], 1.f / s);
-      if (lane == 0) a.q8.scale[b * a.q8.lds + r] = s;
+        for (int k = 0; k < 4; ++k)
+          if (128 * i + 32 * k < left) m = max_abs(m, k & 1 ? hi_f(h[i][k / 2]) : lo_f(h[i][k / 2]));
+      }
+      const float s = q8_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+      if (128 * i < left) store8<VEC>(q + 128 * i, left - 128 * i, h[i], q8_inv(s));
+      if (lane == 0 && 128 * i < left) sp[i * a.q8.lds] = s;
     }
   }
 }
@@ -200,8 +207,9 @@ __global__ void __launch_bounds__(1024) k_rows8_wide(int C, const __grid_constan
     float v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = b * 128 + 32 * k + lane < C ? y(b * 128 + 32 * k + lane) : 0.f;
-    const float s = q8_scale(amax4(v));
-    store8<false>(reinterpret_cast<uint8_t*>(a.q8.q) + r * a.q8.ldq + b * 128, lane, C - b * 128, v, 1.f / s);
+    const f32x2 v2[2] = {f2u(v[0], v[1]), f2u(v[2], v[3])};
+    const float s = q8_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(amax4(v2))));
+    store8<false>(reinterpret_cast<uint8_t*>(a.q8.q) + r * a.q8.ldq + b * 128 + lane, C - b * 128 - lane, v2, q8_inv(s));
     if (lane == 0) a.q8.scale[b * a.q8.lds + r] = s;
   }
 }
@@ -209,42 +217,46 @@ __global__ void __launch_bounds__(1024) k_rows8_wide(int C, const __grid_constan
 // 128 x 128 blocks of a weight: 16 rows to a warp, four columns to a lane.
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_quant8_tile(long long rows, int C, const T* x, long long ldx, const Quant8Out o) {
-  __shared__ uint32_t red[8];
+  __shared__ float red[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c0 = blockIdx.x * 128, n = C - c0;
+  const int c0 = blockIdx.x * 128 + at<VEC>(lane), left = C - c0;
   const long long r0 = (long long)blockIdx.y * 128 + warp * 16;
-  const bool in = (VEC ? 4 * lane : lane) < n;
+  const int n = left > 0 ? (int)max(0ll, min(16ll, rows - r0)) : 0;
   Four<T, VEC> f[16];
   pdl_trigger();
   pdl_wait();
+  const T* p = x + r0 * ldx + c0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (in && r0 + i < rows) f[i].load(x + (r0 + i) * ldx + c0, lane, n);
-  uint32_t m = 0;
+  for (int i = 0; i < 16; ++i, p += ldx)
+    if (i < n) f[i].load(p, left);
+  float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (in && r0 + i < rows) f[i].get(v);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m = max(m, abs_bits(v[k]));
+    f32x2 v[2] = {0, 0};
+    if (i < n) f[i].get(v);
+    m = max_abs(m, amax4(v));
   }
-  m = __reduce_max_sync(0xffffffffu, m);
+  m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
   if (lane == 0) red[warp] = m;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 8; ++k) m = max(m, red[k]);
-  const float s = q8_scale(m), inv = 1.f / s;
+  for (int k = 0; k < 8; ++k) m = max_abs(m, red[k]);
+  const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
+  uint8_t* q = reinterpret_cast<uint8_t*>(o.q) + r0 * o.ldq + c0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if (!in || r0 + i >= rows) continue;
-    float v[4];
+  for (int i = 0; i < 16; ++i, q += o.ldq) {
+    if (i >= n) continue;
+    f32x2 v[2];
     f[i].get(v);
-    store8<VEC>(reinterpret_cast<uint8_t*>(o.q) + (r0 + i) * o.ldq + c0, lane, n, v, inv);
+    store8<VEC>(q, left, v, inv);
   }
   if (threadIdx.x == 0) o.scale[blockIdx.y * o.lds + blockIdx.x] = s;
 }
 
-constexpr int NB_MAX = 16;   // 64 fp32 values to a thread
+// blocks to a warp: at most 16 (64 fp32 values to a thread), four where eight warps
+// hold the row with them (14566 x 2048 with residual and 8-bit output: 45 us with
+// four, 53 with two, 47 with eight, 56 with sixteen)
+constexpr int NB_MAX = 16, NB_PREF = 4;
 
 template <class T, bool VEC, bool NORM, bool Q8>
 cudaError_t rows8_nb(int nb, int W, long long rows, int C, const RmsArgs& a, cudaStream_t s) {
@@ -252,6 +264,7 @@ cudaError_t rows8_nb(int nb, int W, long long rows, int C, const RmsArgs& a, cud
   cudaError_t e;
   if (nb <= 1) e = launch_pdl(k_rows8<T, 1, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
   else if (nb <= 2) e = launch_pdl(k_rows8<T, 2, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
+  else if (nb <= 3) e = launch_pdl(k_rows8<T, 3, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
   else if (nb <= 4) e = launch_pdl(k_rows8<T, 4, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
   else if (nb <= 8) e = launch_pdl(k_rows8<T, 8, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
   else e = launch_pdl(k_rows8<T, NB_MAX, VEC, NORM, Q8>, (unsigned)grid, 256, 0, s, rows, C, W, a);
@@ -266,11 +279,10 @@ template <class T> bool al4(const void* p, long long ld) {
 template <class T, bool NORM>
 cudaError_t rows8(long long rows, int C, const RmsArgs& a, cudaStream_t s) {
   const int blocks = (C + 127) / 128;
-  // Warps to a row: as few as hold it with 16 blocks each, more while the rows alone
-  // leave the SMs without 8 warps each (1 x 2048: one block to a warp and the
-  // other half of them idle, instead of 16 in one).
+  // Warps to a row: as few as hold it with NB_PREF blocks each, more while the rows
+  // alone leave the SMs without 8 warps each.
   int W = 1;
-  while (W < 8 && (blocks > NB_MAX * W || (rows * W < 152 * 8 && blocks > W))) W *= 2;
+  while (W < 8 && (blocks > NB_PREF * W || (rows * W < 152 * 8 && blocks > W))) W *= 2;
   const int nb = (blocks + W - 1) / W;
   if constexpr (NORM) {
     if (nb > NB_MAX) {

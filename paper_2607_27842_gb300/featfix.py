@@ -455,52 +455,62 @@ def _bad(msg):
 # element types: those of the C ABI, then 8-bit values and positions
 _F32, _BF16, _Q8, _I32 = range(4)
 _torch_types = None
+_INTS = [_I * n for n in range(9)]
 
 
-def _typed(t, name, dtype):
+def _types():
+    """The torch types that stand for each element type."""
     global _torch_types
     if _torch_types is None:
         import torch
         _torch_types = ((torch.float32,), (torch.bfloat16,), (torch.float8_e4m3fn, torch.uint8), (torch.int32,))
-    if t.dtype not in _torch_types[dtype]:
-        _bad("%s: %s where %s is expected" % (name, t.dtype, _torch_types[dtype][0]))
+    return _torch_types
+
+
+def _refuse(t, name, dtype, dims):
+    """Says what is wrong with a tensor that _mat or _vec would not take."""
     if not t.is_cuda:
         _bad("%s is not on the GPU" % name)
+    if t.dtype not in _types()[dtype]:
+        _bad("%s: %s where %s is expected" % (name, t.dtype, _types()[dtype][0]))
+    _bad("%s: expected adjacent columns of %s, got %s with strides %s" % (name, list(dims), list(t.shape), list(t.stride())))
 
 
 def _dims(t, name):
-    if len(t.shape) != 2:
-        _bad("%s: expected two dimensions, got %s" % (name, list(t.shape)))
-    return t.shape
+    sh = t.shape
+    if len(sh) != 2:
+        _bad("%s: expected two dimensions, got %s" % (name, list(sh)))
+    return sh
 
 
 def _mat(t, name, dtype, rows, cols):
     """(address, row stride) of a 2-D tensor of the given size; None -> NULL."""
     if t is None:
         return None, 0
-    sh, st = t.shape, t.stride()
-    if len(sh) != 2 or sh[0] != rows or sh[1] != cols:
-        _bad("%s: expected a tensor [%d, %d], got %s" % (name, rows, cols, list(sh)))
-    if cols > 1 and st[1] != 1:
-        _bad("%s: columns must be adjacent" % name)
-    _typed(t, name, dtype)
-    # (the stride of a single row says nothing)
-    return t.data_ptr(), st[0] if rows > 1 else cols if dtype != _Q8 else (cols + 15) // 16 * 16
+    if t.shape != (rows, cols) or t.dtype not in _types()[dtype] or not t.is_cuda:
+        _refuse(t, name, dtype, (rows, cols))
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        _refuse(t, name, dtype, (rows, cols))
+    if rows == 1:   # (the stride of a single row says nothing)
+        ld = cols if dtype != _Q8 else (cols + 15) // 16 * 16
+    return t.data_ptr(), ld
 
 
 def _vec(t, name, dtype, n):
     """Address of n adjacent elements; None -> NULL."""
     if t is None:
         return None
-    if t.numel() != n or not t.is_contiguous():
-        _bad("%s: expected %d adjacent elements" % (name, n))
-    _typed(t, name, dtype)
+    if t.numel() != n or t.dtype not in _types()[dtype] or not t.is_cuda or not t.is_contiguous():
+        _refuse(t, name, dtype, (n,))
     return t.data_ptr()
 
 
 def _quant8(q, scale, rows, cols, tile=1):
     """(q address, ld, scale address, ld) of an 8-bit tensor and its scales."""
-    if (q is None) != (scale is None):
+    if q is None and scale is None:
+        return None, 0, None, 0
+    if q is None or scale is None:
         _bad("8-bit values and their scales come together")
     nb = (cols + 127) // 128
     return _mat(q, "8-bit values", _Q8, rows, cols) + (
@@ -559,7 +569,7 @@ def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None,
         side += [*_mat(x, name, dt, rows, width), width // head_dim, _vec(w, name + "_weight", dt, head_dim),
                  *_mat(o, name + "_out", dt, rows, width)]
     flags = (ROPE_HALVES if halves else 0) | (ROPE_ONE_LADDER if one_ladder else 0) | (ROPE_INVERSE if inverse else 0)
-    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_I * n)(*axis_dims), *_mat(pos, "pos", _I32, n, rows), theta,
+    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_INTS[n] if n < 9 else _I * n)(*axis_dims), *_mat(pos, "pos", _I32, n, rows), theta,
                                  flags, *side, eps, _stream_ptr(stream)))
 
 
