@@ -115,23 +115,23 @@ __device__ __forceinline__ void arrive_read(uint32_t bar_cluster) {
 // exponential): each denominator is capped at 2^30, past which the result is below
 // 2^-26 of x, the rounding of the tanh form.  Within 1e-6 of the exact value; the
 // hardware tanh (2^-11) would show in an 8-bit result's scales.
-__device__ __forceinline__ void gelu4(float& a, float& b, float& c, float& d) {
-  constexpr float K0 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, K1 = K0 * 0.044715f;
-  float v[4] = {a, b, c, d}, e[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float t = fminf(v[i] * __fmaf_rn(v[i] * v[i], K1, K0), 30.f);
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(t));
-    e[i] += 1.f;
-  }
-  const float ab = e[0] * e[1], cd = e[2] * e[3];
+__device__ __forceinline__ void gelu4(f32x2& a, f32x2& b) {
+  constexpr float C0 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, C1 = C0 * 0.044715f;
+  const f32x2 k0 = f2u(C0, C0), k1 = f2u(C1, C1), one = f2u(1.f, 1.f);
+  auto denominators = [&](f32x2 v) {
+    const f32x2 t = fmul2(v, ffma2(fmul2(v, v), k1, k0));
+    float e0, e1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(lo_f(t), 30.f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(hi_f(t), 30.f)));
+    return fadd2(f2u(e0, e1), one);
+  };
+  const f32x2 da = denominators(a), db = denominators(b);
+  const float pa = lo_f(da) * hi_f(da), pb = lo_f(db) * hi_f(db);
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(ab * cd));
-  const float rab = r * cd, rcd = r * ab;
-  a *= rab * e[1];
-  b *= rab * e[0];
-  c *= rcd * e[3];
-  d *= rcd * e[2];
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(pa * pb));
+  const float ra = r * pb, rb = r * pa;   // 1 / pa, 1 / pb
+  a = f2u(lo_f(a) * (ra * hi_f(da)), hi_f(a) * (ra * lo_f(da)));
+  b = f2u(lo_f(b) * (rb * hi_f(db)), hi_f(b) * (rb * lo_f(db)));
 }
 
 // ---------------------------------------------------------------------------
@@ -184,39 +184,50 @@ __device__ __forceinline__ void consts_in(const Gemm8Args& g, uint8_t* cst, int 
   cp_commit();
 }
 
+// 16 bytes in shared memory as fp32 pairs
+__device__ __forceinline__ void pairs16(const float* p, f32x2 (&v)[2]) {
+  const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(p);
+  v[0] = q.x; v[1] = q.y;
+}
+__device__ __forceinline__ void pairs16(const bf16* p, f32x2 (&v)[4]) {
+  const uint4 q = *reinterpret_cast<const uint4*>(p);
+  v[0] = bf2u(q.x); v[1] = bf2u(q.y); v[2] = bf2u(q.z); v[3] = bf2u(q.w);
+}
+
 // bias, GELU and gate of a row's columns n0 + c .. n0 + c + 31.  `gate`: the row's 128
 // columns in shared memory, or null where the warp's rows have more than two samples
 // (fewer than 32 rows to one).
-template <class T>
+template <class T, bool Q8>
 __device__ __forceinline__ void finish32(const Gemm8Args& g, const uint8_t* cst, const float* gate, int m, int n0, int c,
-                                         int N, float (&y)[32]) {
+                                         int N, f32x2* y) {
   if (g.bias) {
-    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int P = 8 / (int)sizeof(T);   // pairs to 16 bytes
 #pragma unroll
-    for (int j = 0; j < 32; j += V) {
-      float b[V];
-      ld16(reinterpret_cast<const T*>(cst) + c + j, b);
+    for (int j = 0; j < 16; j += P) {
+      f32x2 b[P];
+      pairs16(reinterpret_cast<const T*>(cst) + c + 2 * j, b);
 #pragma unroll
-      for (int i = 0; i < V; ++i) y[j + i] += b[i];
+      for (int i = 0; i < P; ++i) y[j + i] = fadd2(y[j + i], b[i]);
     }
   }
   if (g.act) {
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) gelu4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+    for (int j = 0; j < 16; j += 2) gelu4(y[j], y[j + 1]);
   }
-  if (g.gate) {
-    const float* gp = g.gate + (long long)(m / g.rpb) * g.gate_stride + n0 + c;
+  if (!Q8 && g.gate) {   // (8-bit results have none)
+    if (gate) {
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      float f[4];
-      if (gate) {
-        ld16(gate + c + j, f);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = n0 + c + j + i < N ? gp[j + i] : 0.f;
+      for (int j = 0; j < 16; j += 2) {
+        f32x2 f[2];
+        pairs16(gate + c + 2 * j, f);
+        y[j] = fmul2(y[j], f[0]);
+        y[j + 1] = fmul2(y[j + 1], f[1]);
       }
+    } else {
+      const float* gp = g.gate + (long long)(m / g.rpb) * g.gate_stride + n0 + c;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[j + i] *= f[i];
+      for (int j = 0; j < 16; ++j)
+        y[j] = fmul2(y[j], f2u(n0 + c + 2 * j < N ? gp[2 * j] : 0.f, n0 + c + 2 * j + 1 < N ? gp[2 * j + 1] : 0.f));
     }
   }
 }
@@ -246,42 +257,43 @@ __device__ __noinline__ void block_out(const uint8_t* b, T* dst, long long ld, i
 // blocks.  A TMA store writes whole 16 bytes, past the last column too: rows that
 // do not end on 16 bytes leave their last tile through block_out.
 template <class T, bool Q8>
-__device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const CUtensorMap* tmO, float (&acc)[128], int row0,
+__device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const CUtensorMap* tmO, f32x2 (&acc)[64], int row0,
                                            int lane, int n0, int M, int N, uint8_t* blk, const uint8_t* cst, uint64_t* rbar,
                                            uint32_t rph, volatile int* abort_flag) {
   cp_wait<0>();
   __syncwarp();
   const int m = min(row0 + lane, M - 1);   // (rows past M repeat the last one and are not stored)
   const int es = Q8 ? 1 : (int)sizeof(T);
-  const int b_lo = row0 / g.rpb, b_hi = min(row0 + 31, M - 1) / g.rpb;
-  const float* gate = b_hi - b_lo > 1 ? nullptr : reinterpret_cast<const float*>(cst + (m / g.rpb == b_lo ? 512 : 1024));
+  const float* gate = nullptr;
+  if (!Q8 && g.gate) {
+    const int b_lo = row0 / g.rpb, b_hi = min(row0 + 31, M - 1) / g.rpb;
+    if (b_hi - b_lo <= 1) gate = reinterpret_cast<const float*>(cst + (m / g.rpb == b_lo ? 512 : 1024));
+  }
   const bool tma = (flags & STAGED) && (n0 + 128 <= N || (long long)N * es % 16 == 0);
   if constexpr (Q8) {
-    uint32_t mx = 0;
+    // (columns past N are sums over rows of zeros: GELU and magnitude 0)
+    float mx = 0.f;
 #pragma unroll
     for (int c = 0; c < 128; c += 32) {
-      float y[32];
+      finish32<T, Q8>(g, cst, gate, m, n0, c, N, acc + c / 2);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) y[j] = acc[c + j];
-      finish32<T>(g, cst, gate, m, n0, c, N, y);
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        if (n0 + c + j >= N) y[j] = 0.f;
-        mx = max(mx, abs_bits(y[j]));
-        acc[c + j] = y[j];
+      for (int j = c / 2; j < c / 2 + 16; ++j) {
+        mx = max_abs(mx, max_abs(lo_f(acc[j]), hi_f(acc[j])));
       }
     }
-    const float s = q8_scale(mx), inv = q8_inv(s);
+    const float s = q8_scale(__float_as_uint(mx)), inv = q8_inv(s);
     if (row0 + lane < M) g.q8.scale[(n0 >> 7) * g.q8.lds + m] = s;
     if (lane == 0) bulk_wait_read<0>();
     __syncwarp();
+    const f32x2 i2 = f2u(inv, inv);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = to_e4m3x4(acc[16 * k + 4 * i] * inv, acc[16 * k + 4 * i + 1] * inv, acc[16 * k + 4 * i + 2] * inv,
-                         acc[16 * k + 4 * i + 3] * inv);
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 u = fmul2(acc[8 * k + 2 * i], i2), v = fmul2(acc[8 * k + 2 * i + 1], i2);
+        w[i] = to_e4m3x4(lo_f(u), hi_f(u), lo_f(v), hi_f(v));
+      }
       *reinterpret_cast<uint4*>(blk + sw128_off(lane, k)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
     if (tma) fence_async_smem();
@@ -316,17 +328,24 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
     }
 #pragma unroll
     for (int d = 0; d < PER; d += 32) {
-      float y[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) y[j] = acc[c + d + j];
-      finish32<T>(g, cst, gate, m, n0, c + d, N, y);
+      f32x2* y = acc + (c + d) / 2;
+      finish32<T, Q8>(g, cst, gate, m, n0, c + d, N, y);
 #pragma unroll
       for (int k = 0; k < 32 / V; ++k) {
         T* p = reinterpret_cast<T*>(b + sw128_off(lane, d / V + k));
-        float o[V], r[V];
-        if (g.resid) ld16(p, r);
+        f32x2* u = y + V / 2 * k;
+        if (g.resid) {
+          f32x2 r[V / 2];
+          pairs16(p, r);
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = g.resid ? y[V * k + i] + r[i] : y[V * k + i];
+          for (int i = 0; i < V / 2; ++i) u[i] = fadd2(u[i], r[i]);
+        }
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          o[2 * i] = lo_f(u[i]);
+          o[2 * i + 1] = hi_f(u[i]);
+        }
         st16(p, o);
       }
     }
@@ -430,6 +449,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
       }
     }
     if (warp == 1 && rank == 0) {
+      const bool mine = elect_one();   // (here: every instruction between a free buffer and its products counts)
       uint32_t it = 0;   // blocks of K over all tiles: ring stage it % STAGES, TMEM buffer it % 2
       bool ok = true;
       for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
@@ -442,7 +462,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
           if (!wait_warp(&full[s], (it / P_STAGES) & 1, abort_flag) ||
               !wait_try(&tempty[buf], ((it >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          if (elect_one()) {
+          if (mine) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // 32 bytes along K inside the swizzle atom
               umma8_pair(tmem_base + buf * 256, ad + 2 * k, wd + 2 * k, idesc8(256, 256), k != 0);
@@ -460,28 +480,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
     const uint32_t tq = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 128);
     const uint32_t tempty0 = map_to(tempty, 0);
     uint32_t it = 0, rph = 0;
-    for (int tile = pair; tile < num_tiles; tile += npairs) {
+    // a warp's first row and column of a tile; whether any of it is in the result
+    auto place = [&](int tile, int& row0, int& n0) {
       int mb, nb;
       tile_at8(tile, num_m, num_n, mb, nb);
-      const int row0 = mb * 256 + (int)rank * 128 + q * 32, n0 = nb * 256 + h * 128;
-      const bool live = n0 < N && row0 < M;   // (warp-uniform)
-      if (live && (flags & RESID_TMA) && lane == 0) {
-        bulk_wait_read<0>();   // the last tile's stores have left the blocks
-        fence_async_smem();    // (and so have block_out's reads)
-        mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
-        tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
-        if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+      row0 = mb * 256 + (int)rank * 128 + q * 32;
+      n0 = nb * 256 + h * 128;
+      return n0 < N && row0 < M;
+    };
+    // Scales of this row and of W's block of rows, two blocks of K ahead; a tile's first
+    // ones are loaded in front of the tile before's results
+    float a0 = 0.f, w0 = 0.f, a1 = 0.f, w1 = 0.f;
+    auto first_scales = [&](int tile) {
+      int row0, n0;
+      if (tile >= num_tiles || !place(tile, row0, n0) || row0 + lane >= M) return;
+      const float* sa = g.sa + row0 + lane;
+      const float* sw = g.sw + (n0 >> 7) * g.ldsw;
+      a0 = sa[0];
+      w0 = sw[0];
+      if (num_kb > 1) {
+        a1 = sa[g.ldsa];
+        w1 = sw[1];
       }
+    };
+    first_scales(pair);
+    for (int tile = pair; tile < num_tiles; tile += npairs) {
+      int row0, n0;
+      const bool live = place(tile, row0, n0);   // (warp-uniform)
+      // the residual's copies begin a block of K late: the last tile's stores have left by then
+      const int rk = live && (flags & RESID_TMA) ? min(1, num_kb - 1) : -1;
+      bool resid_on = false;
       if (live) {
         __syncwarp();   // the last tile's are read
         consts_in<T>(g, cst, row0, n0, M, N, lane);
       }
-      // scales of this row and of W's block of rows, two blocks of K ahead
       const bool in = live && row0 + lane < M;
       const float* sa = g.sa + row0 + lane;
       const float* sw = g.sw + (n0 >> 7) * g.ldsw;
-      float a0 = in ? sa[0] : 0.f, w0 = in ? sw[0] : 0.f;
-      float a1 = in && num_kb > 1 ? sa[g.ldsa] : 0.f, w1 = in && num_kb > 1 ? sw[1] : 0.f;
       f32x2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
@@ -494,6 +529,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
         if (in && kb + 2 < num_kb) {
           a1 = sa[(kb + 2) * g.ldsa];
           w1 = sw[kb + 2];
+        }
+        if (kb == rk) {
+          resid_on = true;
+          if (lane == 0) {
+            bulk_wait_read<0>();
+            fence_async_smem();    // (block_out's reads)
+            mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
+            tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
+            if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+          }
+          __syncwarp();
         }
         if (!wait_try(&tfull[buf], (it >> 1) & 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -517,22 +563,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
           if (lane == 0) arrive_read(tempty0 + 8 * buf);
         }
       }
-      if (live) {
-        float y[128];
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          y[2 * i] = lo_f(acc[i]);
-          y[2 * i + 1] = hi_f(acc[i]);
-        }
-        if (ok) {
-          ok = finish_row<T, Q8>(g, flags, &tmO, y, row0, lane, n0, M, N, blk, cst, &rbar[warp - 4], rph, abort_flag);
-        } else if ((flags & RESID_TMA) && lane == 0) {   // its copies still land before the CTA exits
-          const unsigned long long t0 = gtimer();
-          while (!mbar_try(&rbar[warp - 4], rph))
-            if (gtimer() - t0 > WAIT_LIMIT_NS) { atomicOr(&g_watchdog8, 2u); break; }
-        }
-        rph ^= 1;
+      first_scales(tile + npairs);
+      if (ok && live) {
+        ok = finish_row<T, Q8>(g, flags, &tmO, acc, row0, lane, n0, M, N, blk, cst, &rbar[warp - 4], rph, abort_flag);
+      } else if (!ok && resid_on && lane == 0) {   // its copies still land before the CTA exits
+        const unsigned long long t0 = gtimer();
+        while (!mbar_try(&rbar[warp - 4], rph))
+          if (gtimer() - t0 > WAIT_LIMIT_NS) { atomicOr(&g_watchdog8, 2u); break; }
       }
+      if (live) rph ^= 1;
       if (!ok) break;
     }
     if (lane == 0) bulk_wait_all();
@@ -679,6 +718,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
   } else if (warp == 1) {
     // the loop's time is this warp's: both barriers are tested together, and the next
     // block's behind this one's products
+    const bool mine = elect_one();
     uint32_t it = 0;
     bool ready = false;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
@@ -694,7 +734,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
         const bool t = mbar_test(&tempty[j & 3], ((j >> 2) & 1) ^ 1), f = mbar_test(&full[j % C::STAGES], (j / C::STAGES) & 1);
         ready = t && f;
       }
-      if (elect_one()) {
+      if (mine) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           umma8(tmem_base + buf * BT, wd + 2 * k, ad + 2 * k, idesc8(128, BT), k != 0);
@@ -789,7 +829,11 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
       for (int i = 0; i < U; ++i) y[i] += bias;
       if (g.act) {
 #pragma unroll
-        for (int i = 0; i < U; i += 4) gelu4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+        for (int i = 0; i < U; i += 4) {
+          f32x2 p = f2u(y[i], y[i + 1]), r = f2u(y[i + 2], y[i + 3]);
+          gelu4(p, r);
+          y[i] = lo_f(p); y[i + 1] = hi_f(p); y[i + 2] = lo_f(r); y[i + 3] = hi_f(r);
+        }
       }
       if constexpr (Q8) {
 #pragma unroll
@@ -925,13 +969,13 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
 }
 
 // The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster: the
-// least time of a model in us fitted to a sweep of both over M from 1 to 4096 (K of 512
+// least time of a model in us fitted to sweeps of both over M from 1 to 4096 (K of 512
 // to 8192): a tile's time is linear in its blocks of K, tiles run in waves over the SMs
 // (two CTAs of the split kernel to an SM up to 64 rows, each slower beside the other),
 // and the cluster's meeting costs more the larger it is.  Measured against the choice's
-// neighbours at 256 x 2048 x 8192: pairs 34 us, 128 rows and 4 CTAs 16.2, 32 rows and 2
-// CTAs 17.0; 512 x 2048 x 2048: pairs 14.6, 32 rows 10.7, 128 rows and 2 CTAs 13.0; from
-// 1024 x 2048 x 2048 (14.8 and 16.1) pairs are the faster.
+// neighbours at 256 x 2048 x 8192: pairs 31 us, 128 rows and 4 CTAs 16.2, 32 rows and 2
+// CTAs 17.0; 512 x 2048 x 2048: 32 rows 10.7, 128 rows and 2 CTAs 13.0, pairs 12.1; at
+// 1024 x 2048 x 2048 pairs 12.3, 64 rows 16.1.
 struct Plan {
   int bt, s;   // bt 0: CTA pairs
 };
@@ -939,7 +983,7 @@ Plan plan8(int M, int N, int K) {
   const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
-  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.42 * kb + 3.6) + 3.6;
+  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.405 * kb + 2.8) + 2.7;
   const int bts[4] = {16, 32, 64, 128};
   const double one[4] = {0.235, 0.29, 0.36, 0.49}, two[4] = {0.30, 0.40, 0.63, 0.49}, fixed[4] = {1.6, 2.2, 3.3, 7.0};
   const double meet[4] = {0, 0.3, 0.6, 1.2};
