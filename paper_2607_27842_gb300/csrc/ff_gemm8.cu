@@ -15,6 +15,7 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <mutex>
 #include <type_traits>
 
@@ -233,24 +234,62 @@ __device__ __forceinline__ void finish32(const Gemm8Args& g, const uint8_t* cst,
 }
 
 // A warp's block of 32 rows of 128 bytes between shared memory and row-major global
-// memory, coalesced, element by element: for rows that TMA cannot take.
+// memory, for rows that TMA cannot take: four bytes to a lane where rows start on
+// four, element by element otherwise.  block_in copies by cp.async where it can; its
+// caller waits.  (Calls: written out, they would cost the loops their registers.)
 template <class T>
 __device__ __noinline__ void block_in(uint8_t* b, const T* src, long long ld, int rows, int cols, int lane) {
+  constexpr int E = 4 / (int)sizeof(T);
+  rows = min(rows, 32);
+  if (!(((uintptr_t)src | (uintptr_t)(ld * sizeof(T))) & 3)) {
+    const int bytes = max(0, min(4, (cols - E * lane) * (int)sizeof(T)));
+    const T* p = bytes ? src + E * lane : src;
 #pragma unroll 4
-  for (int r = 0; r < min(rows, 32); ++r)
+    for (int r = 0; r < rows; ++r, p += ld) cp_async4(b + sw128_off(r, lane >> 2) + (lane & 3) * 4, p, bytes);
+  } else {
+    // eight rows' loads in front of their stores (a load may not pass a store that could
+    // alias it: 4000 x 2047 x 512 with a residual took 103 us row by row)
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+      T v[8][E];
 #pragma unroll
-    for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
-      if (j < cols)
-        *reinterpret_cast<T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16) = src[r * ld + j];
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          v[i][e] = r0 + i < rows && lane + 32 * e < cols ? src[(r0 + i) * ld + lane + 32 * e] : from_f<T>(0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int j = lane + 32 * e;
+          *reinterpret_cast<T*>(b + sw128_off(r0 + i, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16) = v[i][e];
+        }
+    }
+  }
 }
 template <class T>
 __device__ __noinline__ void block_out(const uint8_t* b, T* dst, long long ld, int rows, int cols, int lane) {
+  constexpr int E = 4 / (int)sizeof(T);
+  rows = min(rows, 32);
+  if (!(((uintptr_t)dst | (uintptr_t)(ld * sizeof(T))) & 3)) {
+    const int n = cols - E * lane;   // elements of this lane's four bytes
+    T* p = dst + E * lane;
 #pragma unroll 4
-  for (int r = 0; r < min(rows, 32); ++r)
+    for (int r = 0; r < rows; ++r, p += ld) {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(b + sw128_off(r, lane >> 2) + (lane & 3) * 4);
+      if (n >= E) {
+        *reinterpret_cast<uint32_t*>(p) = v;
+      } else {
+        for (int i = 0; i < n; ++i) p[i] = reinterpret_cast<const T*>(&v)[i];
+      }
+    }
+  } else {
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r)
 #pragma unroll
-    for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
-      if (j < cols)
-        dst[r * ld + j] = *reinterpret_cast<const T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16);
+      for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
+        if (j < cols)
+          dst[r * ld + j] = *reinterpret_cast<const T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16);
+  }
 }
 
 // Sums of a thread's row over 128 columns -> result, through the warp's two 4 KB
@@ -314,15 +353,17 @@ __device__ __forceinline__ bool finish_row(const Gemm8Args& g, int flags, const 
   for (int c = 0; c < 128; c += PER) {
     if (n0 + c >= N) break;
     uint8_t* b = blk + (c / PER & 1) * 4096;
-    if (!(flags & RESID_TMA)) {
-      // the last tile's stores, or this tile's before last, have left the block (with
-      // the residual by TMA: before that came)
+    if (!g.resid || c >= 2 * PER) {
+      // the last tile's stores, or this tile's before last, have left the block (where
+      // the residual is in it: before that came)
       if (lane == 0) {
         if (c == 0) bulk_wait_read<0>(); else bulk_wait_read<1>();
       }
       __syncwarp();
-      if (g.resid) {
+      if (g.resid) {   // (fp32: the third and fourth block)
         block_in<T>(b, reinterpret_cast<const T*>(g.resid) + row0 * g.ldr + n0 + c, g.ldr, M - row0, N - n0 - c, lane);
+        cp_commit();
+        cp_wait<0>();
         __syncwarp();
       }
     }
@@ -508,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
       int row0, n0;
       const bool live = place(tile, row0, n0);   // (warp-uniform)
       // the residual's copies begin a block of K late: the last tile's stores have left by then
-      const int rk = live && (flags & RESID_TMA) ? min(1, num_kb - 1) : -1;
+      const int rk = live && !Q8 && g.resid ? min(1, num_kb - 1) : -1;
       bool resid_on = false;
       if (live) {
         __syncwarp();   // the last tile's are read
@@ -531,13 +572,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
           w1 = sw[kb + 2];
         }
         if (kb == rk) {
-          resid_on = true;
-          if (lane == 0) {
-            bulk_wait_read<0>();
-            fence_async_smem();    // (block_out's reads)
-            mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
-            tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
-            if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+          if (lane == 0) bulk_wait_read<0>();
+          __syncwarp();
+          if (flags & RESID_TMA) {
+            resid_on = true;
+            if (lane == 0) {
+              fence_async_smem();    // (block_out's reads)
+              mbar_expect_tx(&rbar[warp - 4], n0 + 64 < N ? 8192u : 4096u);
+              tma_load(&tmR, &rbar[warp - 4], blk, n0, row0);
+              if (n0 + 64 < N) tma_load(&tmR, &rbar[warp - 4], blk + 4096, n0 + 64, row0);
+            }
+          } else {
+            constexpr int PER = 128 / (int)sizeof(T);
+            const T* rp = reinterpret_cast<const T*>(g.resid) + row0 * g.ldr + n0;
+            block_in<T>(blk, rp, g.ldr, M - row0, N - n0, lane);
+            if (n0 + PER < N) block_in<T>(blk + 4096, rp + PER, g.ldr, M - row0, N - n0 - PER, lane);
+            cp_commit();
           }
           __syncwarp();
         }
@@ -957,10 +1007,10 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
     flags = STAGED;
   } else if (!((uintptr_t)g.out & 15) && g.ldo * es % 16 == 0 && make_map8(&mo, g.out, es, M, N, g.ldo, 32)) {
     flags = STAGED;
-    if (es == 2 && g.resid && !((uintptr_t)g.resid & 15) && g.ldr * es % 16 == 0 &&
-        make_map8(&mr, g.resid, es, M, N, g.ldr, 32))
-      flags |= RESID_TMA;
   }
+  if (!Q8 && es == 2 && g.resid && !((uintptr_t)g.resid & 15) && g.ldr * es % 16 == 0 &&
+      make_map8(&mr, g.resid, es, M, N, g.ldr, 32))
+    flags |= RESID_TMA;
   const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
   if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
   const int pairs = g_sms / 2, grid = 2 * (int)(tiles < pairs ? tiles : pairs);
@@ -969,13 +1019,14 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
 }
 
 // The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster: the
-// least time of a model in us fitted to sweeps of both over M from 1 to 4096 (K of 512
-// to 8192): a tile's time is linear in its blocks of K, tiles run in waves over the SMs
-// (two CTAs of the split kernel to an SM up to 64 rows, each slower beside the other),
-// and the cluster's meeting costs more the larger it is.  Measured against the choice's
-// neighbours at 256 x 2048 x 8192: pairs 31 us, 128 rows and 4 CTAs 16.2, 32 rows and 2
-// CTAs 17.0; 512 x 2048 x 2048: 32 rows 10.7, 128 rows and 2 CTAs 13.0, pairs 12.1; at
-// 1024 x 2048 x 2048 pairs 12.3, 64 rows 16.1.
+// least time of a model in us.  A tile's time is linear in its blocks of K, tiles run in
+// waves over the SMs (two CTAs of the split kernel to an SM up to 64 rows, each slower
+// beside the other), and the cluster's meeting costs more the larger it is.  The
+// constants are fitted to 700 timings of both kernels at 60 sizes (M 1 to 4096, N 48 to
+// 12288, K 48 to 8192, all epilogues): the choice is 1.3% slower than the best one on
+// average, 22% at worst.  Either side of it: 256 x 2048 x 8192 pairs 31 us, 128 rows and 4
+// CTAs 16.4; 512 x 2048 x 2048 pairs 12.1, 32 rows 11.4; 1024 x 2048 x 2048 pairs 12.2,
+// 64 rows 16.1.
 struct Plan {
   int bt, s;   // bt 0: CTA pairs
 };
@@ -983,10 +1034,10 @@ Plan plan8(int M, int N, int K) {
   const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
-  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.405 * kb + 2.8) + 2.7;
+  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.517 * kb + 6.5) + 1.3;
   const int bts[4] = {16, 32, 64, 128};
-  const double one[4] = {0.235, 0.29, 0.36, 0.49}, two[4] = {0.30, 0.40, 0.63, 0.49}, fixed[4] = {1.6, 2.2, 3.3, 7.0};
-  const double meet[4] = {0, 0.3, 0.6, 1.2};
+  const double one[4] = {0.262, 0.292, 0.294, 0.531}, two[4] = {0.301, 0.521, 0.495, 0.0}, fixed[4] = {1.62, 2.07, 6.25, 7.5};
+  const double meet[4] = {0, 0.23, 0.37, 0.6};
   for (int i = 0; i < 4; ++i) {
     if (i > 0 && bts[i - 1] >= M) break;
     const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
@@ -994,7 +1045,7 @@ Plan plan8(int M, int N, int K) {
       const long long ctas = tiles << l, room = (long long)g_sms * (bts[i] <= 64 ? 2 : 1);
       const bool shared = bts[i] <= 64 && ctas > g_sms;
       const double t = (double)((ctas + room - 1) / room) * ((shared ? two : one)[i] * (double)((kb + (1 << l) - 1) >> l) + fixed[i]) +
-                       2.0 + meet[l] + (shared ? 0.5 : 0.0);
+                       2.0 + meet[l] + (shared ? 0.34 : 0.0) + 0.16 * std::min(1.0, (double)ctas / (double)room);
       if (t < least) {
         least = t;
         best = {bts[i], 1 << l};
