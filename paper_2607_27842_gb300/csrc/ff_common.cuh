@@ -525,58 +525,6 @@ cudaError_t gemm_tc_grouped(int M0, const void* A0, const void* W0, const EpiArg
 unsigned int gemm_tc_watchdog_take();
 cudaError_t watchdog_probe(unsigned long long limit_ns, cudaStream_t s);
 
-// 8-bit layers (formats and formulas: featfix_ops.h)
-struct Quant8Out {   // an 8-bit tensor and its scales
-  void* q;
-  long long ldq;
-  float* scale;
-  long long lds;
-};
-struct RmsArgs {
-  const void* x; long long ldx;
-  const void* resid; long long ldr;   // nullable
-  void* sum; long long ldsum;         // nullable
-  const void* weight;                 // nullable
-  float eps;
-  void* out; long long ldo;           // null: q8
-  Quant8Out q8;
-};
-cudaError_t launch_rms_norm(DType dt, long long rows, int C, const RmsArgs& a, cudaStream_t s);
-cudaError_t launch_quant8(DType dt, int tile, long long rows, int cols, const void* x, long long ldx,
-                          const Quant8Out& o, cudaStream_t s);
-constexpr int ROPE_PAIRS = 128;   // head widths up to 256
-struct RopeSide {
-  const void* x; long long ldx;
-  void* out; long long ldo;
-  const void* weight;   // nullable: no norm
-  int heads;
-};
-struct RopeArgs {
-  RopeSide side[2];     // q, k
-  const int* pos;
-  long long ld_pos;
-  int hd, rot, halves;
-  float eps;
-  // turns per position of every pair (negative: the inverse), as an unevaluated
-  // sum of two floats, and the pair's axis
-  float2 freq[ROPE_PAIRS];
-  unsigned char axis[ROPE_PAIRS];
-};
-cudaError_t launch_rope(DType dt, long long rows, const RopeArgs& a, cudaStream_t s);
-struct Gemm8Args {
-  const void* a; long long lda;
-  const float* sa; long long ldsa;
-  const void* w; long long ldw;
-  const float* sw; long long ldsw;
-  const void* bias;                    // nullable, [N]
-  int act;
-  const float* gate; long long gate_stride; int rpb;   // nullable
-  const void* resid; long long ldr;    // nullable
-  void* out; long long ldo;            // null: q8
-  Quant8Out q8;
-};
-cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s);
-
 // attention over the token-row layout (see featfix_token_row)
 struct AttnArgs {
   const void* q; const void* k; const void* v;  // base pointers (column offsets applied)

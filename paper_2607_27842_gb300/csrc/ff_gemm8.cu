@@ -1022,9 +1022,9 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
 // least time of a model in us.  A tile's time is linear in its blocks of K, tiles run in
 // waves over the SMs (two CTAs of the split kernel to an SM up to 64 rows, each slower
 // beside the other), and the cluster's meeting costs more the larger it is.  The
-// constants are fitted to 700 timings of both kernels at 60 sizes (M 1 to 4096, N 48 to
-// 12288, K 48 to 8192, all epilogues): the choice is 1.3% slower than the best one on
-// average, 22% at worst.  Either side of it: 256 x 2048 x 8192 pairs 31 us, 128 rows and 4
+// constants are fitted to 1000 timings of both kernels at 90 sizes (M 1 to 9000, N 48 to
+// 12288, K 48 to 8192, all epilogues): the choice is 1.5% slower than the best one on
+// average, 25% at worst.  Either side of it: 256 x 2048 x 8192 pairs 31 us, 128 rows and 4
 // CTAs 16.4; 512 x 2048 x 2048 pairs 12.1, 32 rows 11.4; 1024 x 2048 x 2048 pairs 12.2,
 // 64 rows 16.1.
 struct Plan {
@@ -1034,10 +1034,10 @@ Plan plan8(int M, int N, int K) {
   const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
-  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.517 * kb + 6.5) + 1.3;
+  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.549 * kb + 3.65) + 4.7;
   const int bts[4] = {16, 32, 64, 128};
-  const double one[4] = {0.262, 0.292, 0.294, 0.531}, two[4] = {0.301, 0.521, 0.495, 0.0}, fixed[4] = {1.62, 2.07, 6.25, 7.5};
-  const double meet[4] = {0, 0.23, 0.37, 0.6};
+  const double one[4] = {0.321, 0.381, 0.365, 0.586}, two[4] = {0.300, 0.467, 0.558, 0.0}, fixed[4] = {1.73, 2.15, 5.57, 7.34};
+  const double meet[4] = {0, 0.27, 0.23, 0.44};
   for (int i = 0; i < 4; ++i) {
     if (i > 0 && bts[i - 1] >= M) break;
     const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
@@ -1045,7 +1045,7 @@ Plan plan8(int M, int N, int K) {
       const long long ctas = tiles << l, room = (long long)g_sms * (bts[i] <= 64 ? 2 : 1);
       const bool shared = bts[i] <= 64 && ctas > g_sms;
       const double t = (double)((ctas + room - 1) / room) * ((shared ? two : one)[i] * (double)((kb + (1 << l) - 1) >> l) + fixed[i]) +
-                       2.0 + meet[l] + (shared ? 0.34 : 0.0) + 0.16 * std::min(1.0, (double)ctas / (double)room);
+                       2.0 + meet[l] + (shared ? 0.61 : 0.0) + 0.18 * std::min(1.0, (double)ctas / (double)room);
       if (t < least) {
         least = t;
         best = {bts[i], 1 << l};

@@ -1,6 +1,7 @@
 // C ABI of include/featfix_ops.h: the hot-path kernels on caller buffers.
 #include "featfix_ops.h"
 #include "ff_common.cuh"
+#include "ff_q8.cuh"
 
 #include <math.h>
 

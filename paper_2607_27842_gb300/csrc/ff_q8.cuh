@@ -1,10 +1,65 @@
-// The 8-bit format of featfix_ops.h: e4m3 values with a scale for each block.
+// Declarations shared by the kernels of the 8-bit layers and their C entries, and the
+// 8-bit format of featfix_ops.h: e4m3 values with a scale for each block.
 #pragma once
+
+#include "ff_common.cuh"
 
 #include <cuda_fp8.h>
 #include <stdint.h>
 
 namespace ff {
+
+// 8-bit layers (formats and formulas: featfix_ops.h)
+struct Quant8Out {   // an 8-bit tensor and its scales
+  void* q;
+  long long ldq;
+  float* scale;
+  long long lds;
+};
+struct RmsArgs {
+  const void* x; long long ldx;
+  const void* resid; long long ldr;   // nullable
+  void* sum; long long ldsum;         // nullable
+  const void* weight;                 // nullable
+  float eps;
+  void* out; long long ldo;           // null: q8
+  Quant8Out q8;
+};
+cudaError_t launch_rms_norm(DType dt, long long rows, int C, const RmsArgs& a, cudaStream_t s);
+cudaError_t launch_quant8(DType dt, int tile, long long rows, int cols, const void* x, long long ldx,
+                          const Quant8Out& o, cudaStream_t s);
+constexpr int ROPE_PAIRS = 128;   // head widths up to 256
+struct RopeSide {
+  const void* x; long long ldx;
+  void* out; long long ldo;
+  const void* weight;   // nullable: no norm
+  int heads;
+};
+struct RopeArgs {
+  RopeSide side[2];     // q, k
+  const int* pos;
+  long long ld_pos;
+  int hd, rot, halves;
+  float eps;
+  // turns per position of every pair (negative: the inverse), as an unevaluated
+  // sum of two floats, and the pair's axis
+  float2 freq[ROPE_PAIRS];
+  unsigned char axis[ROPE_PAIRS];
+};
+cudaError_t launch_rope(DType dt, long long rows, const RopeArgs& a, cudaStream_t s);
+struct Gemm8Args {
+  const void* a; long long lda;
+  const float* sa; long long ldsa;
+  const void* w; long long ldw;
+  const float* sw; long long ldsw;
+  const void* bias;                    // nullable, [N]
+  int act;
+  const float* gate; long long gate_stride; int rpb;   // nullable
+  const void* resid; long long ldr;    // nullable
+  void* out; long long ldo;            // null: q8
+  Quant8Out q8;
+};
+cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s);
 
 // Magnitudes compare as their bits do; a NaN is above infinity, so a block's
 // maximum carries both on into its scale (fmaxf would drop the NaN).

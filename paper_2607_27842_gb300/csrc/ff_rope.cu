@@ -3,6 +3,7 @@
 // Bound by memory: q and k are read and written once; a row's sines and cosines are
 // formed once for all of its heads.
 #include "ff_common.cuh"
+#include "ff_q8.cuh"
 
 #include <algorithm>
 
@@ -64,170 +65,231 @@ template <> struct Eight<bf16> {
 
 constexpr int ROPE_ROWS = 8;   // most rows to a block
 
-// R rows to a block, 2^lgl lanes to a head.  A group of lanes keeps its head (its
-// addresses and the norm's weight) and goes down the rows, four at a time: hc heads
-// lie side by side over the groups, and where that leaves groups over, `par` rows do.
-// The first loads are under way while the block forms its sines and cosines.
-// NORM: some side has a weight.  HALVES: pairs are half a width apart.
-template <class T, bool NORM, bool HALVES>
-__global__ void __launch_bounds__(256) k_rope(long long rows, int R, int lgl, int hc, int par,
-                                              const __grid_constant__ RopeArgs a) {
-  __shared__ __align__(16) float2 cs[ROPE_ROWS][ROPE_PAIRS];
-  const int np = a.rot >> 1, hq = a.side[0].heads, H = hq + a.side[1].heads;
-  const long long r0 = (long long)blockIdx.x * R;
-  const int n = (int)min((long long)R, rows - r0);
-  const int l = threadIdx.x & ((1 << lgl) - 1), grp = threadIdx.x >> lgl;
-  const int first = grp / hc, h0 = grp - first * hc;   // the group's first row and head
-  const bool turned = 8 * l < a.rot;
-  // the lane's columns: first four, last four
-  const int lo = HALVES && turned ? 4 * l : 8 * l, hi = HALVES && turned ? np + 4 * l : 8 * l + 4;
-  pdl_trigger();
-  pdl_wait();
-  const float inv_hd = 1.f / (float)a.hd;
-  bool made = false;
-  for (int hb = blockIdx.y * hc; hb < H; hb += gridDim.y * hc) {   // (the same count of rounds for every thread, as below)
-    const int head = hb + h0;
-    const bool second = head >= hq, on = head < H && first < par && 8 * l < a.hd;
-    const T* x = reinterpret_cast<const T*>(second ? a.side[1].x : a.side[0].x);
-    T* o = reinterpret_cast<T*>(second ? a.side[1].out : a.side[0].out);
-    const T* wt = reinterpret_cast<const T*>(second ? a.side[1].weight : a.side[0].weight);
-    const long long ldx = second ? a.side[1].ldx : a.side[0].ldx, ldo = second ? a.side[1].ldo : a.side[0].ldo;
-    const int col = (second ? head - hq : head) * a.hd;
-    x += (r0 + first) * ldx + col;
-    o += (r0 + first) * ldo + col;
-    f32x2 w[4];
-    if (NORM && wt && on) {
-      Eight<T> e;
-      e.load(wt + lo, wt + hi);
-      e.get(w);
-    }
-    for (int rb = 0; rb < R; rb += 4 * par) {
-      Eight<T> e[4];
+// Turns (and norms) a group of lanes' share of one side's heads of one row: heads g, g +
+// step, .., four at a time, their loads in front.  c, s: the lane's four cosines and
+// sines.
+template <class T, bool NORM, bool HALVES, class Make>
+__device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g, int step, int l, int lo, int hi, bool on,
+                                          bool turned, int hd, float inv_hd, float eps, float (&c)[4], float (&s)[4],
+                                          const float2* cs, bool& made, const Make& make) {
+  const T* x = reinterpret_cast<const T*>(sd.x) + r * sd.ldx;
+  T* o = reinterpret_cast<T*>(sd.out) + r * sd.ldo;
+  const T* wt = reinterpret_cast<const T*>(sd.weight);
+  f32x2 w[4];
+  if (NORM && wt && on) {
+    Eight<T> e;
+    e.load(wt + lo, wt + hi);
+    e.get(w);
+  }
+  for (int h0 = 0; h0 < sd.heads; h0 += 4 * step) {   // (the same count of rounds for every lane)
+    Eight<T> e[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (on && rb + i * par + first < n) e[i].load(x + (rb + i * par) * ldx + lo, x + (rb + i * par) * ldx + hi);
-      if (!made) {
-        for (int i = threadIdx.x; i < n * np; i += 256) {
-          const int r = i / np, p = i - r * np;
-          cs[r][p] = turn(a.pos[a.axis[p] * a.ld_pos + r0 + r], a.freq[p]);
-        }
-        __syncthreads();
-        made = true;
+    for (int i = 0; i < 4; ++i) {
+      const int h = h0 + i * step + g;
+      if (on && h < sd.heads) e[i].load(x + h * hd + lo, x + h * hd + hi);
+    }
+    if (!made) {   // the block's sines and cosines; this lane's
+      make();
+      __syncthreads();
+      made = true;
+      if (on && turned) {
+        const float4 c01 = reinterpret_cast<const float4*>(cs + 4 * l)[0], c23 = reinterpret_cast<const float4*>(cs + 4 * l)[1];
+        c[0] = c01.x; c[1] = c01.z; c[2] = c23.x; c[3] = c23.z;
+        s[0] = c01.y; s[1] = c01.w; s[2] = c23.y; s[3] = c23.w;
       }
+    }
+    float rs[4];
+    if (NORM && wt) {
+      // Four sums over the group's lanes at once: the first two steps also halve the sums
+      // a lane holds, so lane l ends with that of head l % 4, and forms one root
+      // for it (9 shuffles and one root where each sum alone takes 16 and four)
+      float q[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = rb + i * par + first;
-        const bool in = on && r < n;
         f32x2 v[4] = {0, 0, 0, 0};
-        if (in) e[i].get(v);
-        if (NORM) {   // (every lane of the warp takes part)
-          const f32x2 s2 = ffma2(v[3], v[3], ffma2(v[2], v[2], ffma2(v[1], v[1], fmul2(v[0], v[0]))));
-          float ss = lo_f(s2) + hi_f(s2);
-          for (int k = 1; k < 1 << lgl; k <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, k);
-          if (wt) {
-            const float rstd = rsqrtf(fmaf(ss, inv_hd, a.eps));
-            const f32x2 r2 = f2u(rstd, rstd);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = fmul2(fmul2(v[k], r2), w[k]);
-          }
-        }
-        if (!in) continue;
-        if (turned) {
-          const float4* c4 = reinterpret_cast<const float4*>(&cs[r][4 * l]);
-          const float4 c01 = c4[0], c23 = c4[1];
-          // (single operations: building packed pairs of cosines costs more than they save)
-          const float c[4] = {c01.x, c01.z, c23.x, c23.z}, s[4] = {c01.y, c01.w, c23.y, c23.w};
-          if (HALVES) {   // v[0], v[1]: four of the first half, v[2], v[3]: of the second
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float x0 = lo_f(v[k]), x1 = hi_f(v[k]), y0 = lo_f(v[k + 2]), y1 = hi_f(v[k + 2]);
-              v[k] = f2u(x0 * c[2 * k] - y0 * s[2 * k], x1 * c[2 * k + 1] - y1 * s[2 * k + 1]);
-              v[k + 2] = f2u(x0 * s[2 * k] + y0 * c[2 * k], x1 * s[2 * k + 1] + y1 * c[2 * k + 1]);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float x = lo_f(v[k]), y = hi_f(v[k]);
-              v[k] = f2u(x * c[k] - y * s[k], x * s[k] + y * c[k]);
-            }
-          }
-        }
-        Eight<T>::store(o + (rb + i * par) * ldo + lo, o + (rb + i * par) * ldo + hi, v);
+        if (on && h0 + i * step + g < sd.heads) e[i].get(v);
+        const f32x2 s2 = ffma2(v[3], v[3], ffma2(v[2], v[2], ffma2(v[1], v[1], fmul2(v[0], v[0]))));
+        q[i] = lo_f(s2) + hi_f(s2);
       }
+      const bool b0 = l & 1, b1 = l & 2;
+      const float p0 = (b0 ? q[1] : q[0]) + __shfl_xor_sync(0xffffffffu, b0 ? q[0] : q[1], 1);
+      const float p1 = (b0 ? q[3] : q[2]) + __shfl_xor_sync(0xffffffffu, b0 ? q[2] : q[3], 1);
+      float ss = (b1 ? p1 : p0) + __shfl_xor_sync(0xffffffffu, b1 ? p0 : p1, 2);
+      for (int k = 4; 8 * k < hd; k <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, k);
+      const float rstd = rsqrtf(fmaf(ss, inv_hd, eps));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rs[i] = __shfl_sync(0xffffffffu, rstd, i, 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int h = h0 + i * step + g;
+      if (!on || h >= sd.heads) continue;
+      f32x2 v[4];
+      e[i].get(v);
+      if (NORM && wt) {
+        const f32x2 r2 = f2u(rs[i], rs[i]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = fmul2(fmul2(v[k], r2), w[k]);
+      }
+      if (turned) {
+        // (single operations: building packed pairs of cosines costs more than they save)
+        if (HALVES) {   // v[0], v[1]: four of the first half, v[2], v[3]: of the second
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float x0 = lo_f(v[k]), x1 = hi_f(v[k]), y0 = lo_f(v[k + 2]), y1 = hi_f(v[k + 2]);
+            v[k] = f2u(x0 * c[2 * k] - y0 * s[2 * k], x1 * c[2 * k + 1] - y1 * s[2 * k + 1]);
+            v[k + 2] = f2u(x0 * s[2 * k] + y0 * c[2 * k], x1 * s[2 * k + 1] + y1 * c[2 * k + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x0 = lo_f(v[k]), y0 = hi_f(v[k]);
+            v[k] = f2u(x0 * c[k] - y0 * s[k], x0 * s[k] + y0 * c[k]);
+          }
+        }
+      }
+      Eight<T>::store(o + h * hd + lo, o + h * hd + hi, v);
     }
   }
 }
 
-// Any head width, stride and alignment: one block to a row, a warp to a head, the head
-// in shared memory.
-template <class T>
-__global__ void __launch_bounds__(256) k_rope_any(const __grid_constant__ RopeArgs a) {
-  __shared__ float2 cs[ROPE_PAIRS];
-  __shared__ float buf[8][2 * ROPE_PAIRS];
-  const long long r = blockIdx.x;
-  const int np = a.rot >> 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// R rows to a block, 2^lgl lanes to a head; a group of lanes stays with one row (its
+// sines and cosines in registers) and takes every step-th head of it, step = groups / R.
+// The first loads are under way while the block forms its sines and cosines.
+// NORM: some side has a weight.  HALVES: pairs are half a width apart.
+template <class T, bool NORM, bool HALVES>
+__global__ void __launch_bounds__(256) k_rope(long long rows, int lgr, int lgl, const __grid_constant__ RopeArgs a) {
+  __shared__ __align__(16) float2 cs[ROPE_ROWS][ROPE_PAIRS];
+  const int np = a.rot >> 1, R = 1 << lgr;
+  const long long r0 = (long long)blockIdx.x << lgr;
+  const int n = (int)min((long long)R, rows - r0);
+  const int l = threadIdx.x & ((1 << lgl) - 1), grp = threadIdx.x >> lgl;
+  const int step = 256 >> (lgl + lgr), row = grp / step, g = grp & (step - 1);   // (a warp's groups: heads side by side)
+  const bool turned = 8 * l < a.rot, on = row < n && 8 * l < a.hd;
+  // the lane's columns of a head: first four, last four
+  const int lo = HALVES && turned ? 4 * l : 8 * l, hi = HALVES && turned ? np + 4 * l : 8 * l + 4;
+  const float inv_hd = 1.f / (float)a.hd;
+  float c[4] = {}, s[4] = {};
+  bool made = false;
   pdl_trigger();
   pdl_wait();
-  for (int p = threadIdx.x; p < np; p += 256) cs[p] = turn(a.pos[a.axis[p] * a.ld_pos + r], a.freq[p]);
+  auto make = [&] {
+    const int up = (np + 3) & ~3;   // (a lane's four pairs may end past the last: not turned)
+    for (int i = threadIdx.x; i < n * up; i += 256) {
+      const int r = i / up, p = i - r * up;
+      cs[r][p] = p < np ? turn(a.pos[a.axis[p] * a.ld_pos + r0 + r], a.freq[p]) : make_float2(1.f, 0.f);
+    }
+  };
+  rope_side<T, NORM, HALVES>(a.side[0], r0 + row, g, step, l, lo, hi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+  rope_side<T, NORM, HALVES>(a.side[1], r0 + row, g, step, l, lo, hi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+}
+
+// Any head width, stride and alignment: R rows to a block, a warp to a head, a lane
+// to every 32nd pair and every 32nd column that is not turned.
+template <class T>
+__global__ void __launch_bounds__(256) k_rope_any(long long rows, int R, const __grid_constant__ RopeArgs a) {
+  __shared__ float2 cs[ROPE_ROWS][ROPE_PAIRS];
+  const long long r0 = (long long)blockIdx.x * R;
+  const int n = (int)min((long long)R, rows - r0);
+  const int np = a.rot >> 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int hq = a.side[0].heads, H = hq + a.side[1].heads;
+  const float inv_hd = 1.f / (float)a.hd;
+  pdl_trigger();
+  pdl_wait();
+  for (int i = threadIdx.x; i < n * np; i += 256) {
+    const int k = i / np, p = i - k * np;
+    cs[k][p] = turn(a.pos[a.axis[p] * a.ld_pos + r0 + k], a.freq[p]);
+  }
   __syncthreads();
-  for (int h = warp; h < a.side[0].heads + a.side[1].heads; h += 8) {
-    const RopeSide& sd = a.side[h < a.side[0].heads ? 0 : 1];
-    const long long at = (long long)(h < a.side[0].heads ? h : h - a.side[0].heads) * a.hd;
-    const T* x = reinterpret_cast<const T*>(sd.x) + r * sd.ldx + at;
-    T* o = reinterpret_cast<T*>(sd.out) + r * sd.ldo + at;
-    const T* w = reinterpret_cast<const T*>(sd.weight);
-    float ss = 0.f;
-    for (int c = lane; c < a.hd; c += 32) {
-      const float v = to_f(x[c]);
-      buf[warp][c] = v;
-      ss = fmaf(v, v, ss);
+  for (int unit = warp; unit < n * H; unit += 8) {
+    const int row = unit / H, h = unit - row * H;
+    const long long r = r0 + row;
+    const bool second = h >= hq;
+    const long long at = (long long)(second ? h - hq : h) * a.hd;
+    const T* x = reinterpret_cast<const T*>(second ? a.side[1].x : a.side[0].x) + r * (second ? a.side[1].ldx : a.side[0].ldx) + at;
+    T* o = reinterpret_cast<T*>(second ? a.side[1].out : a.side[0].out) + r * (second ? a.side[1].ldo : a.side[0].ldo) + at;
+    const T* w = reinterpret_cast<const T*>(second ? a.side[1].weight : a.side[0].weight);
+    const T* x1 = x + (a.halves ? np : 1);   // a pair's second column
+    const int ps = a.halves ? 1 : 2, rest = a.hd - a.rot;
+    float u[4], v[4], t[8], ss = 0.f;   // pairs, columns past rot
+    // (the loops end, for the whole warp, with the last column)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (32 * i >= np) break;
+      const int p = lane + 32 * i;
+      u[i] = p < np ? to_f(x[ps * p]) : 0.f;
+      v[i] = p < np ? to_f(x1[ps * p]) : 0.f;
+      ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (32 * i >= rest) break;
+      t[i] = lane + 32 * i < rest ? to_f(x[a.rot + lane + 32 * i]) : 0.f;
+      ss = fmaf(t[i], t[i], ss);
     }
     if (w) {
 #pragma unroll
       for (int k = 16; k; k >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, k);
-      const float rstd = rsqrtf(ss / (float)a.hd + a.eps);
-      for (int c = lane; c < a.hd; c += 32) buf[warp][c] *= rstd * to_f(w[c]);
+      const float rstd = rsqrtf(fmaf(ss, inv_hd, a.eps));
+      const T* w1 = w + (a.halves ? np : 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (32 * i >= np) break;
+        const int p = min(lane + 32 * i, np - 1);
+        u[i] *= rstd * to_f(w[ps * p]);
+        v[i] *= rstd * to_f(w1[ps * p]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (32 * i >= rest) break;
+        t[i] *= rstd * to_f(w[min(a.rot + lane + 32 * i, a.hd - 1)]);
+      }
     }
-    __syncwarp();
-    for (int p = lane; p < np; p += 32) {
-      const int i = a.halves ? p : 2 * p, j = a.halves ? p + np : 2 * p + 1;
-      const float u = buf[warp][i], v = buf[warp][j];
-      o[i] = from_f<T>(u * cs[p].x - v * cs[p].y);
-      o[j] = from_f<T>(u * cs[p].y + v * cs[p].x);
+    T* o1 = o + (a.halves ? np : 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (32 * i >= np) break;
+      const int p = lane + 32 * i;
+      if (p < np) {
+        const float2 c = cs[row][p];
+        o[ps * p] = from_f<T>(u[i] * c.x - v[i] * c.y);
+        o1[ps * p] = from_f<T>(u[i] * c.y + v[i] * c.x);
+      }
     }
-    for (int c = a.rot + lane; c < a.hd; c += 32) o[c] = from_f<T>(buf[warp][c]);
-    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (32 * i >= rest) break;
+      if (lane + 32 * i < rest) o[a.rot + lane + 32 * i] = from_f<T>(t[i]);
+    }
   }
 }
 
 template <class T>
 cudaError_t rope(long long rows, const RopeArgs& a, cudaStream_t s) {
-  // four-element vectors: rows, heads and both halves on their boundary
-  bool vec = a.hd % 8 == 0 && a.rot % 8 == 0;
+  // four-element vectors: rows, heads and both halves on their boundary; four lanes to a
+  // head at least
+  bool vec = a.hd % 8 == 0 && (!a.halves || a.rot % 8 == 0) && a.hd > 16;
   for (const RopeSide& sd : a.side)
     if (sd.heads)
       vec = vec && sd.ldx % 4 == 0 && sd.ldo % 4 == 0 &&
             !(((uintptr_t)sd.x | (uintptr_t)sd.out | (uintptr_t)sd.weight) & (4 * sizeof(T) - 1));
   if (!vec) {
-    const cudaError_t e = launch_pdl(k_rope_any<T>, (unsigned)rows, 256, 0, s, a);
+    int R = ROPE_ROWS;
+    while (R > 1 && rows / R < 4 * 152) R /= 2;
+    const cudaError_t e = launch_pdl(k_rope_any<T>, (unsigned)((rows + R - 1) / R), 256, 0, s, rows, R, a);
     return e != cudaSuccess ? e : launched();
   }
-  int lgl = 0;
+  int lgl = 0, lgr = 0;
   while (8 << lgl < a.hd) ++lgl;
-  const int H = a.side[0].heads + a.side[1].heads, groups = 256 >> lgl;
-  // even rounds over the heads; rows side by side where the heads leave groups over;
-  // four rows at a time to a group, fewer where the rows would not fill the SMs
-  const int rounds = (H + groups - 1) / groups, hc = (H + rounds - 1) / rounds;
-  const int par = std::min(ROPE_ROWS, groups / hc);
-  int R = std::min(ROPE_ROWS, 4 * par);
-  while (R > par && (rows + R - 1) / R < 2 * 152) R = std::max(par, R / 2);
-  const long long grid = (rows + R - 1) / R;
-  // few rows: the rounds over the heads are blocks of their own
-  const dim3 grid2((unsigned)grid, grid < 152 ? rounds : 1);
+  // rows to a block: as many as leave a group of lanes four heads of the larger side at
+  // a time, fewer where the rows would not fill the SMs twice
+  const int heads = std::max(a.side[0].heads, a.side[1].heads), groups = 256 >> lgl;
+  while ((2 << lgr) <= std::min(ROPE_ROWS, groups) && (groups >> lgr) * 4 > heads && rows >> (lgr + 1) >= 2 * 152) ++lgr;
+  const long long grid = (rows + (1 << lgr) - 1) >> lgr;
   const bool norm = a.side[0].weight || a.side[1].weight;
   auto fn = norm ? (a.halves ? k_rope<T, true, true> : k_rope<T, true, false>)
                  : (a.halves ? k_rope<T, false, true> : k_rope<T, false, false>);
-  const cudaError_t e = launch_pdl(fn, grid2, 256, 0, s, rows, R, lgl, hc, par, a);
+  const cudaError_t e = launch_pdl(fn, (unsigned)grid, 256, 0, s, rows, lgr, lgl, a);
   return e != cudaSuccess ? e : launched();
 }
 

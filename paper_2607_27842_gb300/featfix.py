@@ -558,19 +558,25 @@ def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None,
     dt = _dt(dtype)
     n = len(axis_dims)
     rows = _dims(pos, "pos")[1]
-    side = []
-    for name, x, o, w in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
-        if x is None:
-            side += [None, 0, 0, None, None, 0]
-            continue
-        width = _dims(x, name)[1]
-        if width % head_dim:
-            _bad("%s: %d columns are no whole number of heads" % (name, width))
-        side += [*_mat(x, name, dt, rows, width), width // head_dim, _vec(w, name + "_weight", dt, head_dim),
-                 *_mat(o, name + "_out", dt, rows, width)]
+    qw = kw = hq = hk = 0
+    if q is not None:
+        qw = _dims(q, "q")[1]
+        hq = qw // head_dim
+    if k is not None:
+        kw = _dims(k, "k")[1]
+        hk = kw // head_dim
+    if hq * head_dim != qw or hk * head_dim != kw:
+        _bad("%d and %d columns are no whole numbers of heads" % (qw, kw))
+    qp, ldq = _mat(q, "q", dt, rows, qw)
+    qo, ldqo = _mat(q_out, "q_out", dt, rows, qw)
+    kp, ldk = _mat(k, "k", dt, rows, kw)
+    ko, ldko = _mat(k_out, "k_out", dt, rows, kw)
+    pp, ldp = _mat(pos, "pos", _I32, n, rows)
     flags = (ROPE_HALVES if halves else 0) | (ROPE_ONE_LADDER if one_ladder else 0) | (ROPE_INVERSE if inverse else 0)
-    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_INTS[n] if n < 9 else _I * n)(*axis_dims), *_mat(pos, "pos", _I32, n, rows), theta,
-                                 flags, *side, eps, _stream_ptr(stream)))
+    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_INTS[n] if n < 9 else _I * n)(*axis_dims), pp, ldp, theta, flags,
+                                 qp, ldq, hq, _vec(q_weight, "q_weight", dt, head_dim), qo, ldqo,
+                                 kp, ldk, hk, _vec(k_weight, "k_weight", dt, head_dim), ko, ldko, eps,
+                                 _stream_ptr(stream)))
 
 
 class FeatFix:
