@@ -172,6 +172,11 @@ FEATFIX_API featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, cons
                                 long long ld_resid, void* dev_out, long long ld_out, void* dev_q, long long ld_q,
                                 float* dev_q_scale, long long ld_q_scale, void* stream);
 
+/* Waits for the current device and returns FEATFIX_ERR_CUDA if a bounded wait inside a
+ * featfix_op_gemm8 kernel gave up since the last call (its results are then
+ * incomplete), FEATFIX_OK otherwise.  Not for use while a stream is captured.   */
+FEATFIX_API featfix_status featfix_op_gemm8_watchdog(void);
+
 /* Rotary positions on the heads of q [rows, q_heads * head_dim] and k [rows,
  * k_heads * head_dim] (shared key heads: k_heads below q_heads; either may be
  * absent with 0 heads).  axis_dims (host, n_axes even numbers, n_axes <= 8) are the

@@ -1076,4 +1076,12 @@ cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_
   return g.out ? gemm8_t<bf16, false>(M, N, K, g, s) : gemm8_t<bf16, true>(M, N, K, g, s);
 }
 
+cudaError_t gemm8_watchdog_take(unsigned int* flags) {
+  const unsigned int zero = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(flags, g_watchdog8, sizeof(*flags));
+  if (e == cudaSuccess && *flags) e = cudaMemcpyToSymbol(g_watchdog8, &zero, sizeof(zero));
+  return e;
+}
+
 }  // namespace ff

@@ -179,6 +179,11 @@ featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, const void* dev_
   return st(gemm8((DType)dtype, M, N, K, g, (cudaStream_t)stream));
 }
 
+featfix_status featfix_op_gemm8_watchdog(void) {
+  unsigned int flags = 0;
+  return gemm8_watchdog_take(&flags) == cudaSuccess && !flags ? FEATFIX_OK : FEATFIX_ERR_CUDA;
+}
+
 featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_axes, const int* axis_dims,
                                const int* dev_pos, long long ld_pos, double theta, unsigned flags, const void* dev_q,
                                long long ld_q, int q_heads, const void* dev_q_weight, void* dev_q_out,

@@ -60,6 +60,8 @@ struct Gemm8Args {
   Quant8Out q8;
 };
 cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s);
+// The watchdog flags of gemm8's kernels, cleared; waits for the device.
+cudaError_t gemm8_watchdog_take(unsigned int* flags);
 
 // Magnitudes compare as their bits do; a NaN is above infinity, so a block's
 // maximum carries both on into its scale (fmaxf would drop the NaN).

@@ -99,6 +99,7 @@ SIGNATURES = {
     "featfix_op_quant8": (_I, [_I, _I, _LL, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP]),
     "featfix_op_gemm8": (_I, [_I, _I, _I, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _I, _VP, _LL, _I, _VP, _LL,
                               _VP, _LL, _VP, _LL, _VP, _LL, _VP]),
+    "featfix_op_gemm8_watchdog": (_I, []),
     "featfix_op_rope": (_I, [_I, _LL, _I, _I, _P(_I), _VP, _LL, _D, ctypes.c_uint, _VP, _LL, _I, _VP, _VP, _LL, _VP,
                              _LL, _I, _VP, _VP, _LL, ctypes.c_float, _VP]),
 }
@@ -549,6 +550,11 @@ def featfix_op_gemm8(dtype, a, a_scale, w, w_scale, out=None, bias=None, act=0, 
                                   _vec(bias, "bias", dt, N), act, gp, gs, rows_per_batch,
                                   *_mat(resid, "resid", dt, M, N), *_mat(out, "out", dt, M, N),
                                   *_quant8(q, q_scale, M, N), _stream_ptr(stream)))
+
+
+def featfix_op_gemm8_watchdog():
+    """Waits for the device; raises if a wait inside a gemm8 kernel gave up."""
+    _check(lib().featfix_op_gemm8_watchdog())
 
 
 def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None, k_out=None, theta=10000.0, halves=False,

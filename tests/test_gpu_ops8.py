@@ -291,7 +291,8 @@ def test_gemm8(cuda, dtype, M, N, K):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,N,K,rpb", [(1, 130, 256, 1), (5, 1000, 300, 2), (70, 512, 128, 7), (300, 1152, 512, 256),
-                                       (1030, 1032, 256, 40), (2050, 2304, 384, 1000)])
+                                       (1030, 1032, 256, 40), (2050, 2304, 384, 1000),
+                                       (3100, 1537, 200, 300), (2600, 2050, 130, 9)])
 @pytest.mark.parametrize("extra", [0, 5, 8])
 def test_gemm8_gate_and_residual(cuda, dtype, M, N, K, rpb, extra):
     td = TD[dtype]
@@ -369,6 +370,13 @@ def test_gemm8_offsets_past_32_bits(cuda):
     check(out, ref + r.double(), "bf16", mag * 2.0 ** -16 + (ref.abs() + r.double().abs()) * 2.0 ** -23)
 
 
+@pytest.mark.parametrize("M", [4, 300, 3000])
+def test_gemm8_watchdog_is_quiet(cuda, M):
+    a, sa, w, sw = gemm_inputs(M, 300, 700, 63)
+    ff.featfix_op_gemm8("f32", a, sa, w, sw, out=held(M, 300, torch.float32))
+    ff.featfix_op_gemm8_watchdog()
+
+
 # ----------------------------------------------------------------------------
 # rotary positions
 # ----------------------------------------------------------------------------
@@ -398,7 +406,8 @@ def rope_ref(x, pos, axes, hd, theta, halves, ladder, inverse, weight, eps):
     (300, 4, 4, 72, (24, 24, 24), False, 8), (33, 2, 1, 80, (20, 30), True, 0), (17, 6, 2, 96, (96,), False, 0),
     (260, 8, 8, 128, (16, 56, 56), False, 0), (9, 5, 5, 256, (64, 64, 64, 64), False, 3), (40, 2, 2, 50, (6, 10, 14), False, 0),
     (2100, 16, 16, 64, (16, 24, 24), False, 0), (70, 3, 0, 128, (64,), True, 8), (3, 40, 10, 66, (66,), False, 0),
-    (4, 1, 1, 16, (2, 2, 2, 2, 2, 2, 2, 2), False, 0)])
+    (4, 1, 1, 16, (2, 2, 2, 2, 2, 2, 2, 2), False, 0),
+    (1300, 6, 2, 128, (54, 20), True, 8), (45, 3, 1, 40, (14, 8), False, 0)])
 def test_rope(cuda, dtype, halves, norm, rows, hq, hk, hd, axes, ladder, extra):
     td, theta, eps = TD[dtype], 10000.0, 1e-6
     qkv = randn((rows, (hq + 2 * hk) * hd + extra), 70).to(td)
