@@ -4,14 +4,17 @@ Each translation unit under csrc/ is compiled to an object in parallel, then
 the objects are linked into ``paper_2607_27842_gb300/libfeatfix.so``.  The
 CUDA runtime is linked statically; the driver entry point used for TMA
 descriptors is resolved at run time, so the library loads on a machine
-without a GPU.
+without a GPU.  Beside it g++ builds ``_ops8.so``, the Python module that
+marshals the 8-bit operators' arguments (csrc/py_ops8.cpp).
 """
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -24,6 +27,11 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", 
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 SOURCES = ["ff_elementwise.cu", "ff_simt.cu", "ff_gemm_tc.cu", "ff_attention.cu", "ff_attention_tc.cu", "ff_runtime.cu", "ff_ops.cu", "ff_noalloc.cu",
            "ff_rows8.cu", "ff_rope.cu", "ff_gemm8.cu"]
+
+
+# the Python module that marshals the 8-bit operators' arguments (C++ only)
+BINDING = "py_ops8.cpp"
+BINDING_LIB = os.path.join(HERE, "_ops8.so")
 
 
 def nvcc():
@@ -42,11 +50,42 @@ def _compile(src, extra):
     return obj, r.stderr
 
 
+def _torch_dir():
+    """PyTorch's folder (headers and libraries), found without importing it."""
+    return importlib.util.find_spec("torch").submodule_search_locations[0]
+
+
+def _run(what, cmd):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed:\n%s\n%s" % (what, r.stdout, r.stderr))
+
+
+def _compile_binding():
+    t = os.path.join(_torch_dir(), "include")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    obj = os.path.join(BUILD_DIR, "py_ops8.o")
+    inc = [t, os.path.join(t, "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda,
+           os.path.join(ROOT, "include")]
+    _run("g++ on " + BINDING, ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden"] +
+         [x for p in inc for x in ("-isystem" if p.startswith(t) else "-I", p)] +
+         ["-c", os.path.join(CSRC, BINDING), "-o", obj])
+    return obj
+
+
+def _link_binding(obj):
+    tmp = BINDING_LIB + ".tmp"
+    _run("link of " + BINDING, ["g++", "-shared", "-o", tmp, obj, LIB, "-Wl,-rpath,$ORIGIN", "-L" +
+                                os.path.join(_torch_dir(), "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    os.replace(tmp, BINDING_LIB)
+
+
 def build(verbose=False, extra=()):
     """Compile and link; returns the library path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     extra = list(extra)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_compile_binding)
         results = list(ex.map(lambda s: _compile(s, extra), SOURCES))
     objs = [o for o, _ in results]
     if verbose:
@@ -54,11 +93,13 @@ def build(verbose=False, extra=()):
             if err.strip():
                 sys.stderr.write(err)
     tmp = LIB + ".tmp"
-    cmd = [nvcc()] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-o", tmp] + objs + ["-cudart", "static"]
+    cmd = [nvcc()] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-Xlinker", "-soname=libfeatfix.so", "-o", tmp] + objs + \
+        ["-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
     os.replace(tmp, LIB)
+    _link_binding(binding.result())
     return LIB
 
 

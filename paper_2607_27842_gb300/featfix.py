@@ -443,113 +443,53 @@ def featfix_op_attention(dtype, qkv, out, batch, n_txt, n_img, heads, head_dim, 
 
 # ----------------------------------------------------------------------------
 # 8-bit layers (featfix_ops.h): tensors are 2-D with unit column stride, any row
-# stride; 8-bit ones have an element of one byte and rows of whole 16 bytes
+# stride; 8-bit ones (float8_e4m3fn or uint8) have rows of whole 16 bytes.  Sizes,
+# types and strides are checked, and refused as FeatFixError, in the _ops8 module
+# (csrc/py_ops8.cpp).
 # ----------------------------------------------------------------------------
 
 ROPE_HALVES, ROPE_ONE_LADDER, ROPE_INVERSE = 1, 2, 4
 
-
-def _bad(msg):
-    raise FeatFixError(ERR_INVALID_ARG, msg)
+_ops8 = None
 
 
-# element types: those of the C ABI, then 8-bit values and positions
-_F32, _BF16, _Q8, _I32 = range(4)
-_torch_types = None
-_INTS = [_I * n for n in range(9)]
+def _marshal():
+    """The _ops8 module (raises when it has not been built)."""
+    global _ops8
+    if _ops8 is None:
+        lib()
+        import torch  # noqa: F401  (its libraries, which the module is linked to)
+        try:
+            from . import _ops8 as m
+        except ImportError as e:
+            raise FeatFixError(ERR_UNSUPPORTED, "_ops8 is not built; run __graft_entry__.build() (%s)" % e)
+        m.set_error(FeatFixError)
+        _ops8 = m
+    return _ops8
 
 
-def _types():
-    """The torch types that stand for each element type."""
-    global _torch_types
-    if _torch_types is None:
-        import torch
-        _torch_types = ((torch.float32,), (torch.bfloat16,), (torch.float8_e4m3fn, torch.uint8), (torch.int32,))
-    return _torch_types
-
-
-def _refuse(t, name, dtype, dims):
-    """Says what is wrong with a tensor that _mat or _vec would not take."""
-    if not t.is_cuda:
-        _bad("%s is not on the GPU" % name)
-    if t.dtype not in _types()[dtype]:
-        _bad("%s: %s where %s is expected" % (name, t.dtype, _types()[dtype][0]))
-    _bad("%s: expected adjacent columns of %s, got %s with strides %s" % (name, list(dims), list(t.shape), list(t.stride())))
-
-
-def _dims(t, name):
-    sh = t.shape
-    if len(sh) != 2:
-        _bad("%s: expected two dimensions, got %s" % (name, list(sh)))
-    return sh
-
-
-def _mat(t, name, dtype, rows, cols):
-    """(address, row stride) of a 2-D tensor of the given size; None -> NULL."""
-    if t is None:
-        return None, 0
-    if t.shape != (rows, cols) or t.dtype not in _types()[dtype] or not t.is_cuda:
-        _refuse(t, name, dtype, (rows, cols))
-    ld, one = t.stride()
-    if one != 1 and cols > 1:
-        _refuse(t, name, dtype, (rows, cols))
-    if rows == 1:   # (the stride of a single row says nothing)
-        ld = cols if dtype != _Q8 else (cols + 15) // 16 * 16
-    return t.data_ptr(), ld
-
-
-def _vec(t, name, dtype, n):
-    """Address of n adjacent elements; None -> NULL."""
-    if t is None:
-        return None
-    if t.numel() != n or t.dtype not in _types()[dtype] or not t.is_cuda or not t.is_contiguous():
-        _refuse(t, name, dtype, (n,))
-    return t.data_ptr()
-
-
-def _quant8(q, scale, rows, cols, tile=1):
-    """(q address, ld, scale address, ld) of an 8-bit tensor and its scales."""
-    if q is None and scale is None:
-        return None, 0, None, 0
-    if q is None or scale is None:
-        _bad("8-bit values and their scales come together")
-    nb = (cols + 127) // 128
-    return _mat(q, "8-bit values", _Q8, rows, cols) + (
-        _mat(scale, "scales", _F32, nb, rows) if tile == 1 else _mat(scale, "scales", _F32, (rows + 127) // 128, nb))
+def _handle(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def featfix_op_rms_norm(dtype, x, weight, eps, resid=None, sum_out=None, out=None, q=None, q_scale=None, stream=None):
     """y = rms_norm(x + resid) * weight into ``out``, or in 8 bits into ``q`` and
     ``q_scale`` [ceil(C / 128), rows]; x + resid into ``sum_out``."""
-    dt = _dt(dtype)
-    rows, C = _dims(x, "x")
-    _check(lib().featfix_op_rms_norm(dt, rows, C, *_mat(x, "x", dt, rows, C), *_mat(resid, "resid", dt, rows, C),
-                                     *_mat(sum_out, "sum_out", dt, rows, C), _vec(weight, "weight", dt, C), eps,
-                                     *_mat(out, "out", dt, rows, C), *_quant8(q, q_scale, rows, C),
-                                     _stream_ptr(stream)))
+    _marshal().rms_norm(_dt(dtype), x, weight, eps, resid, sum_out, out, q, q_scale, _handle(stream))
 
 
 def featfix_op_quant8(dtype, x, q, q_scale, tile=1, stream=None):
     """x in 8 bits: ``tile`` 1 for activations (q_scale [ceil(cols / 128), rows]),
     128 for weights (q_scale [ceil(rows / 128), ceil(cols / 128)])."""
-    dt = _dt(dtype)
-    rows, cols = _dims(x, "x")
-    _check(lib().featfix_op_quant8(dt, int(tile), rows, cols, *_mat(x, "x", dt, rows, cols),
-                                   *_quant8(q, q_scale, rows, cols, tile), _stream_ptr(stream)))
+    _marshal().quant8(_dt(dtype), x, q, q_scale, tile, _handle(stream))
 
 
 def featfix_op_gemm8(dtype, a, a_scale, w, w_scale, out=None, bias=None, act=0, gate=None, rows_per_batch=0, resid=None,
                      q=None, q_scale=None, stream=None):
     """act(a w^T + bias) of 8-bit a and w into ``out`` (resid + gate * it, where
     given), or in 8 bits into ``q`` and ``q_scale``."""
-    dt = _dt(dtype)
-    M, K = _dims(a, "a")
-    N = _dims(w, "w")[0]
-    gp, gs = (None, 0) if gate is None else _mat(gate, "gate", _F32, -(-M // max(1, rows_per_batch)), N)
-    _check(lib().featfix_op_gemm8(dt, M, N, K, *_quant8(a, a_scale, M, K), *_quant8(w, w_scale, N, K, 128),
-                                  _vec(bias, "bias", dt, N), act, gp, gs, rows_per_batch,
-                                  *_mat(resid, "resid", dt, M, N), *_mat(out, "out", dt, M, N),
-                                  *_quant8(q, q_scale, M, N), _stream_ptr(stream)))
+    _marshal().gemm8(_dt(dtype), a, a_scale, w, w_scale, out, bias, act, gate, rows_per_batch, resid, q, q_scale,
+                     _handle(stream))
 
 
 def featfix_op_gemm8_watchdog():
@@ -561,28 +501,9 @@ def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None,
                     one_ladder=False, inverse=False, q_weight=None, k_weight=None, eps=1e-6, stream=None):
     """Rotary positions on q [rows, heads * head_dim] and k: ``pos`` int32 [axes,
     rows], ``axis_dims`` the columns of a head that each axis turns."""
-    dt = _dt(dtype)
-    n = len(axis_dims)
-    rows = _dims(pos, "pos")[1]
-    qw = kw = hq = hk = 0
-    if q is not None:
-        qw = _dims(q, "q")[1]
-        hq = qw // head_dim
-    if k is not None:
-        kw = _dims(k, "k")[1]
-        hk = kw // head_dim
-    if hq * head_dim != qw or hk * head_dim != kw:
-        _bad("%d and %d columns are no whole numbers of heads" % (qw, kw))
-    qp, ldq = _mat(q, "q", dt, rows, qw)
-    qo, ldqo = _mat(q_out, "q_out", dt, rows, qw)
-    kp, ldk = _mat(k, "k", dt, rows, kw)
-    ko, ldko = _mat(k_out, "k_out", dt, rows, kw)
-    pp, ldp = _mat(pos, "pos", _I32, n, rows)
     flags = (ROPE_HALVES if halves else 0) | (ROPE_ONE_LADDER if one_ladder else 0) | (ROPE_INVERSE if inverse else 0)
-    _check(lib().featfix_op_rope(dt, rows, head_dim, n, (_INTS[n] if n < 9 else _I * n)(*axis_dims), pp, ldp, theta, flags,
-                                 qp, ldq, hq, _vec(q_weight, "q_weight", dt, head_dim), qo, ldqo,
-                                 kp, ldk, hk, _vec(k_weight, "k_weight", dt, head_dim), ko, ldko, eps,
-                                 _stream_ptr(stream)))
+    _marshal().rope(_dt(dtype), pos, axis_dims, head_dim, q, q_out, k, k_out, theta, flags, q_weight, k_weight, eps,
+                    _handle(stream))
 
 
 class FeatFix:
