@@ -273,22 +273,38 @@ __device__ __noinline__ void block_out(const uint8_t* b, T* dst, long long ld, i
   if (!(((uintptr_t)dst | (uintptr_t)(ld * sizeof(T))) & 3)) {
     const int n = cols - E * lane;   // elements of this lane's four bytes
     T* p = dst + E * lane;
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r, p += ld) {
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(b + sw128_off(r, lane >> 2) + (lane & 3) * 4);
-      if (n >= E) {
-        *reinterpret_cast<uint32_t*>(p) = v;
-      } else {
-        for (int i = 0; i < n; ++i) p[i] = reinterpret_cast<const T*>(&v)[i];
+    for (int r0 = 0; r0 < rows; r0 += 8) {   // (as in block_in: loads in front of stores)
+      uint32_t v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const uint32_t*>(b + sw128_off(r0 + i, lane >> 2) + (lane & 3) * 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i, p += ld) {
+        if (r0 + i >= rows) break;
+        if (n >= E) {
+          *reinterpret_cast<uint32_t*>(p) = v[i];
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (e < n) p[e] = reinterpret_cast<const T*>(&v[i])[e];
+        }
       }
     }
   } else {
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r)
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+      T v[8][E];
 #pragma unroll
-      for (int j = lane; j < 128 / (int)sizeof(T); j += 32)
-        if (j < cols)
-          dst[r * ld + j] = *reinterpret_cast<const T*>(b + sw128_off(r, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16);
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int j = lane + 32 * e;
+          v[i][e] = *reinterpret_cast<const T*>(b + sw128_off(r0 + i, j * (int)sizeof(T) / 16) + j * sizeof(T) % 16);
+        }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (r0 + i < rows && lane + 32 * e < cols) dst[(r0 + i) * ld + lane + 32 * e] = v[i][e];
+    }
   }
 }
 
