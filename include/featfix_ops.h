@@ -133,7 +133,8 @@ FEATFIX_API featfix_status featfix_op_attention(int dtype, const void* dev_qkv, 
  * Pointers to 8-bit tensors are 16-byte aligned, all others need only their
  * element's alignment (16-byte aligned rows are faster); dtypes are
  * FEATFIX_DTYPE_F32 / _BF16; row strides are in elements.  Sizes of zero rows
- * are allowed and do nothing.  No call allocates or keeps anything.
+ * are allowed and do nothing; no dimension exceeds 2^31 - 256.  No call allocates or
+ * keeps anything.
  * ------------------------------------------------------------------------- */
 
 /* Root-mean-square norm of rows of C columns (C <= 32768) with the residual's
@@ -190,7 +191,7 @@ FEATFIX_API featfix_status featfix_op_gemm8_watchdog(void);
  * so the gradient of the rotation.  q_weight / k_weight ([head_dim] in dtype,
  * nullable) put the root-mean-square norm of each head, times the weight, in front
  * of the rotation (not with INVERSE).  Outputs may be their inputs.  head_dim is
- * even and at most 256.                                                      */
+ * even and at most 256, q_heads + k_heads at most 65535.                                                      */
 #define FEATFIX_ROPE_HALVES 1u
 #define FEATFIX_ROPE_ONE_LADDER 2u
 #define FEATFIX_ROPE_INVERSE 4u

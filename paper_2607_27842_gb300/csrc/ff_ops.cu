@@ -13,6 +13,8 @@ namespace {
 
 bool dt_ok(int dt) { return dt == FEATFIX_DTYPE_F32 || dt == FEATFIX_DTYPE_BF16; }
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// largest dimension of the 8-bit layers: rounding up to a tile stays an int
+constexpr long long DIM_MAX = 0x7fffff00;
 // every given pointer on its element's boundary
 bool el_al(int dt, std::initializer_list<const void*> ps) {
   for (const void* p : ps)
@@ -131,7 +133,7 @@ featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void*
                                    const void* dev_resid, long long ld_resid, void* dev_sum, long long ld_sum,
                                    const void* dev_weight, float eps, void* dev_out, long long ld_out, void* dev_q,
                                    long long ld_q, float* dev_scale, long long ld_scale, void* stream) {
-  if (!dt_ok(dtype) || rows < 0 || rows > 0x7fffffff || C <= 0 || C > 32768 || !(eps >= 0.f))
+  if (!dt_ok(dtype) || rows < 0 || rows > DIM_MAX || C <= 0 || C > 32768 || !(eps >= 0.f))
     return FEATFIX_ERR_INVALID_ARG;
   if (rows == 0) return FEATFIX_OK;
   if (!dev_x || ld_x < C || (dev_out != nullptr) == (dev_q != nullptr)) return FEATFIX_ERR_INVALID_ARG;
@@ -145,7 +147,7 @@ featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void*
 
 featfix_status featfix_op_quant8(int dtype, int tile, long long rows, int cols, const void* dev_x, long long ld_x,
                                  void* dev_q, long long ld_q, float* dev_scale, long long ld_scale, void* stream) {
-  if (!dt_ok(dtype) || (tile != 1 && tile != 128) || rows < 0 || rows > 0x7fffffff || cols <= 0)
+  if (!dt_ok(dtype) || (tile != 1 && tile != 128) || rows < 0 || rows > DIM_MAX || cols <= 0 || cols > DIM_MAX)
     return FEATFIX_ERR_INVALID_ARG;
   if (rows == 0) return FEATFIX_OK;
   if (!dev_x || ld_x < cols) return FEATFIX_ERR_INVALID_ARG;
@@ -160,7 +162,8 @@ featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, const void* dev_
                                 const float* dev_gate, long long gate_stride, int rows_per_batch, const void* dev_resid,
                                 long long ld_resid, void* dev_out, long long ld_out, void* dev_q, long long ld_q,
                                 float* dev_q_scale, long long ld_q_scale, void* stream) {
-  if (!dt_ok(dtype) || M < 0 || N <= 0 || K <= 0 || (act != 0 && act != 1)) return FEATFIX_ERR_INVALID_ARG;
+  if (!dt_ok(dtype) || M < 0 || N <= 0 || K <= 0 || M > DIM_MAX || N > DIM_MAX || K > DIM_MAX || (act != 0 && act != 1))
+    return FEATFIX_ERR_INVALID_ARG;
   if (M == 0) return FEATFIX_OK;
   if ((dev_out != nullptr) == (dev_q != nullptr)) return FEATFIX_ERR_INVALID_ARG;
   // (the operands' scales are only read: q8_ok asks for the same of inputs and outputs)
@@ -190,9 +193,10 @@ featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_ax
                                long long ld_q_out, const void* dev_k, long long ld_k, int k_heads,
                                const void* dev_k_weight, void* dev_k_out, long long ld_k_out, float eps,
                                void* stream) {
-  if (!dt_ok(dtype) || rows < 0 || rows > 0x7fffffff || head_dim <= 0 || head_dim % 2 || head_dim > 2 * ROPE_PAIRS ||
+  if (!dt_ok(dtype) || rows < 0 || rows > DIM_MAX || head_dim <= 0 || head_dim % 2 || head_dim > 2 * ROPE_PAIRS ||
       n_axes < 1 || n_axes > 8 || !axis_dims ||
       !(theta > 0.0) || isinf(theta) || (flags & ~7u) || q_heads < 0 || k_heads < 0 || q_heads + (long long)k_heads < 1 ||
+      q_heads + (long long)k_heads > 65535 ||
       !(eps >= 0.f))
     return FEATFIX_ERR_INVALID_ARG;
   int rot = 0;

@@ -54,6 +54,11 @@ BAD += [("featfix_op_gemm8", GEMM, b) for b in (
     dict(out=NULL, gate=NULL, resid=NULL, q=P, ldq=200, qs=P, ldqs=4),
     dict(out=NULL, gate=NULL, resid=NULL, q=P, ldq=208, qs=NULL, ldqs=4),
     dict(out=NULL, gate=NULL, resid=NULL, q=P, ldq=208, qs=P, ldqs=3))]
+BIG = (1 << 31) - 255
+BAD += [("featfix_op_gemm8", GEMM, b) for b in (dict(M=BIG, ldsa=1 << 31), dict(N=BIG, gs=1 << 31, ldr=1 << 31, ldo=1 << 31),
+                                               dict(K=BIG, lda=1 << 31, ldw=1 << 31, ldsw=1 << 25))]
+BAD += [("featfix_op_quant8", QUANT, dict(cols=BIG, ldx=1 << 31, ldq=1 << 31)),
+        ("featfix_op_rope", ROPE, dict(hq=65530, hd=2, axes=(2,), n_axes=1, ldq=1 << 20, ldqo=1 << 20, hk=6))]
 BAD += [("featfix_op_rope", ROPE, b) for b in (
     dict(dtype=3), dict(rows=-1), dict(hd=63), dict(hd=0), dict(hd=258, ldq=2000, ldqo=2000, ldk=2000, ldko=2000),
     dict(n_axes=0), dict(n_axes=9), dict(axes=None), dict(axes=(32, 34)), dict(axes=(31, 33)), dict(axes=(0, 64)),
