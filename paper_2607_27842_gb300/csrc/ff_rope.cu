@@ -33,26 +33,26 @@ __device__ __forceinline__ float2 turn(int pos, float2 f) {
 template <class T> struct Eight;
 template <> struct Eight<float> {
   ulonglong2 r[2];
-  __device__ __forceinline__ void load(const float* lo, const float* hi) {
+  __device__ __forceinline__ void load(const float* lo, const float* hi, int, int) {
     r[0] = *reinterpret_cast<const ulonglong2*>(lo);
     r[1] = *reinterpret_cast<const ulonglong2*>(hi);
   }
   __device__ __forceinline__ void get(f32x2 (&v)[4]) const { v[0] = r[0].x; v[1] = r[0].y; v[2] = r[1].x; v[3] = r[1].y; }
-  static __device__ __forceinline__ void store(float* lo, float* hi, const f32x2 (&v)[4]) {
+  static __device__ __forceinline__ void store(float* lo, float* hi, int, int, const f32x2 (&v)[4]) {
     *reinterpret_cast<ulonglong2*>(lo) = make_ulonglong2(v[0], v[1]);
     *reinterpret_cast<ulonglong2*>(hi) = make_ulonglong2(v[2], v[3]);
   }
 };
 template <> struct Eight<bf16> {
   uint2 r[2];
-  __device__ __forceinline__ void load(const bf16* lo, const bf16* hi) {
+  __device__ __forceinline__ void load(const bf16* lo, const bf16* hi, int, int) {
     r[0] = *reinterpret_cast<const uint2*>(lo);
     r[1] = *reinterpret_cast<const uint2*>(hi);
   }
   __device__ __forceinline__ void get(f32x2 (&v)[4]) const {
     v[0] = bf2u(r[0].x); v[1] = bf2u(r[0].y); v[2] = bf2u(r[1].x); v[3] = bf2u(r[1].y);
   }
-  static __device__ __forceinline__ void store(bf16* lo, bf16* hi, const f32x2 (&v)[4]) {
+  static __device__ __forceinline__ void store(bf16* lo, bf16* hi, int, int, const f32x2 (&v)[4]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -64,30 +64,57 @@ template <> struct Eight<bf16> {
   }
 };
 
+// The same element by element, nlo and nhi of each four: any alignment, pairs and heads
+// that end inside a lane's share.
+template <class T> struct EightAny {
+  T r[8];
+  __device__ __forceinline__ void load(const T* lo, const T* hi, int nlo, int nhi) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      r[k] = k < nlo ? lo[k] : from_f<T>(0.f);
+      r[4 + k] = k < nhi ? hi[k] : from_f<T>(0.f);
+    }
+  }
+  __device__ __forceinline__ void get(f32x2 (&v)[4]) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = f2u(to_f(r[2 * k]), to_f(r[2 * k + 1]));
+  }
+  static __device__ __forceinline__ void store(T* lo, T* hi, int nlo, int nhi, const f32x2 (&v)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k < nlo) lo[k] = from_f<T>(k & 1 ? hi_f(v[k / 2]) : lo_f(v[k / 2]));
+      if (k < nhi) hi[k] = from_f<T>(k & 1 ? hi_f(v[2 + k / 2]) : lo_f(v[2 + k / 2]));
+    }
+  }
+};
+
+template <bool C, class A, class B> struct Pick { using type = A; };
+template <class A, class B> struct Pick<false, A, B> { using type = B; };
+
 constexpr int ROPE_ROWS = 8;   // most rows to a block
 
 // Turns (and norms) a group of lanes' share of one side's heads of one row: heads g, g +
 // step, .., four at a time, their loads in front.  c, s: the lane's four cosines and
 // sines.
-template <class T, bool NORM, bool HALVES, class Make>
-__device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g, int step, int l, int lo, int hi, bool on,
-                                          bool turned, int hd, float inv_hd, float eps, float (&c)[4], float (&s)[4],
+template <class T, class E, bool NORM, bool HALVES, class Make>
+__device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g, int step, int l, int lanes, int lo, int hi,
+                                          int nlo, int nhi, bool on, bool turned, int hd, float inv_hd, float eps, float (&c)[4], float (&s)[4],
                                           const float2* cs, bool& made, const Make& make) {
   const T* x = reinterpret_cast<const T*>(sd.x) + r * sd.ldx;
   T* o = reinterpret_cast<T*>(sd.out) + r * sd.ldo;
   const T* wt = reinterpret_cast<const T*>(sd.weight);
   f32x2 w[4];
   if (NORM && wt && on) {
-    Eight<T> e;
-    e.load(wt + lo, wt + hi);
+    E e;
+    e.load(wt + lo, wt + hi, nlo, nhi);
     e.get(w);
   }
   for (int h0 = 0; h0 < sd.heads; h0 += 4 * step) {   // (the same count of rounds for every lane)
-    Eight<T> e[4];
+    E e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int h = h0 + i * step + g;
-      if (on && h < sd.heads) e[i].load(x + h * hd + lo, x + h * hd + hi);
+      if (on && h < sd.heads) e[i].load(x + h * hd + lo, x + h * hd + hi, nlo, nhi);
     }
     if (!made) {   // the block's sines and cosines; this lane's
       make();
@@ -116,7 +143,7 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
       const float p0 = (b0 ? q[1] : q[0]) + __shfl_xor_sync(0xffffffffu, b0 ? q[0] : q[1], 1);
       const float p1 = (b0 ? q[3] : q[2]) + __shfl_xor_sync(0xffffffffu, b0 ? q[2] : q[3], 1);
       float ss = (b1 ? p1 : p0) + __shfl_xor_sync(0xffffffffu, b1 ? p0 : p1, 2);
-      for (int k = 4; 8 * k < hd; k <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, k);
+      for (int k = 4; k < lanes; k <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, k);
       const float rstd = rsqrtf(fmaf(ss, inv_hd, eps));
 #pragma unroll
       for (int i = 0; i < 4; ++i) rs[i] = __shfl_sync(0xffffffffu, rstd, i, 4);
@@ -149,7 +176,7 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
           }
         }
       }
-      Eight<T>::store(o + h * hd + lo, o + h * hd + hi, v);
+      E::store(o + h * hd + lo, o + h * hd + hi, nlo, nhi, v);
     }
   }
 }
@@ -159,17 +186,31 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
 // The first loads are under way while the block forms its sines and cosines.
 // NORM: some side has a weight.  HALVES: pairs are half a width apart.  bf16: at most 64
 // registers, four blocks to an SM (14566 rows with norm 49.9 -> 44.7 us; five 50.5).
-template <class T, bool NORM, bool HALVES>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_rope(long long rows, int lgr, int lgl, const __grid_constant__ RopeArgs a) {
+// ANY: rows of any alignment and pairs that end inside a lane's four, element by element.
+template <class T, bool NORM, bool HALVES, bool ANY>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && !ANY ? 4 : 2)
+    k_rope(long long rows, int lgr, int lgl, const __grid_constant__ RopeArgs a) {
+  using E = typename Pick<ANY, EightAny<T>, Eight<T>>::type;
   __shared__ __align__(16) float2 cs[ROPE_ROWS][ROPE_PAIRS];
   const int np = a.rot >> 1, R = 1 << lgr;
   const long long r0 = (long long)blockIdx.x << lgr;
   const int n = (int)min((long long)R, rows - r0);
   const int l = threadIdx.x & ((1 << lgl) - 1), grp = threadIdx.x >> lgl;
   const int step = 256 >> (lgl + lgr), row = grp / step, g = grp & (step - 1);   // (a warp's groups: heads side by side)
-  const bool turned = 8 * l < a.rot, on = row < n && 8 * l < a.hd;
-  // the lane's columns of a head: first four, last four
-  const int lo = HALVES && turned ? 4 * l : 8 * l, hi = HALVES && turned ? np + 4 * l : 8 * l + 4;
+  // the lane's columns of a head: first four and last four, and how many of each there are
+  const bool turned = HALVES ? 4 * l < np : 8 * l < a.rot;
+  int lo = 8 * l, hi = 8 * l + 4, nlo = 4, nhi = 4;
+  if (HALVES && turned) {
+    lo = 4 * l;
+    hi = np + 4 * l;
+    if (ANY) nlo = nhi = min(4, np - 4 * l);
+  } else if (ANY) {
+    if (HALVES) lo = a.rot + 8 * (l - ((np + 3) >> 2));
+    hi = lo + 4;
+    nlo = max(0, min(4, a.hd - lo));
+    nhi = max(0, min(4, a.hd - hi));
+  }
+  const bool on = row < n && (ANY ? nlo > 0 : 8 * l < a.hd);
   const float inv_hd = 1.f / (float)a.hd;
   float c[4] = {}, s[4] = {};
   bool made = false;
@@ -182,14 +223,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_rope(long long 
       cs[r][p] = p < np ? turn(a.pos[a.axis[p] * a.ld_pos + r0 + r], a.freq[p]) : make_float2(1.f, 0.f);
     }
   };
-  rope_side<T, NORM, HALVES>(a.side[0], r0 + row, g, step, l, lo, hi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
-  rope_side<T, NORM, HALVES>(a.side[1], r0 + row, g, step, l, lo, hi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+  rope_side<T, E, NORM, HALVES>(a.side[0], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+  rope_side<T, E, NORM, HALVES>(a.side[1], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
 }
 
-// Any head width, stride and alignment: R rows to a block, a warp to a head, a lane
-// to every 32nd pair and every 32nd column that is not turned.  A head's loads, norm and
-// stores follow one another: 4000 rows of 16 heads, 74 of 128 columns turned by halves,
-// with norm 30 us (1.1 TB/s).
+// Halves with columns behind them that together need more than 32 lanes (head widths of 250
+// and up): R rows to a block, a warp to a head, a lane
+// to every 32nd pair and every 32nd column that is not turned. 
 template <class T>
 __global__ void __launch_bounds__(256) k_rope_any(long long rows, int R, const __grid_constant__ RopeArgs a) {
   __shared__ float2 cs[ROPE_ROWS][ROPE_PAIRS];
@@ -270,29 +310,34 @@ __global__ void __launch_bounds__(256) k_rope_any(long long rows, int R, const _
 
 template <class T>
 cudaError_t rope(long long rows, const RopeArgs& a, cudaStream_t s) {
-  // four-element vectors: rows, heads and both halves on their boundary; four lanes to a
-  // head at least
-  bool vec = a.hd % 8 == 0 && (!a.halves || a.rot % 8 == 0) && a.hd > 16;
+  // four-element vectors: rows, heads and both halves on their boundary
+  bool vec = a.hd % 8 == 0 && (!a.halves || a.rot % 8 == 0);
   for (const RopeSide& sd : a.side)
     if (sd.heads)
       vec = vec && sd.ldx % 4 == 0 && sd.ldo % 4 == 0 &&
             !(((uintptr_t)sd.x | (uintptr_t)sd.out | (uintptr_t)sd.weight) & (4 * sizeof(T) - 1));
-  if (!vec) {
+  // lanes to a head: eight columns each, halves that are not whole vectors with lanes of
+  // their own for the columns behind them; four at least
+  const int lanes = a.halves && !vec ? (a.rot / 2 + 3) / 4 + (a.hd - a.rot + 7) / 8 : (a.hd + 7) / 8;
+  if (lanes > 32) {
     int R = ROPE_ROWS;
     while (R > 1 && rows / R < 4 * 152) R /= 2;
     const cudaError_t e = launch_pdl(k_rope_any<T>, (unsigned)((rows + R - 1) / R), 256, 0, s, rows, R, a);
     return e != cudaSuccess ? e : launched();
   }
-  int lgl = 0, lgr = 0;
-  while (8 << lgl < a.hd) ++lgl;
+  int lgl = 2, lgr = 0;
+  while (1 << lgl < lanes) ++lgl;
   // rows to a block: as many as leave a group of lanes four heads of the larger side at
   // a time, fewer where the rows would not fill the SMs twice
   const int heads = std::max(a.side[0].heads, a.side[1].heads), groups = 256 >> lgl;
   while ((2 << lgr) <= std::min(ROPE_ROWS, groups) && (groups >> lgr) * 4 > heads && rows >> (lgr + 1) >= 2 * 152) ++lgr;
   const long long grid = (rows + (1 << lgr) - 1) >> lgr;
   const bool norm = a.side[0].weight || a.side[1].weight;
-  auto fn = norm ? (a.halves ? k_rope<T, true, true> : k_rope<T, true, false>)
-                 : (a.halves ? k_rope<T, false, true> : k_rope<T, false, false>);
+  using Fn = decltype(&k_rope<T, false, false, false>);
+  static const Fn fns[2][2][2] = {
+      {{k_rope<T, false, false, false>, k_rope<T, false, false, true>}, {k_rope<T, false, true, false>, k_rope<T, false, true, true>}},
+      {{k_rope<T, true, false, false>, k_rope<T, true, false, true>}, {k_rope<T, true, true, false>, k_rope<T, true, true, true>}}};
+  const Fn fn = fns[norm][a.halves != 0][!vec];
   const cudaError_t e = launch_pdl(fn, (unsigned)grid, 256, 0, s, rows, lgr, lgl, a);
   return e != cudaSuccess ? e : launched();
 }

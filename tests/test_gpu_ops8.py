@@ -407,7 +407,8 @@ def rope_ref(x, pos, axes, hd, theta, halves, ladder, inverse, weight, eps):
     (260, 8, 8, 128, (16, 56, 56), False, 0), (9, 5, 5, 256, (64, 64, 64, 64), False, 3), (40, 2, 2, 50, (6, 10, 14), False, 0),
     (2100, 16, 16, 64, (16, 24, 24), False, 0), (70, 3, 0, 128, (64,), True, 8), (3, 40, 10, 66, (66,), False, 0),
     (4, 1, 1, 16, (2, 2, 2, 2, 2, 2, 2, 2), False, 0),
-    (1300, 6, 2, 128, (54, 20), True, 8), (45, 3, 1, 40, (14, 8), False, 0)])
+    (1300, 6, 2, 128, (54, 20), True, 8), (45, 3, 1, 40, (14, 8), False, 0),
+    (20, 3, 1, 256, (200, 54), False, 0), (700, 5, 3, 72, (10, 20, 16), True, 1), (9, 2, 2, 34, (6, 12), False, 2)])
 def test_rope(cuda, dtype, halves, norm, rows, hq, hk, hd, axes, ladder, extra):
     td, theta, eps = TD[dtype], 10000.0, 1e-6
     qkv = randn((rows, (hq + 2 * hk) * hd + extra), 70).to(td)
