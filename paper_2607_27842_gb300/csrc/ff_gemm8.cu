@@ -111,28 +111,33 @@ __device__ __forceinline__ void arrive_read(uint32_t bar_cluster) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
 }
 
-// GELU (tanh form) of four values: x (1 + tanh u) / 2 = x / (1 + 2^t), t = -2 u
+// GELU (tanh form) of four values: x (1 + tanh u) / 2 = x f, f = 1 / (1 + 2^t), t = -2 u
 // log2(e).  One reciprocal for the four (16 a clock and SM against 32 for the
-// exponential): each denominator is capped at 2^30, past which the result is below
-// 2^-26 of x, the rounding of the tanh form.  Within 1e-6 of the exact value; the
-// hardware tanh (2^-11) would show in an 8-bit result's scales.
+// exponential): each t is capped at 31, so that the four denominators' product stays
+// finite.  A little more than the f of that cap is taken off, saturated to [0, 1], in
+// the last product of f: it is exactly 0 from the cap on (x below -5.6), however
+// large -x is, and minus infinity gives NaN as the formula does.  Within 2^-21 |x| and
+// 3e-9 of the exact value; the hardware tanh (2^-11) would show in an 8-bit result's
+// scales.
 __device__ __forceinline__ void gelu4(f32x2& a, f32x2& b) {
   constexpr float C0 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, C1 = C0 * 0.044715f;
+  constexpr float CAP = 31.f, OFF = 0x1p-31f * (1.f + 0x1p-18f);
   const f32x2 k0 = f2u(C0, C0), k1 = f2u(C1, C1), one = f2u(1.f, 1.f);
   auto denominators = [&](f32x2 v) {
     const f32x2 t = fmul2(v, ffma2(fmul2(v, v), k1, k0));
     float e0, e1;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(lo_f(t), 30.f)));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(hi_f(t), 30.f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(lo_f(t), CAP)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(hi_f(t), CAP)));
     return fadd2(f2u(e0, e1), one);
   };
+  auto factor = [](float x, float y) { return __saturatef(__fmaf_rn(x, y, -OFF)); };
   const f32x2 da = denominators(a), db = denominators(b);
   const float pa = lo_f(da) * hi_f(da), pb = lo_f(db) * hi_f(db);
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(pa * pb));
   const float ra = r * pb, rb = r * pa;   // 1 / pa, 1 / pb
-  a = f2u(lo_f(a) * (ra * hi_f(da)), hi_f(a) * (ra * lo_f(da)));
-  b = f2u(lo_f(b) * (rb * hi_f(db)), hi_f(b) * (rb * lo_f(db)));
+  a = f2u(lo_f(a) * factor(ra, hi_f(da)), hi_f(a) * factor(ra, lo_f(da)));
+  b = f2u(lo_f(b) * factor(rb, hi_f(db)), hi_f(b) * factor(rb, lo_f(db)));
 }
 
 // ---------------------------------------------------------------------------
