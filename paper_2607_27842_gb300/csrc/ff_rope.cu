@@ -93,12 +93,19 @@ template <class A, class B> struct Pick<false, A, B> { using type = B; };
 
 constexpr int ROPE_ROWS = 8;   // most rows to a block
 
+// How a head's pairs lie: neighbours whose axes fill whole lanes; neighbours, and the axes
+// end inside a lane's four; half a width apart.
+enum Form { PAIRS, PAIRS_TAIL, HALVES };
+
 // Turns (and norms) a group of lanes' share of one side's heads of one row: heads g, g +
 // step, .., four at a time, their loads in front.  c, s: the lane's four cosines and
-// sines.
-template <class T, class E, bool NORM, bool HALVES, class Make>
+// sines.  np: all pairs of a head; PAIRS_TAIL keeps what lies behind them as it is (an
+// infinity there would make its neighbour NaN, times a sine of zero).  A form of its own:
+// with the choice 14566 rows of 16 + 16 heads of 128, 74 columns turned, take 44.3 us with
+// norm instead of 41.9, and all 128 turned would take 46.6 instead of 44.6.
+template <class T, class E, bool NORM, Form FORM, class Make>
 __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g, int step, int l, int lanes, int lo, int hi,
-                                          int nlo, int nhi, bool on, bool turned, int hd, float inv_hd, float eps, float (&c)[4], float (&s)[4],
+                                          int nlo, int nhi, bool on, bool turned, int np, int hd, float inv_hd, float eps, float (&c)[4], float (&s)[4],
                                           const float2* cs, bool& made, const Make& make) {
   const T* x = reinterpret_cast<const T*>(sd.x) + r * sd.ldx;
   T* o = reinterpret_cast<T*>(sd.out) + r * sd.ldo;
@@ -161,7 +168,7 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
       }
       if (turned) {
         // (single operations: building packed pairs of cosines costs more than they save)
-        if (HALVES) {   // v[0], v[1]: four of the first half, v[2], v[3]: of the second
+        if (FORM == HALVES) {   // v[0], v[1]: four of the first half, v[2], v[3]: of the second
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const float x0 = lo_f(v[k]), x1 = hi_f(v[k]), y0 = lo_f(v[k + 2]), y1 = hi_f(v[k + 2]);
@@ -172,7 +179,8 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float x0 = lo_f(v[k]), y0 = hi_f(v[k]);
-            v[k] = f2u(x0 * c[k] - y0 * s[k], x0 * s[k] + y0 * c[k]);
+            const f32x2 t = f2u(x0 * c[k] - y0 * s[k], x0 * s[k] + y0 * c[k]);
+            v[k] = FORM == PAIRS || 4 * l + k < np ? t : v[k];
           }
         }
       }
@@ -184,10 +192,10 @@ __device__ __forceinline__ void rope_side(const RopeSide& sd, long long r, int g
 // R rows to a block, 2^lgl lanes to a head; a group of lanes stays with one row (its
 // sines and cosines in registers) and takes every step-th head of it, step = groups / R.
 // The first loads are under way while the block forms its sines and cosines.
-// NORM: some side has a weight.  HALVES: pairs are half a width apart.  bf16: at most 64
+// NORM: some side has a weight.  bf16: at most 64
 // registers, four blocks to an SM (14566 rows with norm 49.9 -> 44.7 us; five 50.5).
 // ANY: rows of any alignment and pairs that end inside a lane's four, element by element.
-template <class T, bool NORM, bool HALVES, bool ANY>
+template <class T, bool NORM, Form FORM, bool ANY>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 && !ANY ? 4 : 2)
     k_rope(long long rows, int lgr, int lgl, const __grid_constant__ RopeArgs a) {
   using E = typename Pick<ANY, EightAny<T>, Eight<T>>::type;
@@ -198,14 +206,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !ANY ? 4 : 2)
   const int l = threadIdx.x & ((1 << lgl) - 1), grp = threadIdx.x >> lgl;
   const int step = 256 >> (lgl + lgr), row = grp / step, g = grp & (step - 1);   // (a warp's groups: heads side by side)
   // the lane's columns of a head: first four and last four, and how many of each there are
-  const bool turned = HALVES ? 4 * l < np : 8 * l < a.rot;
+  const bool turned = FORM == HALVES ? 4 * l < np : 8 * l < a.rot;
   int lo = 8 * l, hi = 8 * l + 4, nlo = 4, nhi = 4;
-  if (HALVES && turned) {
+  if (FORM == HALVES && turned) {
     lo = 4 * l;
     hi = np + 4 * l;
     if (ANY) nlo = nhi = min(4, np - 4 * l);
   } else if (ANY) {
-    if (HALVES) lo = a.rot + 8 * (l - ((np + 3) >> 2));
+    if (FORM == HALVES) lo = a.rot + 8 * (l - ((np + 3) >> 2));
     hi = lo + 4;
     nlo = max(0, min(4, a.hd - lo));
     nhi = max(0, min(4, a.hd - hi));
@@ -217,14 +225,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !ANY ? 4 : 2)
   pdl_trigger();
   pdl_wait();
   auto make = [&] {
-    const int up = (np + 3) & ~3;   // (a lane's four pairs may end past the last: not turned)
+    const int up = (np + 3) & ~3;   // (whole fours: a lane reads its four at once)
     for (int i = threadIdx.x; i < n * up; i += 256) {
       const int r = i / up, p = i - r * up;
       cs[r][p] = p < np ? turn(a.pos[a.axis[p] * a.ld_pos + r0 + r], a.freq[p]) : make_float2(1.f, 0.f);
     }
   };
-  rope_side<T, E, NORM, HALVES>(a.side[0], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
-  rope_side<T, E, NORM, HALVES>(a.side[1], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+  rope_side<T, E, NORM, FORM>(a.side[0], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, np, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
+  rope_side<T, E, NORM, FORM>(a.side[1], r0 + row, g, step, l, 1 << lgl, lo, hi, nlo, nhi, on, turned, np, a.hd, inv_hd, a.eps, c, s, cs[row], made, make);
 }
 
 // Halves with columns behind them that together need more than 32 lanes (head widths of 250
@@ -333,11 +341,13 @@ cudaError_t rope(long long rows, const RopeArgs& a, cudaStream_t s) {
   while ((2 << lgr) <= std::min(ROPE_ROWS, groups) && (groups >> lgr) * 4 > heads && rows >> (lgr + 1) >= 2 * 152) ++lgr;
   const long long grid = (rows + (1 << lgr) - 1) >> lgr;
   const bool norm = a.side[0].weight || a.side[1].weight;
-  using Fn = decltype(&k_rope<T, false, false, false>);
-  static const Fn fns[2][2][2] = {
-      {{k_rope<T, false, false, false>, k_rope<T, false, false, true>}, {k_rope<T, false, true, false>, k_rope<T, false, true, true>}},
-      {{k_rope<T, true, false, false>, k_rope<T, true, false, true>}, {k_rope<T, true, true, false>, k_rope<T, true, true, true>}}};
-  const Fn fn = fns[norm][a.halves != 0][!vec];
+  using Fn = decltype(&k_rope<T, false, PAIRS, false>);
+  static const Fn fns[2][2][3] = {   // [norm][any][form]
+      {{k_rope<T, false, PAIRS, false>, k_rope<T, false, PAIRS_TAIL, false>, k_rope<T, false, HALVES, false>},
+       {nullptr, k_rope<T, false, PAIRS_TAIL, true>, k_rope<T, false, HALVES, true>}},
+      {{k_rope<T, true, PAIRS, false>, k_rope<T, true, PAIRS_TAIL, false>, k_rope<T, true, HALVES, false>},
+       {nullptr, k_rope<T, true, PAIRS_TAIL, true>, k_rope<T, true, HALVES, true>}}};
+  const Fn fn = fns[norm][!vec][a.halves ? HALVES : vec && a.rot % 8 == 0 ? PAIRS : PAIRS_TAIL];
   const cudaError_t e = launch_pdl(fn, (unsigned)grid, 256, 0, s, rows, lgr, lgl, a);
   return e != cudaSuccess ? e : launched();
 }
