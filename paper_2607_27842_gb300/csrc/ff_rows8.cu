@@ -3,6 +3,7 @@
 // weights.  Both are bound by memory: every element is read once into registers, and
 // what is written is computed from there.
 #include "ff_common.cuh"
+#include "ff_host.h"
 #include "ff_q8.cuh"
 
 #include <algorithm>
@@ -315,27 +316,20 @@ cudaError_t quant8(int tile, long long rows, int C, const void* x, long long ldx
     a.q8 = o;
     return rows8<T, false>(rows, C, a, s);
   }
-  if (tile == 1) {   // wider rows than registers hold: runs of columns, each a matrix of its own
-    for (int c = 0; c < C; c += 128 * 8 * NB_MAX) {
-      const Quant8Out part = {reinterpret_cast<uint8_t*>(o.q) + c, o.ldq, o.scale + (c / 128) * o.lds, o.lds};
-      const cudaError_t e = quant8<T>(1, rows, std::min(C - c, 128 * 8 * NB_MAX), reinterpret_cast<const T*>(x) + c, ldx, part, s);
-      if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
-  }
+  if (tile == 1)   // wider rows than registers hold: runs of columns, each a matrix of its own
+    return for_runs(C, 128 * 8 * NB_MAX, [&](long long c, long long n) {
+      const Quant8Out part = {reinterpret_cast<uint8_t*>(o.q) + c, o.ldq, o.scale + c / 128 * o.lds, o.lds};
+      return quant8<T>(1, rows, (int)n, reinterpret_cast<const T*>(x) + c, ldx, part, s);
+    });
   // (row blocks in the grid's second dimension, at most 65535 to a launch)
-  for (long long r = 0; r < rows; r += 65535 * 128ll) {
-    const long long n = std::min(rows - r, 65535 * 128ll);
+  return for_runs(rows, 65535 * 128ll, [&](long long r, long long n) {
     const T* xr = reinterpret_cast<const T*>(x) + r * ldx;
     const Quant8Out part = {reinterpret_cast<uint8_t*>(o.q) + r * o.ldq, o.ldq, o.scale + (r / 128) * o.lds, o.lds};
     const dim3 grid((C + 127) / 128, (unsigned)((n + 127) / 128));
     const cudaError_t e = C % 4 == 0 && al4<T>(x, ldx) ? launch_pdl(k_quant8_tile<T, true>, grid, 256, 0, s, n, C, xr, ldx, part)
                                                        : launch_pdl(k_quant8_tile<T, false>, grid, 256, 0, s, n, C, xr, ldx, part);
-    if (e != cudaSuccess) return e;
-    const cudaError_t l = launched();
-    if (l != cudaSuccess) return l;
-  }
-  return cudaSuccess;
+    return e != cudaSuccess ? e : launched();
+  });
 }
 
 }  // namespace
