@@ -133,7 +133,7 @@ featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void*
                                    const void* dev_resid, long long ld_resid, void* dev_sum, long long ld_sum,
                                    const void* dev_weight, float eps, void* dev_out, long long ld_out, void* dev_q,
                                    long long ld_q, float* dev_scale, long long ld_scale, void* stream) {
-  if (!dt_ok(dtype) || rows < 0 || rows > DIM_MAX || C <= 0 || C > 32768 || !(eps >= 0.f))
+  if (!dt_ok(dtype) || rows < 0 || rows > DIM_MAX || C <= 0 || C > RMS_COLS_MAX || !(eps >= 0.f))
     return FEATFIX_ERR_INVALID_ARG;
   if (rows == 0) return FEATFIX_OK;
   if (!dev_x || ld_x < C || (dev_out != nullptr) == (dev_q != nullptr)) return FEATFIX_ERR_INVALID_ARG;

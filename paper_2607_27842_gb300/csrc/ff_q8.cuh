@@ -16,6 +16,7 @@ struct Quant8Out {   // an 8-bit tensor and its scales
   float* scale;
   long long lds;
 };
+constexpr int RMS_COLS_MAX = 32768;   // widest row of the norm
 struct RmsArgs {
   const void* x; long long ldx;
   const void* resid; long long ldr;   // nullable

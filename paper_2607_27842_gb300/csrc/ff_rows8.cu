@@ -290,10 +290,11 @@ cudaError_t rows8(long long rows, int C, const RmsArgs& a, cudaStream_t s) {
   const int nb = (blocks + W - 1) / W;
   if constexpr (NORM) {
     if (nb > NB_MAX) {
-      const size_t smem = (size_t)C * 4;
-      const cudaError_t e = cudaFuncSetAttribute(k_rows8_wide<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      // (the limit of the widest row, not of this one: it is the process's, and a narrower
+      // row's call on another thread may come between it and the launch)
+      const cudaError_t e = cudaFuncSetAttribute(k_rows8_wide<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, RMS_COLS_MAX * 4);
       if (e != cudaSuccess) return e;
-      const cudaError_t l = launch_pdl(k_rows8_wide<T>, (unsigned)rows, 1024, smem, s, C, a);
+      const cudaError_t l = launch_pdl(k_rows8_wide<T>, (unsigned)rows, 1024, (size_t)C * 4, s, C, a);
       return l != cudaSuccess ? l : launched();
     }
   }
