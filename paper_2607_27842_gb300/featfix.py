@@ -443,9 +443,9 @@ def featfix_op_attention(dtype, qkv, out, batch, n_txt, n_img, heads, head_dim, 
 
 # ----------------------------------------------------------------------------
 # 8-bit layers (featfix_ops.h): tensors are 2-D with unit column stride, any row
-# stride; 8-bit ones (float8_e4m3fn or uint8) have rows of whole 16 bytes.  Sizes,
-# types and strides are checked, and refused as FeatFixError, in the _ops8 module
-# (csrc/py_ops8.cpp).
+# stride, on the current GPU; 8-bit ones (float8_e4m3fn or uint8) have rows of whole 16
+# bytes.  Devices, sizes, types and strides are checked, and refused as FeatFixError, in
+# the _ops8 module (csrc/py_ops8.cpp).
 # ----------------------------------------------------------------------------
 
 ROPE_HALVES, ROPE_ONE_LADDER, ROPE_INVERSE = 1, 2, 4
