@@ -9,6 +9,7 @@
 // a single product of scales per block and finds the largest magnitude of an 8-bit
 // result's block by itself.
 #include "ff_common.cuh"
+#include "ff_host.h"
 #include "ff_q8.cuh"
 #include "ff_tc.cuh"
 
@@ -953,7 +954,6 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
 // ---------------------------------------------------------------------------
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::once_flag g_once;
-int g_sms = 0;
 
 bool init_driver() {
   std::call_once(g_once, [] {
@@ -962,12 +962,23 @@ bool init_driver() {
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) == cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
       g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-    int dev = 0;
-    cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&g_sms, cudaDevAttrMultiProcessorCount, dev);
-    if (g_sms <= 0) g_sms = 148;
-    auto smem = [](const void* fn, size_t bytes) {
-      cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  });
+  return g_encode != nullptr;
+}
+
+// SMs of the current device; its first call sets the kernels' shared-memory limits there
+// (both are a device's own).
+PerDevice<int> g_devices;
+cudaError_t device_sms(int* sms) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= g_devices.devices) return cudaErrorInvalidDevice;
+  return g_devices.get(dev, sms, [&](int& n) {
+    cudaError_t first = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    auto smem = [&](const void* fn, size_t bytes) {
+      const cudaError_t r = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+      if (first == cudaSuccess) first = r;
     };
     auto both = [&](auto t, auto q8) {
       using T = decltype(t);
@@ -982,8 +993,8 @@ bool init_driver() {
     both(0.f, std::true_type());
     both(bf16(), std::false_type());
     both(bf16(), std::true_type());
+    return first;
   });
-  return g_encode != nullptr;
 }
 
 // Row-major [rows, cols] of `es`-byte elements in boxes of box_rows rows of 128
@@ -1025,7 +1036,7 @@ cudaError_t launch_split(int M, int N, int K, int S, const Gemm8Args& g, cudaStr
 }
 
 template <class T, bool Q8>
-cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
+cudaError_t launch_pair(int M, int N, int K, int sms, const Gemm8Args& g, cudaStream_t s) {
   constexpr int es = (int)sizeof(T);
   CUtensorMap ma, mw, mo, mr;
   if (!make_map8(&ma, g.a, 1, M, K, g.lda, 128) || !make_map8(&mw, g.w, 1, N, K, g.ldw, 128))
@@ -1043,7 +1054,7 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
     flags |= RESID_TMA;
   const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
   if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
-  const int pairs = g_sms / 2, grid = 2 * (int)(tiles < pairs ? tiles : pairs);
+  const int pairs = sms / 2, grid = 2 * (int)(tiles < pairs ? tiles : pairs);
   const cudaError_t e = launch_pdl(k_gemm8_pair<T, Q8>, grid, P_THREADS, P_SMEM, s, ma, mw, mo, mr, M, N, K, flags, g);
   return e != cudaSuccess ? e : launched();
 }
@@ -1060,11 +1071,11 @@ cudaError_t launch_pair(int M, int N, int K, const Gemm8Args& g, cudaStream_t s)
 struct Plan {
   int bt, s;   // bt 0: CTA pairs
 };
-Plan plan8(int M, int N, int K) {
+Plan plan8(int M, int N, int K, int sms) {
   const long long kb = (K + BK - 1) / BK, wt = (N + 127) / 128;
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
-  double least = (double)((pt + g_sms / 2 - 1) / (g_sms / 2)) * (0.549 * kb + 3.65) + 4.7;
+  double least = (double)((pt + sms / 2 - 1) / (sms / 2)) * (0.549 * kb + 3.65) + 4.7;
   const int bts[4] = {16, 32, 64, 128};
   const double one[4] = {0.321, 0.381, 0.365, 0.586}, two[4] = {0.300, 0.467, 0.558, 0.0}, fixed[4] = {1.73, 2.15, 5.57, 7.34};
   const double meet[4] = {0, 0.27, 0.23, 0.44};
@@ -1072,8 +1083,8 @@ Plan plan8(int M, int N, int K) {
     if (i > 0 && bts[i - 1] >= M) break;
     const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
     for (int l = 0; l < 4 && (1 << l) <= kb; ++l) {
-      const long long ctas = tiles << l, room = (long long)g_sms * (bts[i] <= 64 ? 2 : 1);
-      const bool shared = bts[i] <= 64 && ctas > g_sms;
+      const long long ctas = tiles << l, room = (long long)sms * (bts[i] <= 64 ? 2 : 1);
+      const bool shared = bts[i] <= 64 && ctas > sms;
       const double t = (double)((ctas + room - 1) / room) * ((shared ? two : one)[i] * (double)((kb + (1 << l) - 1) >> l) + fixed[i]) +
                        2.0 + meet[l] + (shared ? 0.61 : 0.0) + 0.18 * std::min(1.0, (double)ctas / (double)room);
       if (t < least) {
@@ -1087,13 +1098,16 @@ Plan plan8(int M, int N, int K) {
 
 template <class T, bool Q8>
 cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
-  const Plan p = plan8(M, N, K);
+  int sms = 0;
+  const cudaError_t e = device_sms(&sms);
+  if (e != cudaSuccess) return e;
+  const Plan p = plan8(M, N, K, sms);
   switch (p.bt) {
     case 16: return launch_split<T, Q8, 16>(M, N, K, p.s, g, s);
     case 32: return launch_split<T, Q8, 32>(M, N, K, p.s, g, s);
     case 64: return launch_split<T, Q8, 64>(M, N, K, p.s, g, s);
     case 128: return launch_split<T, Q8, 128>(M, N, K, p.s, g, s);
-    default: return launch_pair<T, Q8>(M, N, K, g, s);
+    default: return launch_pair<T, Q8>(M, N, K, sms, g, s);
   }
 }
 

@@ -1,6 +1,9 @@
 // Host-side helpers of the 8-bit layers that need no CUDA (tests compile them alone).
 #pragma once
 
+#include <atomic>
+#include <mutex>
+
 namespace ff {
 
 // Calls f(first, n) for every run of at most `step` of `total` things, in order, until one
@@ -15,5 +18,30 @@ inline auto for_runs(long long total, long long step, F f) -> decltype(f(0ll, 0l
   }
   return R(0);
 }
+
+// A value for each device, made by f(value) the first time the device is asked for; f
+// returns zero, or an error that get() returns, and the next call tries again.  Calls of
+// several threads make it once.
+template <class T, int DEVICES = 64> class PerDevice {
+  std::mutex m_;
+  std::atomic<bool> made_[DEVICES] = {};
+  T v_[DEVICES] = {};
+
+ public:
+  static constexpr int devices = DEVICES;
+  template <class F> auto get(int device, T* out, F f) -> decltype(f(v_[0])) {
+    using R = decltype(f(v_[0]));
+    if (!made_[device].load(std::memory_order_acquire)) {
+      std::lock_guard<std::mutex> lock(m_);
+      if (!made_[device].load(std::memory_order_relaxed)) {
+        const R r = f(v_[device]);
+        if (r != R(0)) return r;
+        made_[device].store(true, std::memory_order_release);
+      }
+    }
+    *out = v_[device];
+    return R(0);
+  }
+};
 
 }  // namespace ff

@@ -47,3 +47,24 @@ int main() {
   printf("%d %d", n, r);
 }""")
     assert out == ["3", "7"]
+
+
+def test_every_device_is_prepared_once(tmp_path):
+    """Each device has its value made on its own first call, by one of several threads;
+    a preparation that failed is tried again."""
+    out = run_cpp(tmp_path, """
+#include <thread>
+int main() {
+  static ff::PerDevice<int> d;
+  std::atomic<int> made[3] = {};
+  auto get = [&](int dev, int* v) { return d.get(dev, v, [&](int& x) { x = 100 + dev; return ++made[dev] == 1 && dev == 2 ? 5 : 0; }); };
+  int v = -1, failed = get(2, &v);
+  printf("%d %d ", failed, v);
+  std::vector<std::thread> t;
+  std::atomic<int> wrong{0};
+  for (int i = 0; i < 8; ++i)
+    t.emplace_back([&] { for (int k = 0; k < 300; ++k) { int x = 0; if (get(k % 3, &x) || x != 100 + k % 3) ++wrong; } });
+  for (auto& x : t) x.join();
+  printf("%d %d %d %d", wrong.load(), made[0].load(), made[1].load(), made[2].load());
+}""")
+    assert out == ["5", "-1", "0", "1", "1", "2"]
