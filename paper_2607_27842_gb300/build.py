@@ -5,7 +5,9 @@ the objects are linked into ``paper_2607_27842_gb300/libfeatfix.so``.  The
 CUDA runtime is linked statically; the driver entry point used for TMA
 descriptors is resolved at run time, so the library loads on a machine
 without a GPU.  Beside it g++ builds ``_ops8.so``, the Python module that
-marshals the 8-bit operators' arguments (csrc/py_ops8.cpp).
+marshals the 8-bit operators' arguments (csrc/py_ops8.cpp); it needs the headers of
+PyTorch and Python, and where they are missing the library is built alone (a note
+says so, and the 8-bit operators' Python calls raise).
 """
 
 import concurrent.futures
@@ -51,8 +53,22 @@ def _compile(src, extra):
 
 
 def _torch_dir():
-    """PyTorch's folder (headers and libraries), found without importing it."""
-    return importlib.util.find_spec("torch").submodule_search_locations[0]
+    """PyTorch's folder (headers and libraries), found without importing it; None
+    where it is not installed."""
+    spec = importlib.util.find_spec("torch")
+    return spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else None
+
+
+def _binding_lacks():
+    """What the binding cannot be built without and is not there, or None."""
+    if shutil.which("g++") is None:
+        return "g++"
+    t = _torch_dir()
+    if t is None or not os.path.exists(os.path.join(t, "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return "PyTorch with its headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    return None
 
 
 def _run(what, cmd):
@@ -84,8 +100,9 @@ def build(verbose=False, extra=()):
     """Compile and link; returns the library path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     extra = list(extra)
+    lacks = _binding_lacks()
     with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        binding = ex.submit(_compile_binding)
+        binding = None if lacks else ex.submit(_compile_binding)
         results = list(ex.map(lambda s: _compile(s, extra), SOURCES))
     objs = [o for o, _ in results]
     if verbose:
@@ -99,7 +116,13 @@ def build(verbose=False, extra=()):
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
     os.replace(tmp, LIB)
-    _link_binding(binding.result())
+    if lacks:
+        if os.path.exists(BINDING_LIB):   # of another build: linked to what the library was then
+            os.remove(BINDING_LIB)
+        sys.stderr.write("%s is not built (%s is missing): no Python calls of the 8-bit operators\n" %
+                         (os.path.basename(BINDING_LIB), lacks))
+    else:
+        _link_binding(binding.result())
     return LIB
 
 
