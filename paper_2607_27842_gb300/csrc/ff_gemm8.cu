@@ -665,7 +665,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
 
 // ---------------------------------------------------------------------------
 // Few rows of A: the product transposed.  128 rows of W are the M side of the
-// products, BT rows of A (16 to 128) their N side, and the blocks of K are shared out
+// products, BT rows of A (16 to 64) their N side, and the blocks of K are shared out
 // to the S CTAs of a cluster, so that a handful of rows still reads W on every SM.
 // A thread holds one row of W for BT / 2 rows of A; the scales' products are the same
 // for all of them and come from shared memory.  The cluster's partial sums meet in
@@ -675,14 +675,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
 //   warp % 4, half of the BT columns (warp - 2) / 4
 // Bound by latencies in a row with few blocks of K (start, first copies, the cluster's
 // meeting: 1 x 6144 x 2048 5.8 us, 1 x 2048 x 8192 6.6) and by the tiles' traffic from L2
-// with many CTAs (256 x 2048 x 8192 16.5 us, 100 MB of tiles).
+// with many CTAs (256 x 2048 x 8192 16.6 us with a bias, 18.3 with gate and residual, 100
+// MB of tiles).
 // ---------------------------------------------------------------------------
 constexpr int S_THREADS = 320;
 constexpr int S_TABLE = 32;   // blocks of K whose scales are in shared memory at a time
 template <int BT> struct SCfg {
-  // two CTAs to an SM up to 64 rows (deeper rings with one CTA were slower, clusters of
+  // two CTAs to an SM (deeper rings with one CTA were slower, clusters of
   // eight by half: 1 x 2048 x 8192 6.6 -> 12.4 us)
-  static constexpr int STAGES = BT == 16 || BT == 128 ? 5 : 4;
+  static constexpr int STAGES = BT == 16 ? 5 : 4;
   static constexpr uint32_t STAGE_BYTES = (128 + BT) * BK;
   static constexpr uint32_t PART_BYTES = BT * 512;   // the tile in fp32
   // up to 32 rows the partial sums have a place of their own, above it they take the
@@ -706,8 +707,7 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
       : "memory");
 }
 template <int C> __device__ __forceinline__ void tmem_read(uint32_t taddr, uint32_t (&r)[C]) {
-  if constexpr (C == 64) tmem_ld64(taddr, r);
-  else if constexpr (C == 8) tmem_ld8(taddr, r);
+  if constexpr (C == 8) tmem_ld8(taddr, r);
   else {
     float v[C];
     if constexpr (C == 32) tmem_ld32(taddr, v); else tmem_ld16(taddr, v);
@@ -723,7 +723,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 template <class T, bool Q8, int BT>
-__global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
+__global__ void __launch_bounds__(S_THREADS, 2)
     k_gemm8_split(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, int M, int N, int K,
                   int S, const __grid_constant__ Gemm8Args g) {
   using C = SCfg<BT>;
@@ -856,7 +856,7 @@ __global__ void __launch_bounds__(S_THREADS, BT == 128 ? 1 : 2)
     }
   }
   // partial sums to the CTA that finishes their rows of A: part[CTA][row of A][row of W]
-  const int lshare = (BT == 128 ? 7 : BT == 64 ? 6 : BT == 32 ? 5 : 4) - (31 - __clz(S)), share = 1 << lshare;
+  const int lshare = (BT == 64 ? 6 : BT == 32 ? 5 : 4) - (31 - __clz(S)), share = 1 << lshare;
   __syncwarp();
   if (S == 1) {
     __syncthreads();
@@ -987,7 +987,6 @@ cudaError_t device_sms(int* sms) {
       smem((const void*)k_gemm8_split<T, Q8, 16>, SCfg<16>::SMEM);
       smem((const void*)k_gemm8_split<T, Q8, 32>, SCfg<32>::SMEM);
       smem((const void*)k_gemm8_split<T, Q8, 64>, SCfg<64>::SMEM);
-      smem((const void*)k_gemm8_split<T, Q8, 128>, SCfg<128>::SMEM);
     };
     both(0.f, std::false_type());
     both(0.f, std::true_type());
@@ -1061,13 +1060,16 @@ cudaError_t launch_pair(int M, int N, int K, int sms, const Gemm8Args& g, cudaSt
 
 // The kernel and, for the split one, its rows of A to a tile and CTAs to a cluster: the
 // least time of a model in us.  A tile's time is linear in its blocks of K, tiles run in
-// waves over the SMs (two CTAs of the split kernel to an SM up to 64 rows, each slower
-// beside the other), and the cluster's meeting costs more the larger it is.  The
-// constants are fitted to 1000 timings of both kernels at 90 sizes (M 1 to 9000, N 48 to
-// 12288, K 48 to 8192, all epilogues): the choice is 1.5% slower than the best one on
-// average, 25% at worst.  Either side of it: 256 x 2048 x 8192 pairs 31 us, 128 rows and 4
-// CTAs 16.4; 512 x 2048 x 2048 pairs 12.1, 32 rows 11.4; 1024 x 2048 x 2048 pairs 12.2,
-// 64 rows 16.1.
+// waves over the SMs (two CTAs of the split kernel to an SM, each slower beside the
+// other), and the cluster's meeting costs more the larger it is.  The constants are fitted
+// to timings of all types and epilogues together, so the pairs' term is above their time
+// with a plain bias (256 x 2048 x 8192: 33 us, 43 here).  At 130 other sizes (M 1 to 14566,
+// N 48 to 12288, K 48 to 8192, all epilogues) the choice is 1.8% slower than the best one on
+// average and more than 10% at eight, most of them with one to three blocks of K; 33% at
+// worst (10585 x 69 x 317: 32 rows 12.8 us, pairs 9.7).  Either side of it, with a bias:
+// 256 x 2048 x 8192 pairs 33 us, 64 rows and 4 CTAs 16.6; 512 x 2048 x 2048 pairs 12.8, 32
+// rows 10.5; 1024 x 2048 x 2048 pairs 13.3, 64 rows 16.5.  (128 rows to a tile cost more in
+// this model than 64 at any size: twice the room, shorter tiles; there is no such kernel.)
 struct Plan {
   int bt, s;   // bt 0: CTA pairs
 };
@@ -1076,15 +1078,15 @@ Plan plan8(int M, int N, int K, int sms) {
   const long long pt = (long long)((M + 255) / 256) * ((N + 255) / 256);
   Plan best = {0, 1};
   double least = (double)((pt + sms / 2 - 1) / (sms / 2)) * (0.549 * kb + 3.65) + 4.7;
-  const int bts[4] = {16, 32, 64, 128};
-  const double one[4] = {0.321, 0.381, 0.365, 0.586}, two[4] = {0.300, 0.467, 0.558, 0.0}, fixed[4] = {1.73, 2.15, 5.57, 7.34};
+  const int bts[3] = {16, 32, 64};
+  const double one[3] = {0.321, 0.381, 0.365}, two[3] = {0.300, 0.467, 0.558}, fixed[3] = {1.73, 2.15, 5.57};
   const double meet[4] = {0, 0.27, 0.23, 0.44};
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 3; ++i) {
     if (i > 0 && bts[i - 1] >= M) break;
     const long long tiles = wt * ((M + bts[i] - 1) / bts[i]);
     for (int l = 0; l < 4 && (1 << l) <= kb; ++l) {
-      const long long ctas = tiles << l, room = (long long)sms * (bts[i] <= 64 ? 2 : 1);
-      const bool shared = bts[i] <= 64 && ctas > sms;
+      const long long ctas = tiles << l, room = 2ll * sms;
+      const bool shared = ctas > sms;
       const double t = (double)((ctas + room - 1) / room) * ((shared ? two : one)[i] * (double)((kb + (1 << l) - 1) >> l) + fixed[i]) +
                        2.0 + meet[l] + (shared ? 0.61 : 0.0) + 0.18 * std::min(1.0, (double)ctas / (double)room);
       if (t < least) {
@@ -1106,7 +1108,6 @@ cudaError_t gemm8_t(int M, int N, int K, const Gemm8Args& g, cudaStream_t s) {
     case 16: return launch_split<T, Q8, 16>(M, N, K, p.s, g, s);
     case 32: return launch_split<T, Q8, 32>(M, N, K, p.s, g, s);
     case 64: return launch_split<T, Q8, 64>(M, N, K, p.s, g, s);
-    case 128: return launch_split<T, Q8, 128>(M, N, K, p.s, g, s);
     default: return launch_pair<T, Q8>(M, N, K, sms, g, s);
   }
 }
