@@ -137,6 +137,16 @@ void* stream(PyObject* o) {
   return reinterpret_cast<void*>(integer(o));
 }
 
+// An operator without the interpreter's lock: its launch may have to wait for room in the
+// stream's queue, and other threads go on meanwhile.
+template <class F, class... A> featfix_status run(F op, A... args) {
+  struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+  } unlocked;
+  return op(args...);
+}
+
 // The call, its status and every refusal as a Python exception.
 template <class F> PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
   if (n != want) {
@@ -171,7 +181,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Mat x = mat(a[1], "x", dt, d.rows, d.cols), r = mat(a[4], "resid", dt, d.rows, d.cols);
     const Mat s = mat(a[5], "sum_out", dt, d.rows, d.cols), o = mat(a[6], "out", dt, d.rows, d.cols);
     const Eight e = eight(a[7], a[8], d.rows, d.cols, 1);
-    return featfix_op_rms_norm(dt, d.rows, size32(d.cols, "C"), x.p, x.ld, r.p, r.ld, s.p, s.ld,
+    return run(featfix_op_rms_norm, dt, d.rows, size32(d.cols, "C"), x.p, x.ld, r.p, r.ld, s.p, s.ld,
                                vec(a[2], "weight", dt, d.cols), (float)real(a[3]), o.p, o.ld, e.q.p, e.q.ld,
                                (float*)e.scale.p, e.scale.ld, stream(a[9]));
   });
@@ -183,7 +193,7 @@ PyObject* quant8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Dims d = dims(a[1], "x");
     const Mat x = mat(a[1], "x", dt, d.rows, d.cols);
     const Eight e = eight(a[2], a[3], d.rows, d.cols, tile);
-    return featfix_op_quant8(dt, tile, d.rows, size32(d.cols, "cols"), x.p, x.ld, e.q.p, e.q.ld, (float*)e.scale.p,
+    return run(featfix_op_quant8, dt, tile, d.rows, size32(d.cols, "cols"), x.p, x.ld, e.q.p, e.q.ld, (float*)e.scale.p,
                              e.scale.ld, stream(a[5]));
   });
 }
@@ -196,7 +206,7 @@ PyObject* gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Eight x = eight(a[1], a[2], M, K, 1), w = eight(a[3], a[4], N, K, 128), q = eight(a[11], a[12], M, N, 1);
     const Mat o = mat(a[5], "out", dt, M, N), r = mat(a[10], "resid", dt, M, N);
     const Mat gate = mat(a[8], "gate", F32, rpb > 0 ? (M + rpb - 1) / rpb : M, N);
-    return featfix_op_gemm8(dt, size32(M, "M"), size32(N, "N"), size32(K, "K"), x.q.p, x.q.ld, (float*)x.scale.p, x.scale.ld,
+    return run(featfix_op_gemm8, dt, size32(M, "M"), size32(N, "N"), size32(K, "K"), x.q.p, x.q.ld, (float*)x.scale.p, x.scale.ld,
                             w.q.p, w.q.ld, (float*)w.scale.p, w.scale.ld, vec(a[6], "bias", dt, N), int32(a[7], "act"),
                             (float*)gate.p, gate.ld, rpb, r.p, r.ld, o.p, o.ld, q.q.p, q.q.ld, (float*)q.scale.p,
                             q.scale.ld, stream(a[13]));
@@ -234,7 +244,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
       s[i] = {mat(a[4 + 2 * i], names[i][0], dt, rows, width), mat(a[5 + 2 * i], names[i][1], dt, rows, width),
               size32(width / hd, "heads")};
     }
-    return featfix_op_rope(dt, rows, hd, (int)na, axes, (const int*)pos.p, pos.ld, real(a[8]), (unsigned)int32(a[9], "flags"),
+    return run(featfix_op_rope, dt, rows, hd, (int)na, axes, (const int*)pos.p, pos.ld, real(a[8]), (unsigned)int32(a[9], "flags"),
                            s[0].x.p, s[0].x.ld, s[0].heads, vec(a[10], "q_weight", dt, hd), s[0].out.p, s[0].out.ld, s[1].x.p,
                            s[1].x.ld, s[1].heads, vec(a[11], "k_weight", dt, hd), s[1].out.p, s[1].out.ld,
                            (float)real(a[12]), stream(a[13]));

@@ -2,6 +2,7 @@
 
 import ctypes
 import threading
+import time
 
 import pytest
 import torch
@@ -41,3 +42,33 @@ def test_wide_norms_of_two_threads(cuda):
     for x, o, C in zip(xs, outs, widths):
         y = rms(x.double(), None, 1e-6)
         check(o, y, "f32", y.abs() * ((C + 8) * 2.0 ** -25 + 2.0 ** -21))
+
+
+def test_a_full_launch_queue_leaves_python_to_other_threads(cuda):
+    """A launch that waits for room in its stream's queue must not hold the interpreter:
+    while one thread launches behind a kernel of a second, this one goes on."""
+    x = randn((4, 256), 40)
+    q, s = torch.empty((4, 256), dtype=torch.uint8, device=cuda), torch.empty((2, 4), device=cuda)
+    stream, done = torch.cuda.Stream(), threading.Event()
+    ff.featfix_op_quant8("f32", x, q, s)
+    torch.cuda.synchronize()
+
+    def work():
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(2_000_000_000)          # about a second
+            for _ in range(6000):
+                ff.featfix_op_quant8("f32", x, q, s)
+        done.set()
+
+    t = threading.Thread(target=work)
+    t.start()
+    gap, last, began = 0.0, time.monotonic(), time.monotonic()
+    while not done.is_set() and time.monotonic() - began < 20:
+        time.sleep(0.002)
+        now = time.monotonic()
+        gap, last = max(gap, now - last), now
+    t.join()
+    took = time.monotonic() - began
+    torch.cuda.synchronize()
+    assert took > 0.5, took                            # the queue was full: its thread had to wait
+    assert gap < 0.25, gap
