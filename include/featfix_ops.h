@@ -178,6 +178,13 @@ FEATFIX_API featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, cons
  * incomplete), FEATFIX_OK otherwise.  Not for use while a stream is captured.   */
 FEATFIX_API featfix_status featfix_op_gemm8_watchdog(void);
 
+/* Failure-detection test hook.  Lets the two bounded waits of featfix_op_gemm8's kernels
+ * run out on the current device, on barriers that nothing arrives on, after a 32nd of
+ * their limits (0.13 s): they raise the flag that featfix_op_gemm8_watchdog reports, the
+ * kernel returns, nothing traps.  limit_ns[2] (host, nullable) receives the limits, 32
+ * times what the waits took.  Uses the default stream and waits for it.        */
+FEATFIX_API featfix_status featfix_op_gemm8_watchdog_probe(unsigned long long* limit_ns);
+
 /* Rotary positions on the heads of q [rows, q_heads * head_dim] and k [rows,
  * k_heads * head_dim] (shared key heads: k_heads below q_heads; either may be
  * absent with 0 heads).  axis_dims (host, n_axes even numbers, n_axes <= 8) are the

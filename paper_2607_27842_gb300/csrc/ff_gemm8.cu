@@ -33,14 +33,15 @@ constexpr int BK = 128;   // one scale block, one 128-byte swizzled row of a sta
 // Bounded wait: polls, and looks at the clock and the abort flag once in 256 polls
 // only (reading the global timer takes long).  Written out at each use: a call would
 // spill the epilogue's sums.
-__device__ __forceinline__ bool wait_poll(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool wait_poll(uint64_t* b, uint32_t parity, volatile int* abort_flag,
+                                          unsigned long long limit_ns = WAIT_LIMIT_NS) {
   unsigned long long t0 = 0;
 #pragma unroll 1
   for (uint32_t i = 1;; ++i) {
     if (mbar_test(b, parity)) return true;
     if ((i & 255) == 0) {
       if (i == 256) t0 = gtimer();
-      if (*abort_flag || gtimer() - t0 > WAIT_LIMIT_NS) {
+      if (*abort_flag || gtimer() - t0 > limit_ns) {
         *abort_flag = 1;
         atomicOr(&g_watchdog8, 1u);
         return false;
@@ -55,17 +56,20 @@ __device__ __forceinline__ bool wait_warp(uint64_t* b, uint32_t parity, volatile
 // The hand-overs of TMEM, on which every block of K waits twice: try_wait suspends the
 // warp between looks, so its polls are not in the way of the other warps', and the loop
 // is as short as it gets, for the code around it competes for the instruction cache.
-// 40000 looks of at most 0.1 ms are the same 4 s.  (8192 x 8192 x 8192: 520 us with the
-// polls above, 494 with this.)
+// A look that finds nothing lasts 4 us here (200 in a row 0.80 ms), however long it may be
+// suspended for, so a million are the same 4 s; the watchdog's probe measures it.  (8192 x
+// 8192 x 8192: 520 us with the polls above, 494 with this.)
+constexpr int WAIT_LOOKS = 1000000;
+template <int LOOKS = WAIT_LOOKS>
 __device__ __forceinline__ bool wait_try(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
   uint32_t n;
   asm volatile(
-      "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, 40000;\n"
+      "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, %4;\n"
       "LOOP_%=:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n @p bra DONE_%=;\n"
       " sub.u32 n, n, 1;\n setp.ne.u32 q, n, 0;\n @q bra LOOP_%=;\n"
       "DONE_%=:\n mov.u32 %0, n;\n}\n"
       : "=r"(n)
-      : "r"(saddr(b)), "r"(parity), "r"(100000u)
+      : "r"(saddr(b)), "r"(parity), "r"(100000u), "n"(LOOKS)
       : "memory");
   if (!__any_sync(0xffffffffu, n == 0)) return true;
   *abort_flag = 1;
@@ -949,6 +953,28 @@ __global__ void __launch_bounds__(S_THREADS, 2)
   }
 }
 
+// Both waits, on barriers that nothing arrives on, with a part of their limits: what they
+// took, in ns.
+constexpr int PROBE_PART = 32;
+__device__ unsigned long long g_probe_ns[2];
+__global__ void __launch_bounds__(64) k_gemm8_probe() {
+  __shared__ uint64_t bar[2];
+  __shared__ int abort_flag[2];
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bar[i], 1);
+      abort_flag[i] = 0;
+    }
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5;
+  const unsigned long long t0 = gtimer();
+  if (warp == 0) wait_poll(&bar[0], 0, &abort_flag[0], WAIT_LIMIT_NS / PROBE_PART);
+  else wait_try<WAIT_LOOKS / PROBE_PART>(&bar[1], 0, &abort_flag[1]);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) g_probe_ns[warp] = gtimer() - t0;
+}
+
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
@@ -1126,6 +1152,14 @@ cudaError_t gemm8_watchdog_take(unsigned int* flags) {
   cudaError_t e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpyFromSymbol(flags, g_watchdog8, sizeof(*flags));
   if (e == cudaSuccess && *flags) e = cudaMemcpyToSymbol(g_watchdog8, &zero, sizeof(zero));
+  return e;
+}
+
+cudaError_t gemm8_watchdog_probe(unsigned long long (&limit_ns)[2]) {
+  k_gemm8_probe<<<1, 64>>>();
+  cudaError_t e = launched();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(limit_ns, g_probe_ns, sizeof(limit_ns));
+  for (unsigned long long& t : limit_ns) t *= PROBE_PART;
   return e;
 }
 

@@ -187,6 +187,14 @@ featfix_status featfix_op_gemm8_watchdog(void) {
   return gemm8_watchdog_take(&flags) == cudaSuccess && !flags ? FEATFIX_OK : FEATFIX_ERR_CUDA;
 }
 
+featfix_status featfix_op_gemm8_watchdog_probe(unsigned long long* limit_ns) {
+  unsigned long long t[2] = {0, 0};
+  const cudaError_t e = gemm8_watchdog_probe(t);
+  if (limit_ns)
+    for (int i = 0; i < 2; ++i) limit_ns[i] = t[i];
+  return st(e);
+}
+
 featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_axes, const int* axis_dims,
                                const int* dev_pos, long long ld_pos, double theta, unsigned flags, const void* dev_q,
                                long long ld_q, int q_heads, const void* dev_q_weight, void* dev_q_out,

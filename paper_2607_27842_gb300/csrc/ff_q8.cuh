@@ -63,6 +63,8 @@ struct Gemm8Args {
 cudaError_t gemm8(DType dt, int M, int N, int K, const Gemm8Args& g, cudaStream_t s);
 // The watchdog flags of gemm8's kernels, cleared; waits for the device.
 cudaError_t gemm8_watchdog_take(unsigned int* flags);
+// Lets a part of both bounded waits run out; their limits, from what it took.
+cudaError_t gemm8_watchdog_probe(unsigned long long (&limit_ns)[2]);
 
 // Magnitudes compare as their bits do; a NaN is above infinity, so a block's
 // maximum carries both on into its scale (fmaxf would drop the NaN).

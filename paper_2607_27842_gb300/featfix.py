@@ -100,6 +100,7 @@ SIGNATURES = {
     "featfix_op_gemm8": (_I, [_I, _I, _I, _I, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _LL, _VP, _I, _VP, _LL, _I, _VP, _LL,
                               _VP, _LL, _VP, _LL, _VP, _LL, _VP]),
     "featfix_op_gemm8_watchdog": (_I, []),
+    "featfix_op_gemm8_watchdog_probe": (_I, [_P(ctypes.c_ulonglong)]),
     "featfix_op_rope": (_I, [_I, _LL, _I, _I, _P(_I), _VP, _LL, _D, ctypes.c_uint, _VP, _LL, _I, _VP, _VP, _LL, _VP,
                              _LL, _I, _VP, _VP, _LL, ctypes.c_float, _VP]),
 }
@@ -495,6 +496,14 @@ def featfix_op_gemm8(dtype, a, a_scale, w, w_scale, out=None, bias=None, act=0, 
 def featfix_op_gemm8_watchdog():
     """Waits for the device; raises if a wait inside a gemm8 kernel gave up."""
     _check(lib().featfix_op_gemm8_watchdog())
+
+
+def featfix_op_gemm8_watchdog_probe():
+    """Lets both bounded waits of the gemm8 kernels run out after a 32nd of their limits;
+    returns the limits in seconds."""
+    limits = (ctypes.c_ulonglong * 2)()
+    _check(lib().featfix_op_gemm8_watchdog_probe(limits))
+    return tuple(v * 1e-9 for v in limits)
 
 
 def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None, k_out=None, theta=10000.0, halves=False,
