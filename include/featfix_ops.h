@@ -122,7 +122,8 @@ FEATFIX_API featfix_status featfix_op_attention(int dtype, const void* dev_qkv, 
  * 8-bit tensors are e4m3 bytes (largest value 448), row-major with a row stride
  * ld of at least the width and a multiple of 16.  A block's scale is
  *   s = max(largest |x| of the block / 448, 2^-100),   q = e4m3(x / s)
- * rounded to nearest even; a block stands for q * s.  A NaN in a block makes its
+ * rounded to nearest even (both within a few 2^-24: a quotient that near a tie may take
+ * either code); a block stands for q * s.  A NaN in a block makes its
  * scale NaN, an infinity makes it infinite: what is computed from the block is
  * NaN, never a finite number.  Activations have one scale per row and 128
  * columns, stored block by block: the scale of row r and column c is
@@ -141,7 +142,8 @@ FEATFIX_API featfix_status featfix_op_attention(int dtype, const void* dev_qkv, 
  * addition in front of it:
  *   h = x + resid   (x alone where dev_resid is NULL),
  *   y = h / sqrt(mean(h^2) + eps) * weight   (weight 1 where dev_weight is NULL).
- * h is kept in fp32 for the norm; dev_sum (NULL: not wanted) receives it rounded
+ * h and its sum of squares are kept in fp32 (rows whose sum passes fp32's range, |h| of
+ * about 1e19, have y = 0); dev_sum (NULL: not wanted) receives it rounded
  * to dtype and may be dev_x or dev_resid.  Exactly one of dev_out (y in dtype)
  * and dev_q (y in 8 bits, with dev_scale) is given.                          */
 FEATFIX_API featfix_status featfix_op_rms_norm(int dtype, long long rows, int C, const void* dev_x, long long ld_x,
@@ -175,7 +177,8 @@ FEATFIX_API featfix_status featfix_op_gemm8(int dtype, int M, int N, int K, cons
 
 /* Waits for the current device and returns FEATFIX_ERR_CUDA if a bounded wait inside a
  * featfix_op_gemm8 kernel gave up since the last call (its results are then
- * incomplete), FEATFIX_OK otherwise.  Not for use while a stream is captured.   */
+ * incomplete), FEATFIX_OK otherwise.  Nothing else reports it: a program asks at its own
+ * checkpoints.  Not for use while a stream is captured.                        */
 FEATFIX_API featfix_status featfix_op_gemm8_watchdog(void);
 
 /* Failure-detection test hook.  Lets the two bounded waits of featfix_op_gemm8's kernels
@@ -192,8 +195,9 @@ FEATFIX_API featfix_status featfix_op_gemm8_watchdog_probe(unsigned long long* l
  * head_dim, the columns past it are only copied.  Pair p, the i-th of axis a, of
  * row r turns by
  *   pos[a * ld_pos + r] * theta^(-2 i / axis_dims[a]),
- * or theta^(-2 p / rot) with FEATFIX_ROPE_ONE_LADDER; the angle is within fp32
- * rounding of a turn up to positions of 2^20, and within 3e-5 at any int32.  Pairs are columns (2p, 2p + 1), or (p, p + rot / 2) with
+ * or theta^(-2 p / rot) with FEATFIX_ROPE_ONE_LADDER; with theta >= 1 the angle is
+ * within fp32 rounding of a turn up to positions of 2^20, and within 3e-5 at any
+ * int32.  Pairs are columns (2p, 2p + 1), or (p, p + rot / 2) with
  * FEATFIX_ROPE_HALVES.  FEATFIX_ROPE_INVERSE turns the other way: the inverse and
  * so the gradient of the rotation.  q_weight / k_weight ([head_dim] in dtype,
  * nullable) put the root-mean-square norm of each head, times the weight, in front

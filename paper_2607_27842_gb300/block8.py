@@ -10,8 +10,9 @@ built from the operators of include/featfix_ops.h as a program uses them:
     h      = GELU(a W1^T + b) in 8 bits                  featfix_op_gemm8
     x      = x + h W2^T + b                              featfix_op_gemm8
 
-It is the kind of block that text encoders and token refiners beside the
-denoiser are made of (the denoiser's own adaLN blocks run inside the library).
+A plain block: full attention over each sample's rows, as many key heads as query
+heads, a GELU MLP; nothing causal, no key cache, no gated activation.  (The
+denoiser's own adaLN blocks run inside the library, in bf16 or fp32.)
 Rows lie as featfix_token_row has them: the text rows of all samples, then
 their image rows.  Every call is asynchronous on the current stream; nothing is
 allocated after construction.

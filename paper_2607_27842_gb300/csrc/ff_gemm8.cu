@@ -158,9 +158,9 @@ __device__ __forceinline__ void gelu4(f32x2& a, f32x2& b) {
 // (80 bytes: 8192 x 8192 x 8192 447 -> 718 us).
 // Bound by the hand-over of the two TMEM buffers: a block of K takes about 820 clocks,
 // 512 of them products; then by a tile's results, during which the products stand
-// still but for two blocks.  Measured: 8192 x 8192 x 8192 430-447 us (2.5 PFLOP/s), 14310 x
-// 2048 x 8192 with gate and residual 205-212 us (2.3), 14310 x 8192 x 2048 with GELU and
-// 8-bit output 245 us (1.96).
+// still but for two blocks.  Measured: 8192 x 8192 x 8192 430-460 us (2.4-2.6 PFLOP/s, at
+// the power cap), 14310 x 2048 x 8192 with gate and residual 205-213 us (2.3), 14310 x
+// 8192 x 2048 with GELU and 8-bit output 245-250 us (1.9).
 // ---------------------------------------------------------------------------
 constexpr int P_THREADS = 384;
 constexpr int P_STAGES = 4;
@@ -678,7 +678,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
 //   warp 0 TMA producer, warp 1 MMA issuer, warps 2-9 epilogue: TMEM lane quarter
 //   warp % 4, half of the BT columns (warp - 2) / 4
 // Bound by latencies in a row with few blocks of K (start, first copies, the cluster's
-// meeting: 1 x 6144 x 2048 5.8 us, 1 x 2048 x 8192 6.6) and by the tiles' traffic from L2
+// meeting: 1 x 6144 x 2048 5.6 us, 1 x 2048 x 8192 6.8) and by the tiles' traffic from L2
 // with many CTAs (256 x 2048 x 8192 16.6 us with a bias, 18.3 with gate and residual, 100
 // MB of tiles).
 // ---------------------------------------------------------------------------

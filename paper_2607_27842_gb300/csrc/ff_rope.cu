@@ -1,6 +1,6 @@
 // Rotary positions with several axes on q and k, with the root-mean-square norm of
 // each head in front of them where its weight is given (formula: featfix_op_rope).
-// Bound by memory without the norm (14566 rows of 16 + 16 heads of 128, bf16: 38.7 us, 6.2
+// Bound by memory without the norm (14566 rows of 16 + 16 heads of 128, bf16: 39.2 us, 6.1
 // TB/s), by shuffles and issue with it (44.6 us, 5.4 TB/s): q and k are read and written
 // once; a row's sines and cosines are formed once for all of its heads.
 #include "ff_common.cuh"

@@ -74,8 +74,8 @@ __device__ __forceinline__ float amax4(const f32x2 (&v)[2]) {
 // are all in the row or none is.  Bound by instruction issue before it was by memory:
 // hence the adjacent blocks (one address, constant offsets), packed pairs and
 // approximate reciprocals (14566 x 2048 with residual and 8-bit output 45 us without
-// them).  Measured there: 34.4 us (6.1 TB/s), bf16 output 35.5 (6.7), the quantiser alone
-// 16.3 (5.5, part of it from L2); rows of 1001 (single elements) 25.6 us (4.0).
+// them).  Measured there: 34.8 us (6.0 TB/s), bf16 output 35.5 (6.7), the quantiser alone
+// 16.6 (5.4, part of it from L2); rows of 1001 (single elements) 26.0 us (3.9).
 template <class T, int NB, bool VEC, bool NORM, bool Q8>
 __global__ void __launch_bounds__(256) k_rows8(long long rows, int C, int W, const __grid_constant__ RmsArgs a) {
   __shared__ float red[8];
@@ -170,7 +170,8 @@ __global__ void __launch_bounds__(256) k_rows8(long long rows, int C, int W, con
 }
 
 // Norm of rows too wide for registers: one block to a row, the fp32 row in shared
-// memory.
+// memory, element by element (2048 x 20480 bf16 with residual and 8-bit output 123 us, 2.4
+// TB/s; the kernel above takes 43 for 16384 columns).
 template <class T>
 __global__ void __launch_bounds__(1024) k_rows8_wide(int C, const __grid_constant__ RmsArgs a) {
   extern __shared__ float row[];
