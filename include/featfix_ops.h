@@ -213,6 +213,104 @@ FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_d
                                const void* dev_k_weight, void* dev_k_out, long long ld_k_out, float eps,
                                void* stream);
 
+/* ---------------------------------------------------------------------------
+ * An 8-bit cache of keys and values in pages, and the attention of one new token
+ * of each sequence over it.  A program that makes tokens one after another, or a
+ * clip piece by piece, keeps what later tokens attend to in it.  (The paper has no
+ * counterpart.)
+ *
+ * A place of the cache holds a head of one token: head_dim e4m3 values and one
+ * scale, by the rule above with the head as the block:
+ *   s = max(largest |x| of the head / 448, 2^-100),   q = e4m3(x / s).
+ * Scales that are NaN or infinite stand for NaN in all of the head.
+ *
+ * k, v are e4m3 bytes; place (page, slot, head) starts stride[0] * page +
+ * stride[1] * slot + stride[2] * head bytes behind the pointer (multiples of 16, at
+ * least head_dim; pointers are 16-byte aligned), its scale that many floats behind
+ * k_scale / v_scale (at least 1): heads inside or outside of a page's tokens, with or
+ * without gaps.  head_dim is a multiple of 8, at most 256.
+ *
+ * Token t of sequence b is in page table[b * ld_table + t / page_size] (t <
+ * table_pages * page_size), slot t % page_size, for t < lens[b]; lens count the
+ * tokens of a call that writes them too.  table and lens are read on the device: a
+ * graph that was captured once follows them.  Lengths below 0 count as 0, past the
+ * table's end as its end.  A page outside of 0 .. pages - 1 is none: nothing is
+ * written to it, its tokens read as zeros and are masked in the attention.  Table
+ * places behind a sequence's last token are never looked at, nor are places of the cache.
+ * Sequences may share pages that are only read; a page that a call writes to has one
+ * place in the table.                                                         */
+typedef struct featfix_kv_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  long long k_stride[3], v_stride[3];               /* page, slot, head; bytes  */
+  long long k_scale_stride[3], v_scale_stride[3];   /* page, slot, head; floats */
+  int pages, page_size, heads, head_dim;
+  const int* table;       /* device, [seqs, table_pages], row stride ld_table   */
+  long long ld_table;
+  int table_pages, seqs;
+  const int* lens;        /* device, [seqs]                                     */
+} featfix_kv_cache;
+
+/* New tokens into the cache: row dev_row_start[b] + i of k and v [rows, heads *
+ * head_dim] becomes token lens[b] - n_b + i of sequence b, n_b = dev_row_start[b + 1] -
+ * dev_row_start[b] (device, seqs + 1 rising numbers; NULL: one row to a sequence, rows =
+ * seqs).  Rows of no sequence and tokens before the first are skipped.          */
+FEATFIX_API featfix_status featfix_op_kv_write(int dtype, const featfix_kv_cache* cache, long long rows,
+                                   const int* dev_row_start, const void* dev_k, long long ld_k, const void* dev_v,
+                                   long long ld_v, void* stream);
+
+/* The same tokens back, in dtype: the inverse of featfix_op_kv_write.  Tokens before the
+ * first are zeros; rows of no sequence are left as they are.                   */
+FEATFIX_API featfix_status featfix_op_kv_read(int dtype, const featfix_kv_cache* cache, long long rows,
+                                  const int* dev_row_start, void* dev_k, long long ld_k, void* dev_v, long long ld_v,
+                                  void* stream);
+
+/* Scratch bytes that featfix_op_kv_attention needs for caches of up to `tokens` tokens to
+ * a sequence (table_pages * page_size), on any GPU; 0 where it needs none.      */
+FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int k_heads, int head_dim,
+                                         long long tokens);
+
+/* One new token of each sequence over its cached tokens (itself among them, where it
+ * has been written): with t from max(0, lens[b] - window) (window 0: from 0) to lens[b] - 1
+ * and h = j / (q_heads / heads),
+ *   x_t = scale * q[b, j] . k_t[h],   out[b, j] = sum_t exp(x_t) v_t[h] / sum_t exp(x_t),
+ *   lse[b, j] = log sum_t exp(x_t)
+ * for the heads j of q [seqs, q_heads * head_dim], q_heads a multiple of the cache's heads;
+ * out as q (and may be q), dev_lse [seqs, q_heads] nullable.  A row without tokens has
+ * out 0 and lse -infinity.  fp32 sums and statistics; q as two fp16 terms with a power of two
+ * apart where dtype is f32 and as one where it is bf16, probabilities the same: relative
+ * errors of 2^-22 and 2^-11, below dtype's own rounding.  The workspace (16-byte aligned) may
+ * hold anything; calls that may run at the same time need one each.  The same inputs
+ * give the same bits.                                                         */
+FEATFIX_API featfix_status featfix_op_kv_attention(int dtype, const featfix_kv_cache* cache, const void* dev_q,
+                                       long long ld_q, int q_heads, float scale, int window, void* dev_out,
+                                       long long ld_out, float* dev_lse, void* dev_workspace, size_t ws_bytes,
+                                       void* stream);
+
+/* The norms at the end of a block and at the beginning of the next one, with the gate and the
+ * residual between them, on rows of C columns (C <= 16384), sample s = row / rows_per_batch:
+ *   h = resid_scale * x + gate[s] * y'      (x absent: gate[s] * y'),
+ *   y' = norm(y) * weight_after with FEATFIX_NORM_AFTER, y without;
+ *   z = norm(h) * weight * (1 + scale[s]) + shift[s],
+ *   norm(u) = u / sqrt(mean(u^2) + eps), of u - mean(u) with FEATFIX_NORM_CENTERED.
+ * Weights [C] in dtype (NULL: 1), gate, scale (NULL: 1 and 0) and shift (NULL: 0) float rows
+ * of their strides.  h and all statistics stay in fp32; dev_sum (nullable) receives h
+ * rounded to dtype, dev_out z, or dev_q and dev_q_scale z in 8 bits (scales as activations
+ * have them); not both, and at least one of dev_sum, dev_out and dev_q is given.  Outputs may be
+ * x or y where they have one row stride.                                        */
+#define FEATFIX_NORM_AFTER 1u
+#define FEATFIX_NORM_CENTERED 2u
+FEATFIX_API featfix_status featfix_op_block_norms(int dtype, long long rows, int C, unsigned flags, float eps,
+                                      const void* dev_y, long long ld_y, const void* dev_weight_after,
+                                      const float* dev_gate, long long gate_stride, const void* dev_x, long long ld_x,
+                                      float resid_scale, void* dev_sum, long long ld_sum, const void* dev_weight,
+                                      const float* dev_scale, long long scale_stride, const float* dev_shift,
+                                      long long shift_stride, int rows_per_batch, void* dev_out, long long ld_out,
+                                      void* dev_q, long long ld_q, float* dev_q_scale, long long ld_q_scale,
+                                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

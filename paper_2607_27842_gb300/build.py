@@ -28,7 +28,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 SOURCES = ["ff_elementwise.cu", "ff_simt.cu", "ff_gemm_tc.cu", "ff_attention.cu", "ff_attention_tc.cu", "ff_runtime.cu", "ff_ops.cu", "ff_noalloc.cu",
-           "ff_rows8.cu", "ff_rope.cu", "ff_gemm8.cu"]
+           "ff_rows8.cu", "ff_rope.cu", "ff_gemm8.cu", "ff_kv8.cu", "ff_kv_attention.cu", "ff_block_norms.cu"]
 
 
 # the Python module that marshals the 8-bit operators' arguments (C++ only)

@@ -1,6 +1,7 @@
 // C ABI of include/featfix_ops.h: the hot-path kernels on caller buffers.
 #include "featfix_ops.h"
 #include "ff_common.cuh"
+#include "ff_kv8.cuh"
 #include "ff_q8.cuh"
 
 #include <math.h>
@@ -31,6 +32,38 @@ featfix_status st(cudaError_t e) {
   if (e == cudaErrorInvalidValue) return FEATFIX_ERR_INVALID_ARG;
   if (e == cudaErrorNotSupported) return FEATFIX_ERR_UNSUPPORTED;
   return FEATFIX_ERR_CUDA;
+}
+
+// Largest page: a sequence's tokens then stay below 2^62.
+constexpr int PAGE_MAX = 1 << 24;
+// Places at least `width` (in units of `unit`) apart along each dimension that has more than one.
+bool strides_ok(const featfix_kv_cache& c, const long long (&st)[3], long long width, int unit) {
+  const int n[3] = {c.pages, c.page_size, c.heads};
+  for (int i = 0; i < 3; ++i)
+    if (n[i] > 1 && (st[i] < width || st[i] % unit || st[i] > (1ll << 46) / n[i])) return false;
+  return true;
+}
+bool cache_ok(const featfix_kv_cache* c) {
+  if (!c || c->pages <= 0 || c->page_size <= 0 || c->page_size > PAGE_MAX || c->heads <= 0 || c->heads > 65535 ||
+      c->head_dim <= 0 || c->head_dim % 8 || c->head_dim > KV_DIM_MAX || c->table_pages <= 0 || c->seqs < 0)
+    return false;
+  if (c->seqs == 0) return true;
+  if (!c->k || !c->v || !al16(c->k) || !al16(c->v) || !c->k_scale || !c->v_scale || ((uintptr_t)c->k_scale & 3) ||
+      ((uintptr_t)c->v_scale & 3) || !c->table || !c->lens || ((uintptr_t)c->table & 3) || ((uintptr_t)c->lens & 3) ||
+      (c->seqs > 1 && c->ld_table < c->table_pages))
+    return false;
+  return strides_ok(*c, c->k_stride, c->head_dim, 16) && strides_ok(*c, c->v_stride, c->head_dim, 16) &&
+         strides_ok(*c, c->k_scale_stride, 1, 1) && strides_ok(*c, c->v_scale_stride, 1, 1);
+}
+featfix_status kv_rows(int dtype, const featfix_kv_cache* cache, const KvRows& r,
+                       cudaError_t (*launch)(DType, const KvCache&, const KvRows&, cudaStream_t), void* stream) {
+  if (!dt_ok(dtype) || !cache_ok(cache) || r.rows < 0 || r.rows > DIM_MAX) return FEATFIX_ERR_INVALID_ARG;
+  if (!r.row_start && r.rows != cache->seqs) return FEATFIX_ERR_INVALID_ARG;
+  if (r.rows == 0 || cache->seqs == 0) return FEATFIX_OK;
+  const long long width = (long long)cache->heads * cache->head_dim;
+  if (!r.k || !r.v || r.ldk < width || r.ldv < width || !el_al(dtype, {r.k, r.v}) || ((uintptr_t)r.row_start & 3))
+    return FEATFIX_ERR_INVALID_ARG;
+  return st(launch((DType)dtype, *cache, r, (cudaStream_t)stream));
 }
 
 }  // namespace
@@ -246,6 +279,73 @@ featfix_status featfix_op_rope(int dtype, long long rows, int head_dim, int n_ax
     }
   }
   return st(launch_rope((DType)dtype, rows, r, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_kv_write(int dtype, const featfix_kv_cache* cache, long long rows, const int* dev_row_start,
+                                   const void* dev_k, long long ld_k, const void* dev_v, long long ld_v, void* stream) {
+  // (k and v are only read)
+  return kv_rows(dtype, cache, {rows, dev_row_start, const_cast<void*>(dev_k), ld_k, const_cast<void*>(dev_v), ld_v},
+                 launch_kv_write, stream);
+}
+
+featfix_status featfix_op_kv_read(int dtype, const featfix_kv_cache* cache, long long rows, const int* dev_row_start,
+                                  void* dev_k, long long ld_k, void* dev_v, long long ld_v, void* stream) {
+  return kv_rows(dtype, cache, {rows, dev_row_start, dev_k, ld_k, dev_v, ld_v}, launch_kv_read, stream);
+}
+
+size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int k_heads, int head_dim, long long tokens) {
+  if (seqs <= 0 || q_heads <= 0 || k_heads <= 0 || q_heads % k_heads || head_dim <= 0 || head_dim > KV_DIM_MAX || tokens <= 0)
+    return 0;
+  return kv_attention_workspace(seqs, q_heads, k_heads, head_dim, tokens);
+}
+
+featfix_status featfix_op_kv_attention(int dtype, const featfix_kv_cache* cache, const void* dev_q, long long ld_q,
+                                       int q_heads, float scale, int window, void* dev_out, long long ld_out,
+                                       float* dev_lse, void* dev_workspace, size_t ws_bytes, void* stream) {
+  if (!dt_ok(dtype) || !cache_ok(cache) || q_heads <= 0 || q_heads > 65535 || q_heads % cache->heads || window < 0 ||
+      !isfinite(scale))
+    return FEATFIX_ERR_INVALID_ARG;
+  if (cache->seqs == 0) return FEATFIX_OK;
+  const long long width = (long long)q_heads * cache->head_dim;
+  if (!dev_q || !dev_out || ld_q < width || ld_out < width || !el_al(dtype, {dev_q, dev_out}) || ((uintptr_t)dev_lse & 3))
+    return FEATFIX_ERR_INVALID_ARG;
+  const size_t need = kv_attention_workspace(cache->seqs, q_heads, cache->heads, cache->head_dim,
+                                             (long long)cache->table_pages * cache->page_size);
+  if (need && (!dev_workspace || ws_bytes < need || !al16(dev_workspace))) return FEATFIX_ERR_INVALID_ARG;
+  const KvAttnArgs a = {dev_q, ld_q, dev_out, ld_out, dev_lse, q_heads, scale, window, dev_workspace};
+  return st(launch_kv_attention((DType)dtype, *cache, a, (cudaStream_t)stream));
+}
+
+featfix_status featfix_op_block_norms(int dtype, long long rows, int C, unsigned flags, float eps, const void* dev_y,
+                                      long long ld_y, const void* dev_weight_after, const float* dev_gate,
+                                      long long gate_stride, const void* dev_x, long long ld_x, float resid_scale,
+                                      void* dev_sum, long long ld_sum, const void* dev_weight, const float* dev_scale,
+                                      long long scale_stride, const float* dev_shift, long long shift_stride,
+                                      int rows_per_batch, void* dev_out, long long ld_out, void* dev_q, long long ld_q,
+                                      float* dev_q_scale, long long ld_q_scale, void* stream) {
+  if (!dt_ok(dtype) || rows < 0 || rows > DIM_MAX || C <= 0 || C > BLOCK_NORMS_COLS_MAX || !(eps >= 0.f) || (flags & ~3u) ||
+      !isfinite(resid_scale))
+    return FEATFIX_ERR_INVALID_ARG;
+  if (rows == 0) return FEATFIX_OK;
+  if (!dev_y || ld_y < C || (dev_out && dev_q) || (!dev_sum && !dev_out && !dev_q) ||
+      (dev_weight_after && !(flags & FEATFIX_NORM_AFTER)))
+    return FEATFIX_ERR_INVALID_ARG;
+  if ((dev_x && ld_x < C) || (dev_sum && ld_sum < C) || (dev_out && ld_out < C)) return FEATFIX_ERR_INVALID_ARG;
+  if (!el_al(dtype, {dev_y, dev_weight_after, dev_x, dev_sum, dev_weight, dev_out}) ||
+      (((uintptr_t)dev_gate | (uintptr_t)dev_scale | (uintptr_t)dev_shift) & 3))
+    return FEATFIX_ERR_INVALID_ARG;
+  if ((dev_gate || dev_scale || dev_shift) && rows_per_batch <= 0) return FEATFIX_ERR_INVALID_ARG;
+  // (one sample has no stride)
+  const bool many = rows > rows_per_batch;
+  if (many && ((dev_gate && gate_stride < C) || (dev_scale && scale_stride < C) || (dev_shift && shift_stride < C)))
+    return FEATFIX_ERR_INVALID_ARG;
+  const Quant8Out q8 = {dev_q, ld_q, dev_q_scale, ld_q_scale};
+  if (dev_q && !q8_ok(q8, C, rows)) return FEATFIX_ERR_INVALID_ARG;
+  const BlockNormsArgs a = {dev_y, ld_y, dev_weight_after, dev_gate, gate_stride, dev_x, ld_x, resid_scale, dev_sum,
+                            ld_sum, dev_weight, dev_scale, scale_stride, dev_shift, shift_stride,
+                            rows_per_batch > 0 ? rows_per_batch : 1, (flags & FEATFIX_NORM_AFTER) != 0,
+                            (flags & FEATFIX_NORM_CENTERED) != 0, eps, dev_out, ld_out, q8};
+  return st(launch_block_norms((DType)dtype, rows, C, a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Argument marshalling of the 8-bit layer operators for Python: the checks of the
+// Argument marshalling of the 8-bit layers' and cache's operators for Python: the checks of the
 // binding and the call into libfeatfix.so, without building a Python object for each
 // size, stride and pointer.  Through ctypes a call of six tensors took 9 us of host time
 // on a Grace core; it takes 3, of which the launch is 2 (the kernels of one token take
@@ -251,6 +251,112 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The cache's values or scales: base address and the strides of page, slot and head, of
+// sizes that the first tensor of a cache sets.
+struct Pool {
+  void* p = nullptr;
+  long long stride[3] = {0, 0, 0};
+};
+Pool pool(PyObject* o, const char* name, int type, const int64_t (&size)[4]) {
+  const at::Tensor& t = tensor(o, name);
+  const int64_t dims = type == Q8 ? 4 : 3;
+  bool same = t.dim() == dims;
+  for (int64_t i = 0; same && i < dims; ++i) same = t.size(i) == size[i];
+  if (!same) {
+    std::string want;
+    for (int64_t i = 0; i < dims; ++i) want += (i ? ", " : "") + std::to_string(size[i]);
+    refuse(std::string(name) + ": expected [" + want + "]");
+  }
+  check(t, name, type);
+  if (type == Q8 && size[3] > 1 && t.stride(3) != 1) refuse(std::string(name) + ": a head's columns must be adjacent");
+  Pool p;
+  p.p = t.data_ptr();
+  for (int i = 0; i < 3; ++i) p.stride[i] = t.stride(i);
+  return p;
+}
+
+// (k8, k_scale, v8, v_scale), the page table and the lengths
+featfix_kv_cache kv_cache(PyObject* cache, PyObject* table, PyObject* lens) {
+  if (!PyTuple_Check(cache) || PyTuple_GET_SIZE(cache) != 4) refuse("cache: expected (k8, k_scale, v8, v_scale)");
+  const at::Tensor& k8 = tensor(PyTuple_GET_ITEM(cache, 0), "k8");
+  if (k8.dim() != 4) refuse("k8: expected [pages, page size, heads, head_dim]");
+  const int64_t size[4] = {k8.size(0), k8.size(1), k8.size(2), k8.size(3)};
+  static const char* names[4] = {"k8", "k_scale", "v8", "v_scale"};
+  Pool p[4];
+  for (int i = 0; i < 4; ++i) p[i] = pool(PyTuple_GET_ITEM(cache, i), names[i], i & 1 ? F32 : Q8, size);
+  featfix_kv_cache c = {};
+  c.k = p[0].p, c.k_scale = (float*)p[1].p, c.v = p[2].p, c.v_scale = (float*)p[3].p;
+  for (int i = 0; i < 3; ++i) {
+    c.k_stride[i] = p[0].stride[i], c.k_scale_stride[i] = p[1].stride[i];
+    c.v_stride[i] = p[2].stride[i], c.v_scale_stride[i] = p[3].stride[i];
+  }
+  c.pages = size32(size[0], "pages"), c.page_size = size32(size[1], "page size");
+  c.heads = size32(size[2], "heads"), c.head_dim = size32(size[3], "head_dim");
+  const Dims d = dims(table, "table");
+  const Mat t = mat(table, "table", I32, d.rows, d.cols);
+  c.table = (const int*)t.p, c.ld_table = t.ld;
+  c.seqs = size32(d.rows, "sequences"), c.table_pages = size32(d.cols, "pages of the table");
+  c.lens = (const int*)vec(lens, "lens", I32, d.rows);
+  return c;
+}
+
+template <class F> PyObject* kv_rows(PyObject* const* a, Py_ssize_t n, F op) {
+  return guarded(n, 8, [&] {   // dtype cache table lens k v row_start stream
+    const int dt = dtype(a[0]);
+    const featfix_kv_cache c = kv_cache(a[1], a[2], a[3]);
+    const int64_t rows = dims(a[4], "k").rows, width = (int64_t)c.heads * c.head_dim;
+    const Mat k = mat(a[4], "k", dt, rows, width), v = mat(a[5], "v", dt, rows, width);
+    return run(op, dt, &c, (long long)rows, (const int*)vec(a[6], "row_start", I32, c.seqs + 1ll), k.p, k.ld, v.p, v.ld,
+               stream(a[7]));
+  });
+}
+PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_rows(a, n, featfix_op_kv_write); }
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_rows(a, n, featfix_op_kv_read); }
+
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&] {   // dtype cache table lens q out workspace scale window lse stream
+    const int dt = dtype(a[0]);
+    const featfix_kv_cache c = kv_cache(a[1], a[2], a[3]);
+    const int64_t width = dims(a[4], "q").cols;
+    if (c.head_dim == 0 || width % c.head_dim) refuse("q: its columns are no whole number of heads");
+    const int heads = size32(width / c.head_dim, "heads");
+    const Mat q = mat(a[4], "q", dt, c.seqs, width), o = mat(a[5], "out", dt, c.seqs, width);
+    const Mat lse = mat(a[9], "lse", F32, c.seqs, heads);
+    if (c.seqs > 1 && lse.p && lse.ld != heads) refuse("lse: rows must be adjacent");
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (a[6] != Py_None) {
+      const at::Tensor& t = tensor(a[6], "workspace");
+      if (!t.is_contiguous()) refuse("workspace: expected adjacent elements");
+      if (!t.is_cuda()) refuse("workspace is not on the GPU");
+      g_current.ask();
+      if (t.get_device() != g_current.device) refuse("workspace is on another GPU than the current one");
+      ws = t.data_ptr();
+      bytes = t.nbytes();
+    }
+    return run(featfix_op_kv_attention, dt, &c, q.p, q.ld, heads, (float)real(a[7]), int32(a[8], "window"), o.p, o.ld,
+               (float*)lse.p, ws, bytes, stream(a[10]));
+  });
+}
+
+PyObject* block_norms(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // dtype y x eps flags weight_after resid_scale gate sum weight shift scale rows_per_batch out q q_scale stream
+  return guarded(n, 17, [&] {
+    const int dt = dtype(a[0]), rpb = int32(a[12], "rows_per_batch");
+    const Dims d = dims(a[1], "y");
+    const Mat y = mat(a[1], "y", dt, d.rows, d.cols), x = mat(a[2], "x", dt, d.rows, d.cols);
+    const Mat sum = mat(a[8], "sum_out", dt, d.rows, d.cols), o = mat(a[13], "out", dt, d.rows, d.cols);
+    const Eight e = eight(a[14], a[15], d.rows, d.cols, 1);
+    const int64_t samples = rpb > 0 ? (d.rows + rpb - 1) / rpb : d.rows;
+    const Mat gate = mat(a[7], "gate", F32, samples, d.cols), shift = mat(a[10], "shift", F32, samples, d.cols);
+    const Mat scale = mat(a[11], "scale", F32, samples, d.cols);
+    return run(featfix_op_block_norms, dt, d.rows, size32(d.cols, "C"), (unsigned)int32(a[4], "flags"), (float)real(a[3]),
+               y.p, y.ld, vec(a[5], "weight_after", dt, d.cols), (const float*)gate.p, gate.ld, x.p, x.ld, (float)real(a[6]),
+               sum.p, sum.ld, vec(a[9], "weight", dt, d.cols), (const float*)scale.p, scale.ld, (const float*)shift.p,
+               shift.ld, rpb, o.p, o.ld, e.q.p, e.q.ld, (float*)e.scale.p, e.scale.ld, stream(a[16]));
+  });
+}
+
 PyObject* set_error(PyObject*, PyObject* type) {
   Py_INCREF(type);
   Py_XDECREF(g_error);
@@ -263,6 +369,10 @@ PyMethodDef methods[] = {
     {"quant8", (PyCFunction)(void (*)())quant8, METH_FASTCALL, nullptr},
     {"gemm8", (PyCFunction)(void (*)())gemm8, METH_FASTCALL, nullptr},
     {"rope", (PyCFunction)(void (*)())rope, METH_FASTCALL, nullptr},
+    {"kv_write", (PyCFunction)(void (*)())kv_write, METH_FASTCALL, nullptr},
+    {"kv_read", (PyCFunction)(void (*)())kv_read, METH_FASTCALL, nullptr},
+    {"kv_attention", (PyCFunction)(void (*)())kv_attention, METH_FASTCALL, nullptr},
+    {"block_norms", (PyCFunction)(void (*)())block_norms, METH_FASTCALL, nullptr},
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops8", "Marshalling of the 8-bit layer operators.", -1, methods,

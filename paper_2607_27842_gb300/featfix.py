@@ -62,6 +62,15 @@ _LL = ctypes.c_longlong
 _D = ctypes.c_double
 _P = ctypes.POINTER
 
+
+class KvCache(ctypes.Structure):
+    """featfix_kv_cache of featfix_ops.h."""
+    _fields_ = [(n, _VP) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, _LL * 3) for n in ("k_stride", "v_stride", "k_scale_stride", "v_scale_stride")] + [
+        (n, _I) for n in ("pages", "page_size", "heads", "head_dim")] + [
+        ("table", _VP), ("ld_table", _LL), ("table_pages", _I), ("seqs", _I), ("lens", _VP)]
+
+
 # name -> (restype, argtypes); every symbol declared in include/*.h
 SIGNATURES = {
     "featfix_weight_count": (_I, [_P(ModelDesc)]),
@@ -103,6 +112,14 @@ SIGNATURES = {
     "featfix_op_gemm8_watchdog_probe": (_I, [_P(ctypes.c_ulonglong)]),
     "featfix_op_rope": (_I, [_I, _LL, _I, _I, _P(_I), _VP, _LL, _D, ctypes.c_uint, _VP, _LL, _I, _VP, _VP, _LL, _VP,
                              _LL, _I, _VP, _VP, _LL, ctypes.c_float, _VP]),
+    "featfix_op_kv_write": (_I, [_I, _P(KvCache), _LL, _VP, _VP, _LL, _VP, _LL, _VP]),
+    "featfix_op_kv_read": (_I, [_I, _P(KvCache), _LL, _VP, _VP, _LL, _VP, _LL, _VP]),
+    "featfix_op_kv_attention_workspace": (ctypes.c_size_t, [_I, _I, _I, _I, _LL]),
+    "featfix_op_kv_attention": (_I, [_I, _P(KvCache), _VP, _LL, _I, ctypes.c_float, _I, _VP, _LL, _VP, _VP,
+                                     ctypes.c_size_t, _VP]),
+    "featfix_op_block_norms": (_I, [_I, _LL, _I, ctypes.c_uint, ctypes.c_float, _VP, _LL, _VP, _VP, _LL, _VP, _LL,
+                                    ctypes.c_float, _VP, _LL, _VP, _VP, _LL, _VP, _LL, _I, _VP, _LL, _VP, _LL, _VP, _LL,
+                                    _VP]),
 }
 
 # argument arrays of the draft and the paid check (at most four history terms)
@@ -513,6 +530,50 @@ def featfix_op_rope(dtype, pos, axis_dims, head_dim, q=None, q_out=None, k=None,
     flags = (ROPE_HALVES if halves else 0) | (ROPE_ONE_LADDER if one_ladder else 0) | (ROPE_INVERSE if inverse else 0)
     _marshal().rope(_dt(dtype), pos, axis_dims, head_dim, q, q_out, k, k_out, theta, flags, q_weight, k_weight, eps,
                     _handle(stream))
+
+
+# ----------------------------------------------------------------------------
+# 8-bit key-value cache (featfix_ops.h).  ``cache`` is (k8, k_scale, v8, v_scale): k8, v8
+# float8_e4m3fn or uint8 [pages, page size, heads, head_dim] with places on 16 bytes,
+# k_scale, v_scale fp32 [pages, page size, heads], any strides otherwise; ``table`` int32
+# [sequences, pages], ``lens`` int32 [sequences], both on the GPU.
+# ----------------------------------------------------------------------------
+
+NORM_AFTER, NORM_CENTERED = 1, 2
+
+
+def featfix_op_kv_write(dtype, k, v, cache, table, lens, row_start=None, stream=None):
+    """Rows row_start[b] .. row_start[b + 1] - 1 of k and v [rows, heads * head_dim] become the
+    last of the lens[b] tokens of sequence b (without ``row_start``: row b the last one)."""
+    _marshal().kv_write(_dt(dtype), cache, table, lens, k, v, row_start, _handle(stream))
+
+
+def featfix_op_kv_read(dtype, cache, table, lens, k, v, row_start=None, stream=None):
+    """The same tokens back out of the cache, into k and v."""
+    _marshal().kv_read(_dt(dtype), cache, table, lens, k, v, row_start, _handle(stream))
+
+
+def featfix_op_kv_attention_workspace(seqs, q_heads, k_heads, head_dim, tokens):
+    """Scratch bytes of featfix_op_kv_attention; ``tokens``: what a sequence's row of the table
+    holds (pages * page size)."""
+    return int(lib().featfix_op_kv_attention_workspace(int(seqs), int(q_heads), int(k_heads), int(head_dim), int(tokens)))
+
+
+def featfix_op_kv_attention(dtype, q, cache, table, lens, out, workspace, scale, window=0, lse=None, stream=None):
+    """One new token of each sequence, q [sequences, heads * head_dim], over its cached tokens
+    (the last ``window`` of them, where given); log-sum-exp into ``lse`` [sequences, heads]."""
+    _marshal().kv_attention(_dt(dtype), cache, table, lens, q, out, workspace, scale, window, lse, _handle(stream))
+
+
+def featfix_op_block_norms(dtype, y, x, eps, weight_after=None, norm_after=True, resid_scale=1.0, gate=None, sum_out=None,
+                           weight=None, shift=None, scale=None, rows_per_batch=0, centered=False, out=None, q=None,
+                           q_scale=None, stream=None):
+    """h = resid_scale * x + gate * norm(y) * weight_after (y itself without ``norm_after``) into
+    ``sum_out``; norm(h) * weight * (1 + scale) + shift into ``out``, or in 8 bits into ``q`` and
+    ``q_scale`` [ceil(C / 128), rows]; gate, scale and shift fp32 [samples, C]."""
+    flags = (NORM_AFTER if norm_after else 0) | (NORM_CENTERED if centered else 0)
+    _marshal().block_norms(_dt(dtype), y, x, eps, flags, weight_after, resid_scale, gate, sum_out, weight, shift, scale,
+                           rows_per_batch, out, q, q_scale, _handle(stream))
 
 
 class FeatFix:

@@ -1,0 +1,121 @@
+"""Transformer layers in 8 bits that take one new token of each sequence at a time,
+over an 8-bit cache of the keys and values of the earlier ones, built from the
+operators of include/featfix_ops.h as a program uses them.  Per layer:
+
+    qkv    = a Wqkv^T + b                                   featfix_op_gemm8
+    q, k   = rotary positions on rms_norm(q), rms_norm(k)   featfix_op_rope
+    cache  <- k, v in 8 bits                                featfix_op_kv_write
+    o      = attention over the sequence's tokens           featfix_op_kv_attention
+    d      = o (in 8 bits) Wproj^T + b                      featfix_op_quant8, featfix_op_gemm8
+    x      = x + rms_norm(d);  a = rms_norm(x) in 8 bits    featfix_op_block_norms
+    h      = GELU(a W1^T + b) in 8 bits                     featfix_op_gemm8
+    d      = h W2^T + b                                     featfix_op_gemm8
+    x      = x + rms_norm(d);  a = the next layer's rms_norm(x)   featfix_op_block_norms
+
+with weights in all norms, and key heads that several query heads share.  Every
+call of a step is asynchronous on the current stream and allocates nothing, and the
+lengths and page tables are read on the device: a step that was captured in a graph
+once serves all later ones.
+"""
+
+import torch
+
+from . import featfix as ff
+from .block8 import quantized
+
+MATRICES = ("qkv", "proj", "fc1", "fc2")
+
+
+class KVCache8:
+    """Pages of 8-bit keys and values of ``layers`` layers, and who has which: the same
+    page table and lengths serve every layer.  ``tokens``: the longest sequence."""
+
+    def __init__(self, layers, pages, page_size, heads, dim, seqs, tokens, device="cuda"):
+        pad = (dim + 15) // 16 * 16
+        held = lambda: torch.zeros((layers, pages, page_size, heads, pad), dtype=torch.uint8, device=device)[..., :dim]
+        scales = lambda: torch.zeros((layers, pages, page_size, heads), device=device)
+        self.k8, self.v8, self.k_scale, self.v_scale = held(), held(), scales(), scales()
+        self.page_size, self.width = page_size, -(-tokens // page_size)
+        self.table = torch.full((seqs, self.width), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(seqs, dtype=torch.int32, device=device)
+        self.free = list(range(pages - 1, -1, -1))
+        self.held = [[] for _ in range(seqs)]
+        self.used = [0] * seqs
+
+    def layer(self, i):
+        return self.k8[i], self.k_scale[i], self.v8[i], self.v_scale[i]
+
+    def grow(self, counts):
+        """Makes room for counts[b] more tokens of sequence b, as the next calls write them.  Raises
+        MemoryError, and changes nothing, where the pages or a sequence's row of the table run out."""
+        used = [u + n for u, n in zip(self.used, counts)]
+        need = [-(-u // self.page_size) for u in used]
+        if max(need, default=0) > self.width or sum(n - len(h) for n, h in zip(need, self.held)) > len(self.free):
+            raise MemoryError("no pages left for %d more tokens" % sum(counts))
+        for b, n in enumerate(need):
+            first = len(self.held[b])
+            if n > first:
+                self.held[b] += [self.free.pop() for _ in range(n - first)]
+                self.table[b, first:n] = torch.tensor(self.held[b][first:], dtype=torch.int32)
+        self.used = used
+        self.lens.copy_(torch.tensor(used, dtype=torch.int32))
+
+    def drop(self, b):
+        """Sequence b is over: its pages are free again."""
+        self.free += reversed(self.held[b])
+        self.held[b], self.used[b] = [], 0
+        self.lens[b] = 0
+        self.table[b] = -1
+
+
+class Step8:
+    """Layers of one model.  ``layers``: a dict of bf16 GPU tensors for each: norm1 [C],
+    qkv.w [(heads + 2 k_heads) d, C], qkv.b, q_norm [d], k_norm [d], proj.w [C, heads d], proj.b,
+    norm1_after [C], norm2 [C], fc1.w [M, C], fc1.b, fc2.w [C, M], fc2.b, norm2_after [C]; the
+    matrices are quantised here, once."""
+
+    def __init__(self, layers, heads, k_heads, cache, theta=10000.0, eps=1e-6):
+        self.w = [{k: v for k, v in w.items() if k.removesuffix(".w") not in MATRICES} for w in layers]
+        self.q8 = [{m: quantized(w[m + ".w"]) for m in MATRICES} for w in layers]
+        self.heads, self.k_heads, self.theta, self.eps, self.cache = heads, k_heads, theta, eps, cache
+        n, (C, M) = cache.lens.numel(), layers[0]["fc2.w"].shape
+        self.dim, dev = layers[0]["q_norm"].numel(), layers[0]["norm1"].device
+        empty = lambda w: torch.empty((n, w), dtype=torch.bfloat16, device=dev)
+        self.qkv, self.o, self.d = empty((heads + 2 * k_heads) * self.dim), empty(heads * self.dim), empty(C)
+        self.pos = torch.empty((1, n), dtype=torch.int32, device=dev)
+        # 8-bit activations with their scales: of width C, of the heads, of width M
+        self.a, self.p, self.h = ((torch.zeros((n, (w + 15) // 16 * 16), dtype=torch.uint8, device=dev)[:, :w],
+                                   torch.empty(((w + 127) // 128, n), dtype=torch.float32, device=dev))
+                                  for w in (C, heads * self.dim, M))
+        bytes_ = ff.featfix_op_kv_attention_workspace(n, heads, k_heads, self.dim, cache.width * cache.page_size)
+        self.workspace = torch.empty(bytes_, dtype=torch.uint8, device=dev)
+
+    def _linear(self, i, name, x, **kw):
+        ff.featfix_op_gemm8("bf16", *x, *self.q8[i][name], bias=self.w[i][name + ".b"], **kw)
+
+    def _norms(self, x, after, before):
+        """x += norm(d) * after; the activations a = norm(x) * before, where there is a next norm."""
+        to = {} if before is None else {"q": self.a[0], "q_scale": self.a[1]}
+        ff.featfix_op_block_norms("bf16", self.d, x, self.eps, weight_after=after, sum_out=x, weight=before, **to)
+
+    def __call__(self, x):
+        """The residual stream x (bf16 [sequences, C]) of the last of each sequence's cache.lens
+        tokens (0: of none, its row means nothing) is updated in place."""
+        w, dim, c = self.w, self.dim, self.cache
+        split = [n * dim for n in (self.heads, self.k_heads, self.k_heads)]
+        q, k, v = self.qkv.split(split, 1)
+        torch.sub(c.lens, 1, out=self.pos[0])
+        ff.featfix_op_rms_norm("bf16", x, w[0]["norm1"], self.eps, q=self.a[0], q_scale=self.a[1])
+        for i, wi in enumerate(w):
+            self._linear(i, "qkv", self.a, out=self.qkv)
+            ff.featfix_op_rope("bf16", self.pos, (dim,), dim, q=q, q_out=q, k=k, k_out=k, theta=self.theta,
+                               q_weight=wi["q_norm"], k_weight=wi["k_norm"], eps=self.eps)
+            ff.featfix_op_kv_write("bf16", k, v, c.layer(i), c.table, c.lens)
+            ff.featfix_op_kv_attention("bf16", q, c.layer(i), c.table, c.lens, self.o, self.workspace, dim ** -0.5)
+            ff.featfix_op_quant8("bf16", self.o, *self.p)
+            self._linear(i, "proj", self.p, out=self.d)
+            self._norms(x, wi["norm1_after"], wi["norm2"])
+            self._linear(i, "fc1", self.a, act=1, q=self.h[0], q_scale=self.h[1])
+            self._linear(i, "fc2", self.h, out=self.d)
+            self._norms(x, wi["norm2_after"], w[i + 1]["norm1"] if i + 1 < len(w) else None)
+        return x
