@@ -231,7 +231,7 @@ FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_d
  * without gaps.  head_dim is a multiple of 8, at most 256.
  *
  * Token t of sequence b is in page table[b * ld_table + t / page_size] (t <
- * table_pages * page_size), slot t % page_size, for t < lens[b]; lens count the
+ * table_pages * page_size, at most 2^31 - 256), slot t % page_size, for t < lens[b]; lens count the
  * tokens of a call that writes them too.  table and lens are read on the device: a
  * graph that was captured once follows them.  Lengths below 0 count as 0, past the
  * table's end as its end.  A page outside of 0 .. pages - 1 is none: nothing is

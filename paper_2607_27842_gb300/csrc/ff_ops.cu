@@ -34,7 +34,6 @@ featfix_status st(cudaError_t e) {
   return FEATFIX_ERR_CUDA;
 }
 
-// Largest page: a sequence's tokens then stay below 2^62.
 constexpr int PAGE_MAX = 1 << 24;
 // Places at least `width` (in units of `unit`) apart along each dimension that has more than one.
 bool strides_ok(const featfix_kv_cache& c, const long long (&st)[3], long long width, int unit) {
@@ -45,7 +44,8 @@ bool strides_ok(const featfix_kv_cache& c, const long long (&st)[3], long long w
 }
 bool cache_ok(const featfix_kv_cache* c) {
   if (!c || c->pages <= 0 || c->page_size <= 0 || c->page_size > PAGE_MAX || c->heads <= 0 || c->heads > 65535 ||
-      c->head_dim <= 0 || c->head_dim % 8 || c->head_dim > KV_DIM_MAX || c->table_pages <= 0 || c->seqs < 0)
+      c->head_dim <= 0 || c->head_dim % 8 || c->head_dim > KV_DIM_MAX || c->table_pages <= 0 || c->seqs < 0 ||
+      (long long)c->table_pages * c->page_size > DIM_MAX)
     return false;
   if (c->seqs == 0) return true;
   if (!c->k || !c->v || !al16(c->k) || !al16(c->v) || !c->k_scale || !c->v_scale || ((uintptr_t)c->k_scale & 3) ||

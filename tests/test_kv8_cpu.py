@@ -48,7 +48,7 @@ BAD_CACHE = [
     dict(k_stride=(4096, 40, 80)), dict(k_stride=(0, 256, 80)), dict(v_stride=(-4096, 256, 80)), dict(v_stride=(1 << 60, 256, 80)),
     dict(k_scale_stride=(48, 0, 1)), dict(v_scale_stride=(48, 3, -1)), dict(pages=0), dict(pages=-1), dict(page_size=0),
     dict(page_size=(1 << 24) + 1), dict(heads=0), dict(heads=65536), dict(head_dim=0), dict(head_dim=12), dict(head_dim=-8),
-    dict(head_dim=264), dict(table_pages=0), dict(ld_table=4), dict(seqs=-1)]
+    dict(head_dim=264), dict(table_pages=0), dict(table_pages=1 << 27, ld_table=1 << 27), dict(ld_table=4), dict(seqs=-1)]
 BAD = [(n, g, dict(cache={**CACHE, **b})) for b in BAD_CACHE
        for n, g in (("featfix_op_kv_write", ROWS), ("featfix_op_kv_attention", ATTN))]
 BAD += [(n, ROWS, b) for n in ("featfix_op_kv_write", "featfix_op_kv_read") for b in (
