@@ -6,9 +6,8 @@
 // its query heads, a step T of its tokens; the units of a sequence follow one another, then
 // the next sequence's.  Every warp of the grid takes an equal stretch of the line,
 // whatever the lengths are, and goes over it on its own: tokens come by asynchronous
-// copies, one or more steps ahead, to a place that only the copying lane reads (so
-// shared memory has no layout to agree on and no bank conflicts); e4m3 becomes fp16 in
-// registers, exactly; products are mma.sync m16n8k16 with tokens or columns as the 16 and
+// copies a step or two ahead, eight lanes to 128 adjacent bytes, into a ring that only this warp
+// knows; e4m3 becomes fp16 in registers, exactly; products are mma.sync m16n8k16 with tokens or columns as the 16 and
 // query heads as the 8, because a token's few query heads would fill 4 of tcgen05's 128
 // rows, and the products are far from a bound here.
 //
@@ -33,23 +32,26 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ff {
 
 namespace {
 
-constexpr int WARPS = 8;
 constexpr int GRID_MAX = 160;      // blocks that the workspace has room for
 constexpr float NONE = -3.0e38f;   // maximum of nothing
 // longest units, in steps, of which every block takes whole ones (no second kernel)
 constexpr int WHOLE_STEPS = 32;
 
 // Shapes of a variant: columns of a head rounded up to DP, NT times 8 query heads.
-template <int DP, int NT> struct Shape {
+template <class E, int DP, int NT> struct Shape {
+  // warps of a block: 16 where their registers (128 to a thread) hold a warp's sums
+  static constexpr int WARPS = DP <= 128 && NT == 1 && sizeof(E) == 2 ? 16 : 8;
   static constexpr int MT = DP == 256 ? 1 : 2;                 // groups of 16 tokens in a step
   static constexpr int T = 16 * MT;
-  static constexpr int STAGES = DP == 64 ? 4 : 2;
+  static constexpr int STAGES = (DP == 64 ? 2 : 1) * (WARPS == 16 ? 1 : 2);
   static constexpr int NK = DP / 64;                           // 16-byte vectors of a key to a lane
+  static constexpr int ROWS = 512 / DP;                        // tokens of a copy by all lanes
   static constexpr int VB = DP >= 128 ? 16 : 8;                // bytes of a value's vector
   static constexpr int NV = DP / 8 / VB;
   static constexpr int STAGE = T * DP * 2 + T * 8 + 16;        // keys, values, scales, mask
@@ -67,6 +69,10 @@ struct Plan {
   int whole;               // blocks take whole units
   int pairs;               // results may be stored in pairs
   float scale;             // softmax scale times log2(e)
+  // strides of page and slot of keys and values in units of 2^shift bytes, by which every place's
+  // offset fits 32 bits; of their scales in floats
+  unsigned k_unit[2], v_unit[2], ks[2], vs[2];
+  unsigned k_bytes, v_bytes;   // 2^shift
 };
 
 __device__ __forceinline__ unsigned cvt_e4m3x2(unsigned short u) {
@@ -98,14 +104,31 @@ __device__ __forceinline__ unsigned half2_bits(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
 }
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void cp_async16s(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async16s(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async4s(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// Where the 16 bytes from column 16 * chunk of token `row` lie in a stage's keys or values: lines of
+// 128 bytes (half a token, a token or two) whose vectors change places from line to line, so
+// that neither products' reads (eight lanes: two tokens by four vectors for keys, four tokens
+// by two for values) have two lanes on one bank.
+template <int DP, int T> __device__ __forceinline__ int place(int row, int chunk) {
+  if constexpr (DP == 64) {
+    const int line = row >> 1;
+    return line * 128 + (((row & 1) * 4 + chunk) ^ (2 * (line & 3))) * 16;
+  } else {
+    return ((chunk >> 3) * T + row) * 128 + ((chunk & 7) ^ ((row & 6) ^ (row & 1) * 4)) * 16;
+  }
+}
+// First of the two columns of a value that lane group g has in its i-th product.
+template <int DP> __device__ __forceinline__ int column(int g, int i) {
+  return DP == 256 ? 128 * (i >> 3) + 16 * g + 2 * (i & 7) : DP / 8 * g + 2 * i;
 }
 
 // Tokens that sequence b's new token sees.
@@ -117,25 +140,31 @@ __device__ __forceinline__ Seen seen(const KvCache& c, int window, int b) {
   return {window && len > window ? len - window : 0, len};
 }
 
-// Where a step of the line is: sequence, unit of it, step of the unit, steps of the unit.
+// Where a step of the line is: sequence, key head, tile of its query heads, step, and how many
+// steps the sequence has.
 struct Spot {
-  int b, unit;
-  int step, steps;
+  int b, head, tile, step, steps;
 };
+template <int T> __device__ __forceinline__ int steps_seen(const KvCache& c, int window, int b) {
+  const Seen s = seen(c, window, b);
+  return (s.end - s.first + T - 1) / T;
+}
 
-// Steps of all sequences before those of each thread's share (exclusive sums in shared
-// memory, the line's length behind them).
-__device__ __forceinline__ int share(int seqs) { return (seqs + 32 * WARPS - 1) / (32 * WARPS); }
-template <int T> __device__ void line_up(const KvCache& c, int window, int units, long long* before, long long* warp_sum) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = share(c.seqs);
+// a / b for a >= 0, b > 0 (lines are mostly short enough for 32 bits, which divide in a fifth of the time)
+__device__ __noinline__ long long div64(long long a, long long b) { return a / b; }
+__device__ __forceinline__ long long quot(long long a, long long b) {
+  return (a | b) >> 32 ? div64(a, b) : (long long)((unsigned)a / (unsigned)b);
+}
+
+// Sequences in a thread's share of them, and the steps of all shares before each one's (the line's
+// length behind them).
+template <int WARPS> __device__ __forceinline__ int share(int seqs) { return (seqs + 32 * WARPS - 1) / (32 * WARPS); }
+template <int T, int WARPS>
+__device__ __forceinline__ void line_up(const KvCache& c, int window, int units, long long* before, long long* warp_sum) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = share<WARPS>(c.seqs);
   long long n = 0;
-  for (int i = 0; i < per; ++i) {
-    const int b = tid * per + i;
-    if (b < c.seqs) {
-      const Seen s = seen(c, window, b);
-      n += (s.end - s.first + T - 1) / T;
-    }
-  }
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < c.seqs) n += steps_seen<T>(c, window, tid * per + i);
   n *= units;
   long long sum = n;
 #pragma unroll
@@ -146,42 +175,42 @@ template <int T> __device__ void line_up(const KvCache& c, int window, int units
   if (lane == 31) warp_sum[warp] = sum;
   __syncthreads();
   long long base = 0;
-  for (int w = 0; w < warp; ++w) base += warp_sum[w];
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) base += w < warp ? warp_sum[w] : 0;
   before[tid] = base + sum - n;
   if (tid == 32 * WARPS - 1) before[32 * WARPS] = base + sum;
   __syncthreads();
 }
-// The spot of step `at` of the line (below its length).
-template <int T>
-__device__ Spot locate(const KvCache& c, int window, int units, const long long* before, long long at) {
-  int lo = 0, hi = 32 * WARPS;   // the last share that starts at or before `at`
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (before[mid] <= at) lo = mid;
-    else hi = mid;
-  }
+// The spot of step `at` of the line (below its length), by a whole warp.
+template <int T, int WARPS>
+__device__ __noinline__ Spot locate(const KvCache& c, int window, int tiles, const long long* before, long long at) {
+  const int lane = threadIdx.x & 31;
+  // the last share that starts at or before `at`: among every WARPS-th, then behind that one
+  int lo = WARPS * (__popc(__ballot_sync(0xffffffffu, before[lane * WARPS] <= at)) - 1);
+  lo += __popc(__ballot_sync(0xffffffffu, lane < WARPS && before[lo + min(lane, WARPS - 1)] <= at)) - 1;
   at -= before[lo];
-  for (int b = lo * share(c.seqs); b < c.seqs; ++b) {
-    const Seen s = seen(c, window, b);
-    const int steps = (s.end - s.first + T - 1) / T;
+  const int units = c.heads * tiles;
+  for (int b = lo * share<WARPS>(c.seqs); b < c.seqs; ++b) {
+    const int steps = steps_seen<T>(c, window, b);
     if (at < (long long)steps * units) {
-      const int unit = (int)(at / steps);
-      return {b, unit, (int)(at - (long long)unit * steps), steps};
+      const int unit = (int)quot(at, steps), head = unit / tiles;
+      return {b, head, unit - head * tiles, (int)(at - (long long)unit * steps), steps};
     }
     at -= (long long)steps * units;
   }
-  return {c.seqs - 1, 0, 0, 1};   // (lengths that change meanwhile: no address out of range)
+  return {c.seqs - 1, 0, 0, 0, 1};   // (lengths that change meanwhile: no address out of range)
 }
 
 // The unit behind the one at s that has steps.
-template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, int window, int units, Spot& s) {
+template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, int window, int tiles, Spot& s) {
   s.step = 0;
-  if (++s.unit < units) return;
-  s.unit = 0;
+  if (++s.tile < tiles) return;
+  s.tile = 0;
+  if (++s.head < c.heads) return;
+  s.head = 0;
   do {
     if (s.b + 1 >= c.seqs) return;   // (as above: the line has an end before)
-    const Seen e = seen(c, window, ++s.b);
-    s.steps = (e.end - e.first + T - 1) / T;
+    s.steps = steps_seen<T>(c, window, ++s.b);
   } while (s.steps == 0);
 }
 
@@ -197,6 +226,11 @@ __device__ __forceinline__ void store_row(T* out, int pairs, int col, int dim, f
     if (col + 1 < dim) out[col + 1] = from_f<T>(y);
   }
 }
+// The largest of the lanes in `mask`, each group of lanes on its own.
+__device__ __forceinline__ float ordered_max(unsigned mask, float x) {
+  const unsigned u = __float_as_uint(x), key = u >> 31 ? ~u : u | 0x80000000u, top = __reduce_max_sync(mask, key);
+  return __uint_as_float(top >> 31 ? top & 0x7fffffffu : ~top);
+}
 // 2^(mw - m - 15) / l, by which sums become results; 0 for a row of no tokens
 __device__ __forceinline__ float closing(float m, float l, float mw) {
   return l == 0.f ? 0.f : ex2(mw - m - 15.f) / l;
@@ -206,38 +240,31 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 }
 
 template <class T, int DP, int NT>
-__global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_constant__ KvCache c,
+__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attention(const __grid_constant__ KvCache c,
                                                                  const __grid_constant__ KvAttnArgs a,
                                                                  const __grid_constant__ Plan p) {
-  typedef Shape<DP, NT> Sh;
-  constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;   // fp16 terms of queries and of weights
+  typedef Shape<T, DP, NT> Sh;
+  constexpr int WARPS = Sh::WARPS, TERMS = sizeof(T) == 4 ? 2 : 1;   // fp16 terms of queries and of weights
   extern __shared__ __align__(16) char smem[];
   __shared__ long long before[32 * WARPS + 1], warp_sum[WARPS];
-  __shared__ int part_unit[WARPS][2][2];          // sequence and unit of a warp's partial results, -1: none
-  __shared__ int part_ends[WARPS];                // whether the first of them has its unit's last step
+  // partial results of the block's units, in the line's order: what a warp has of a unit that began
+  // before its stretch, then of one that goes on behind it
+  __shared__ int2 part_of[2 * WARPS];             // sequence (-1: none), 2 * unit + whether its last step is in
+  __shared__ float4 part_by[2 * WARPS][Sh::NQ];   // factors of sums and softmax sum, the unit's maxima
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, j = lane & 3;
-  const int units = c.heads * p.tiles, dim = c.head_dim;
+  const int dim = c.head_dim;
+  if (threadIdx.x < 2 * WARPS) part_of[threadIdx.x] = make_int2(-1, 0);
   pdl_trigger();
   pdl_wait();
 
-  // rows of sequences without tokens
-  for (int b = blockIdx.x; b < c.seqs; b += gridDim.x) {
-    const Seen s = seen(c, a.window, b);
-    if (s.end > s.first) continue;
-    T* out = reinterpret_cast<T*>(a.out) + b * a.ldo;
-    for (int i = threadIdx.x; i < a.q_heads * dim; i += 32 * WARPS) out[i] = from_f<T>(0.f);
-    if (a.lse)
-      for (int i = threadIdx.x; i < a.q_heads; i += 32 * WARPS) a.lse[(long long)b * a.q_heads + i] = __int_as_float(0xff800000);
-  }
-
-  line_up<Sh::T>(c, a.window, units, before, warp_sum);
+  line_up<Sh::T, WARPS>(c, a.window, c.heads * p.tiles, before, warp_sum);
   const long long total = before[32 * WARPS];
   // blocks that have a share: with a step to every warp
   const long long blocks = max(1ll, min((long long)gridDim.x, (total + WARPS - 1) / WARPS));
   auto edge = [&](long long i) {   // of block i: its first step of the line
-    long long at = total * min(i, blocks) / blocks;
+    long long at = quot(total * min(i, blocks), blocks);
     if (p.whole && at < total) {
-      const Spot s = locate<Sh::T>(c, a.window, units, before, at);
+      const Spot s = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, at);
       if (s.step) at += s.steps - s.step;
     }
     return at;
@@ -245,7 +272,6 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
   const long long c0 = edge(blockIdx.x), c1 = edge(blockIdx.x + 1ll);
   // (rounded up: the first warp has steps where any has)
   const long long w0 = c0 + ((c1 - c0) * warp + WARPS - 1) / WARPS, w1 = c0 + ((c1 - c0) * (warp + 1) + WARPS - 1) / WARPS;
-  if (lane == 0) part_unit[warp][0][0] = part_unit[warp][1][0] = -1, part_ends[warp] = 0;
 
   char* ring = smem + warp * Sh::RING;
   float* part0 = reinterpret_cast<float*>(smem + WARPS * Sh::RING) + warp * Sh::PART;
@@ -253,7 +279,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
   if (w0 < w1) {
-    Spot in = locate<Sh::T>(c, a.window, units, before, w0), at = in;
+    Spot in = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, w0), at = in;
     int to_issue = (int)min((long long)0x7fffffff, w1 - w0), to_do = to_issue;
     Seen in_seen = seen(c, a.window, in.b);
 
@@ -266,77 +292,86 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
     };
     int entry = look_up();
     int stage_in = 0;
-    auto issue = [&] {
+    // this lane's part of every copy: 16 bytes of the token at lane / (DP / 16) behind the copy's first
+    const int col = 16 * (lane % (DP / 16)), sub = lane / (DP / 16), n_col = min(16, max(0, dim - col));
+    const char *kb, *vb;   // of the unit's key head
+    const float *ksb, *vsb;
+    auto heads_of = [&](int head) {
+      kb = reinterpret_cast<const char*>(c.k) + head * c.k_stride[2];
+      vb = reinterpret_cast<const char*>(c.v) + head * c.v_stride[2];
+      ksb = c.k_scale + head * c.k_scale_stride[2];
+      vsb = c.v_scale + head * c.v_scale_stride[2];
+    };
+    heads_of(in.head);
+    unsigned in_page = 0, in_slot = 0, in_mask = 0;
+    // Copies of a step's tokens from base + unit * (their offsets) to dst; `all`: no token of it is masked
+    // and no column is missing.
+    auto copy = [&](auto all, uint32_t dst, const char* base, unsigned unit, unsigned at) {
+      base += n_col ? col : 0;
+#pragma unroll
+      for (int i = 0; i < Sh::T / Sh::ROWS; ++i) {
+        const int row = Sh::ROWS * i + sub;
+        const char* src = base + (unsigned long long)__shfl_sync(0xffffffffu, at, row) * unit;
+        const uint32_t to = dst + place<DP, Sh::T>(row, lane % (DP / 16));
+        if (all) cp_async16s(to, src);
+        else cp_async16s(to, src, in_mask >> row & 1 ? n_col : 0);
+      }
+    };
+    // The next step's keys, then its values, each a group of copies on its own (an empty one
+    // behind the last step keeps the count).
+    auto issue_keys = [&] {
       if (to_issue > 0) {
-        const int t = token(), slot = t - page_of(t) * c.page_size;
+        const int t = token();
         const bool there = (unsigned)entry < (unsigned)c.pages && t < in_seen.end;
-        const long long page = there ? entry : 0, sl = there ? slot : 0;
-        const unsigned mask = __ballot_sync(0xffffffffu, there);
-        const int head = in.unit / p.tiles;
-        const long long ko = page * c.k_stride[0] + sl * c.k_stride[1], vo = page * c.v_stride[0] + sl * c.v_stride[1];
-        const char* kb = reinterpret_cast<const char*>(c.k) + head * c.k_stride[2];
-        const char* vb = reinterpret_cast<const char*>(c.v) + head * c.v_stride[2];
+        in_page = there ? entry : 0;
+        in_slot = there ? t - page_of(t) * c.page_size : 0;
+        in_mask = __ballot_sync(0xffffffffu, there);
         const uint32_t st = ring_s + stage_in * Sh::STAGE;
-#pragma unroll
-        for (int mt = 0; mt < Sh::MT; ++mt)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int k = 16 * mt + 8 * r + g;
-            const char* src = kb + __shfl_sync(0xffffffffu, ko, k);
-            const bool ok = mask >> k & 1;
-#pragma unroll
-            for (int i = 0; i < Sh::NK; ++i) {
-              const int col = 16 * (j + 4 * i), n = ok ? min(16, max(0, dim - col)) : 0;
-              cp_async16s(st + ((mt * 2 + r) * Sh::NK + i) * 512 + lane * 16, src + (n ? col : 0), n);
-            }
-          }
-        const uint32_t sv = st + Sh::T * DP;
-#pragma unroll
-        for (int mt = 0; mt < Sh::MT; ++mt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int k = 16 * mt + 8 * (r >> 1) + 2 * j + (r & 1);
-            const char* src = vb + __shfl_sync(0xffffffffu, vo, k);
-            const bool ok = mask >> k & 1;
-#pragma unroll
-            for (int i = 0; i < Sh::NV; ++i) {
-              const int col = DP / 8 * g + Sh::VB * i, n = ok ? min(Sh::VB, max(0, dim - col)) : 0;
-              const uint32_t dst = sv + ((mt * 4 + r) * Sh::NV + i) * (32 * Sh::VB) + lane * Sh::VB;
-              if constexpr (Sh::VB == 16) cp_async16s(dst, src + (n ? col : 0), n);
-              else cp_async8(dst, src + (n ? col : 0), n);
-            }
-          }
-        const uint32_t ss = st + Sh::T * DP * 2;
-        if (lane < Sh::T) {
-          cp_async4s(ss + 4 * lane, c.k_scale + (page * c.k_scale_stride[0] + sl * c.k_scale_stride[1] + head * c.k_scale_stride[2]),
-                     there ? 4 : 0);
-          cp_async4s(ss + 4 * (Sh::T + lane),
-                     c.v_scale + (page * c.v_scale_stride[0] + sl * c.v_scale_stride[1] + head * c.v_scale_stride[2]), there ? 4 : 0);
-        }
-        if (lane == 0) *reinterpret_cast<unsigned*>(ring + stage_in * Sh::STAGE + Sh::T * DP * 2 + Sh::T * 8) = mask;
+        const unsigned kat = in_page * p.k_unit[0] + in_slot * p.k_unit[1];
+        if (in_mask == 0xffffffffu && dim == DP) copy(std::true_type(), st, kb, p.k_bytes, kat);
+        else copy(std::false_type(), st, kb, p.k_bytes, kat);
+        if (lane < Sh::T)
+          cp_async4s(st + Sh::T * DP * 2 + 4 * lane,
+                     ksb + ((unsigned long long)in_page * p.ks[0] + (unsigned long long)in_slot * p.ks[1]), there ? 4 : 0);
+        if (lane == 0) *reinterpret_cast<unsigned*>(ring + stage_in * Sh::STAGE + Sh::T * DP * 2 + Sh::T * 8) = in_mask;
+      }
+      cp_commit();
+    };
+    auto issue_values = [&] {
+      if (to_issue > 0) {
+        const uint32_t st = ring_s + stage_in * Sh::STAGE + Sh::T * DP;
+        const unsigned vat = in_page * p.v_unit[0] + in_slot * p.v_unit[1];
+        if (in_mask == 0xffffffffu && dim == DP) copy(std::true_type(), st, vb, p.v_bytes, vat);
+        else copy(std::false_type(), st, vb, p.v_bytes, vat);
+        if (lane < Sh::T)
+          cp_async4s(st + Sh::T * DP + 4 * (Sh::T + lane),
+                     vsb + ((unsigned long long)in_page * p.vs[0] + (unsigned long long)in_slot * p.vs[1]), in_mask >> lane & 1 ? 4 : 0);
         stage_in = stage_in + 1 == Sh::STAGES ? 0 : stage_in + 1;
         if (--to_issue > 0) {
           if (++in.step == in.steps) {
-            next_unit<Sh::T>(c, a.window, units, in);
+            next_unit<Sh::T>(c, a.window, p.tiles, in);
             in_seen = seen(c, a.window, in.b);
+            heads_of(in.head);
           }
           entry = look_up();
         }
       }
-      cp_commit();   // (an empty group keeps the count)
+      cp_commit();
     };
-#pragma unroll
-    for (int i = 0; i < Sh::STAGES; ++i) issue();
-
     unsigned qf[NT][TERMS][DP / 16][2];
     float qs[NT][2];                         // of queries 2j, 2j + 1: what a product is multiplied by
     float m[NT][2], l[NT][2], mw[NT][2], o[NT][DP / 16][4];
-    int stage = 0, begun = at.step == 0;     // whether this warp has the unit's first step
-    bool fresh = true;
-    while (to_do > 0) {
+    int stage = 0;
+    bool begun = at.step == 0, fresh = true;   // whether this warp has the unit's first step; its queries come next
+    // (the first rounds only fill the ring: one copy of the code that does)
+    for (int round = -Sh::STAGES; to_do > 0; ++round) {
+      const bool on = round >= 0;
+      unsigned mask = 0;
+      float s[Sh::MT][NT][4];
+      if (on) {
       if (fresh) {
         fresh = false;
-        const int head = at.unit / p.tiles, tile = at.unit - head * p.tiles;
+        const int head = at.head, tile = at.tile;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           // query g of the tile: four adjacent columns for each 16 of the sum
@@ -383,12 +418,11 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
         }
       }
 
-      cp_wait<Sh::STAGES - 1>();
+      cp_wait<2 * Sh::STAGES - 1>();
       __syncwarp();
       const char* st = ring + stage * Sh::STAGE;
       const float* sc = reinterpret_cast<const float*>(st + Sh::T * DP * 2);
-      const unsigned mask = *reinterpret_cast<const unsigned*>(sc + 2 * Sh::T);
-      float s[Sh::MT][NT][4];
+      mask = *reinterpret_cast<const unsigned*>(sc + 2 * Sh::T);
 #pragma unroll
       for (int mt = 0; mt < Sh::MT; ++mt) {
 #pragma unroll
@@ -397,8 +431,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
           for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.f;
 #pragma unroll
         for (int i = 0; i < Sh::NK; ++i) {
-          const uint4 u = *reinterpret_cast<const uint4*>(st + (mt * 2 * Sh::NK + i) * 512 + lane * 16);
-          const uint4 v = *reinterpret_cast<const uint4*>(st + ((mt * 2 + 1) * Sh::NK + i) * 512 + lane * 16);
+          const uint4 u = *reinterpret_cast<const uint4*>(st + place<DP, Sh::T>(16 * mt + g, j + 4 * i));
+          const uint4 v = *reinterpret_cast<const uint4*>(st + place<DP, Sh::T>(16 * mt + 8 + g, j + 4 * i));
           const unsigned uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -413,8 +447,32 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
         }
       }
 
-      // scores of tokens 16 mt + 8 r + g (masked: -infinity, the scales 0)
-      float sv[Sh::MT][2];
+      // scores of tokens 16 mt + 8 r + g (masked: -infinity)
+#pragma unroll
+      for (int mt = 0; mt < Sh::MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int k = 16 * mt + 8 * r + g;
+          const float ks = kv_scale(sc[k]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& x = s[mt][nt][2 * r + e];
+              x *= ks * qs[nt][e];
+              if (mask != 0xffffffffu && !(mask >> k & 1)) x = __int_as_float(0xff800000);
+            }
+        }
+      __syncwarp();   // the stage's keys, their scales and the mask have been read
+      }
+      issue_keys();
+      if (on) {
+      cp_wait<2 * Sh::STAGES - 1>();
+      __syncwarp();
+      const char* st = ring + stage * Sh::STAGE;
+      const float* sc = reinterpret_cast<const float*>(st + Sh::T * DP * 2);
+
+      float sv[Sh::MT][2];   // (of masked tokens 0)
       float top[NT][2], topw[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -425,16 +483,13 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int k = 16 * mt + 8 * r + g;
-          const bool ok = mask >> k & 1;
-          const float ks = kv_scale(sc[k]);
           sv[mt][r] = kv_scale(sc[Sh::T + k]);
           const float lsv = lg2(sv[mt][r]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float& x = s[mt][nt][2 * r + e];
-              x = ok ? x * (ks * qs[nt][e]) : __int_as_float(0xff800000);
+              const float x = s[mt][nt][2 * r + e];
               top[nt][e] = fmaxf(top[nt][e], x);
               topw[nt][e] = fmaxf(topw[nt][e], x + lsv);
             }
@@ -503,7 +558,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
           unsigned w[4][Sh::VB / 4];   // tokens 2j, 2j + 1, 2j + 8, 2j + 9: VB adjacent columns
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const char* src = st + Sh::T * DP + ((mt * 4 + r) * Sh::NV + i) * (32 * Sh::VB) + lane * Sh::VB;
+            const int row = 16 * mt + 8 * (r >> 1) + 2 * j + (r & 1), at = column<DP>(g, i * (Sh::VB / 2));
+            const char* src = st + Sh::T * DP + place<DP, Sh::T>(row, at / 16) + at % 16;
             if constexpr (Sh::VB == 16) {
               const uint4 u = *reinterpret_cast<const uint4*>(src);
               w[r][0] = u.x, w[r][1] = u.y, w[r][2] = u.z, w[r][3] = u.w;
@@ -513,21 +569,26 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
             }
           }
 #pragma unroll
-          for (int k = 0; k < Sh::VB / 2; ++k) {
-            unsigned x[4];
+          for (int k = 0; k < Sh::VB / 4; ++k) {
+            // bytes of two tokens side by side: a conversion makes a column's pair of tokens
+            const unsigned x[2] = {__byte_perm(w[0][k], w[1][k], 0x5140), __byte_perm(w[0][k], w[1][k], 0x7362)};
+            const unsigned y[2] = {__byte_perm(w[2][k], w[3][k], 0x5140), __byte_perm(w[2][k], w[3][k], 0x7362)};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = cvt_e4m3x2((unsigned short)(w[r][k / 2] >> (16 * (k & 1))));
-            const unsigned a0 = __byte_perm(x[0], x[1], 0x5410), a1 = __byte_perm(x[0], x[1], 0x7632);
-            const unsigned a2 = __byte_perm(x[2], x[3], 0x5410), a3 = __byte_perm(x[2], x[3], 0x7632);
+            for (int h = 0; h < 2; ++h) {
+              const unsigned a0 = cvt_e4m3x2((unsigned short)x[h]), a1 = cvt_e4m3x2((unsigned short)(x[h] >> 16));
+              const unsigned a2 = cvt_e4m3x2((unsigned short)y[h]), a3 = cvt_e4m3x2((unsigned short)(y[h] >> 16));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+              for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int t = 0; t < TERMS; ++t)
-                mma16816(o[nt][i * (Sh::VB / 2) + k], a0, a1, a2, a3, pb[mt][nt][t][0], pb[mt][nt][t][1]);
+                for (int t = 0; t < TERMS; ++t)
+                  mma16816(o[nt][i * (Sh::VB / 2) + 2 * k + h], a0, a1, a2, a3, pb[mt][nt][t][0], pb[mt][nt][t][1]);
+            }
           }
         }
-      __syncwarp();   // the stage's scales and mask have been read
-      issue();
+      __syncwarp();   // the stage's values and their scales have been read
+      }
+      issue_values();
+      if (!on) continue;
       stage = stage + 1 == Sh::STAGES ? 0 : stage + 1;
       --to_do;
 
@@ -537,7 +598,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
         continue;
       }
       // the unit, or this warp's part of it, is over
-      const int head = at.unit / p.tiles, tile = at.unit - head * p.tiles;
+      const int head = at.head, tile = at.tile;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -555,7 +616,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
             T* out = reinterpret_cast<T*>(a.out) + at.b * a.ldo + (long long)qh * dim;
             const float f = closing(m[nt][e], l[nt][e], mw[nt][e]);
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) store_row(out, p.pairs, DP / 8 * g + 2 * i, dim, o[nt][i][e] * f, o[nt][i][2 + e] * f);
+            for (int i = 0; i < DP / 16; ++i) store_row(out, p.pairs, column<DP>(g, i), dim, o[nt][i][e] * f, o[nt][i][2 + e] * f);
             if (a.lse && g == 0) a.lse[(long long)at.b * a.q_heads + qh] = lse_of(m[nt][e], l[nt][e]);
           }
       } else {
@@ -572,89 +633,98 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
             float* row = part + (nt * 8 + 2 * j + e) * DP;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i)
-              *reinterpret_cast<float2*>(row + DP / 8 * g + 2 * i) = make_float2(o[nt][i][e], o[nt][i][2 + e]);
+              *reinterpret_cast<float2*>(row + column<DP>(g, i)) = make_float2(o[nt][i][e], o[nt][i][2 + e]);
             if (g == 0)
               *reinterpret_cast<float4*>(part + Sh::NQ * DP + 4 * (nt * 8 + 2 * j + e)) = make_float4(m[nt][e], l[nt][e], mw[nt][e], 0.f);
           }
-        if (lane == 0) {
-          part_unit[warp][which][0] = at.b;
-          part_unit[warp][which][1] = at.unit;
-          if (!which) part_ends[warp] = ends;
-        }
+        if (lane == 0) part_of[2 * warp + which] = make_int2(at.b, 2 * (head * p.tiles + tile) + ends);
       }
-      begun = 1;
+      begun = true;
       fresh = true;
       if (to_do > 0) {
-        if (ends) next_unit<Sh::T>(c, a.window, units, at);
+        if (ends) next_unit<Sh::T>(c, a.window, p.tiles, at);
       }
     }
   }
-  __syncthreads();
 
-  // Units of several warps of this block: chain 0 is one that began before the block (warp 0 has
-  // its first step here), chain w + 1 the one that warp w began and did not end.
+  // rows of sequences without tokens
+  for (int b = blockIdx.x; b < c.seqs; b += gridDim.x) {
+    if (steps_seen<Sh::T>(c, a.window, b)) continue;
+    T* out = reinterpret_cast<T*>(a.out) + b * a.ldo;
+    for (int i = threadIdx.x; i < a.q_heads * dim; i += 32 * WARPS) out[i] = from_f<T>(0.f);
+    if (a.lse)
+      for (int i = threadIdx.x; i < a.q_heads; i += 32 * WARPS) a.lse[(long long)b * a.q_heads + i] = __int_as_float(0xff800000);
+  }
+
   float* ws = reinterpret_cast<float*>(a.ws) + (long long)blockIdx.x * 2 * Sh::PART;
   int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART) + 4 * blockIdx.x;
-  bool opened = false;   // a unit goes on in the next blocks
-  for (int chain = 0; chain <= WARPS; ++chain) {
-    const int w = chain ? chain - 1 : 0, k0 = chain ? 1 : 0;
-    const int b = part_unit[w][k0][0];
-    if (b < 0) continue;
-    const int unit = part_unit[w][k0][1];
-    int n = 1;   // warps that it goes over, some of them without steps
-    bool ends = k0 ? false : part_ends[w];
-    while (!ends && w + n < WARPS) {
-      if (part_unit[w + n][0][0] == b && part_unit[w + n][0][1] == unit) ends = part_ends[w + n];
-      else if (part_unit[w + n][0][0] >= 0) break;
-      ++n;
-    }
-    const int head = unit / p.tiles, tile = unit - head * p.tiles;
-    for (int x = threadIdx.x; x < Sh::NQ * (DP / 4); x += 32 * WARPS) {
-      const int q = x / (DP / 4), d = 4 * (x - q * (DP / 4)), qi = tile * Sh::NQ + q;
-      if (qi >= p.group) continue;
-      float4 sum = make_float4(0, 0, 0, 0);
-      float m = NONE, mw = NONE, l = 0.f;
-      for (int k = 0; k < n; ++k) {
-        const int kind = k ? 0 : k0;
-        if (part_unit[w + k][kind][0] != b || part_unit[w + k][kind][1] != unit) continue;   // a warp without steps
-        const float* part = kind ? reinterpret_cast<const float*>(smem + (w + k) * Sh::RING)
-                                 : reinterpret_cast<const float*>(smem + WARPS * Sh::RING) + (w + k) * Sh::PART;
-        const float4 st = *reinterpret_cast<const float4*>(part + Sh::NQ * DP + 4 * q);
-        const float4 v = *reinterpret_cast<const float4*>(part + q * DP + d);
-        const float mn = fmaxf(m, st.x), mwn = fmaxf(mw, st.z), f = ex2(mw - mwn), fk = ex2(st.z - mwn);
-        l = l * ex2(m - mn) + st.y * ex2(st.x - mn);
-        sum = make_float4(sum.x * f + v.x * fk, sum.y * f + v.y * fk, sum.z * f + v.z * fk, sum.w * f + v.w * fk);
-        m = mn;
-        mw = mwn;
+  __syncthreads();
+  // Partial results join in every thread's registers; lane r holds which unit the r-th is of.
+  const int2 of = lane < 2 * WARPS ? part_of[lane] : make_int2(-1, 0);
+  const unsigned have = __ballot_sync(0xffffffffu, of.x >= 0);
+  if (have == 0) {
+    if (!p.whole && threadIdx.x == 0) meta[2] = 0;
+    return;
+  }
+  auto part = [&](int r) { return r & 1 ? reinterpret_cast<const float*>(smem + (r >> 1) * Sh::RING)
+                                        : reinterpret_cast<const float*>(smem + WARPS * Sh::RING) + (r >> 1) * Sh::PART; };
+  // factors that bring a unit's partial results to its maxima: a warp to a query, a lane to each
+  const unsigned same = __match_any_sync(0xffffffffu, (unsigned long long)(unsigned)of.x << 32 | (unsigned)(of.y >> 1));
+  for (int q = warp; q < Sh::NQ; q += WARPS) {
+    const float4 v = of.x >= 0 ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
+    const float m = ordered_max(same, v.x), mw = ordered_max(same, v.z);
+    if (lane < 2 * WARPS) part_by[lane][q] = make_float4(ex2(v.z - mw), v.y * ex2(v.x - m), m, mw);
+  }
+  __syncthreads();
+  const unsigned last_of = have & ~__ballot_sync(0xffffffffu, of.x >= 0 && same >> lane >> 1 != 0);   // of their units
+  for (int x = threadIdx.x; x < Sh::NQ * (DP / 4); x += 32 * WARPS) {
+    const int q = x / (DP / 4), d = 4 * (x - q * (DP / 4));
+    float4 sum = make_float4(0, 0, 0, 0);
+    float l = 0.f;
+    bool first = true, here = false;   // whether the unit began in this block
+    for (unsigned left = have; left; left &= left - 1) {
+      const int r = __ffs(left) - 1;
+      const float4 by = part_by[r][q], v = *reinterpret_cast<const float4*>(part(r) + q * DP + d);
+      sum = make_float4(fmaf(v.x, by.x, sum.x), fmaf(v.y, by.x, sum.y), fmaf(v.z, by.x, sum.z), fmaf(v.w, by.x, sum.w));
+      l += by.y;
+      if (first) here = r & 1;
+      first = false;
+      if (!(last_of >> r & 1)) continue;
+      const int2 u = part_of[r];
+      const int unit = u.y >> 1, head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
+      if (qi < p.group) {
+        if (here && (u.y & 1)) {
+          const int qh = head * p.group + qi;
+          T* out = reinterpret_cast<T*>(a.out) + u.x * a.ldo + (long long)qh * dim;
+          const float f = closing(by.z, l, by.w);
+          store_row(out, p.pairs, d, dim, sum.x * f, sum.y * f);
+          store_row(out, p.pairs, d + 2, dim, sum.z * f, sum.w * f);
+          if (a.lse && d == 0) a.lse[(long long)u.x * a.q_heads + qh] = lse_of(by.z, l);
+        } else {
+          float* to = ws + (here ? Sh::PART : 0);
+          *reinterpret_cast<float4*>(to + q * DP + d) = sum;
+          if (d == 0) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(by.z, l, by.w, 0.f);
+        }
       }
-      if (chain && ends) {
-        const int qh = head * p.group + qi;
-        T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * dim;
-        const float f = closing(m, l, mw);
-        store_row(out, p.pairs, d, dim, sum.x * f, sum.y * f);
-        store_row(out, p.pairs, d + 2, dim, sum.z * f, sum.w * f);
-        if (a.lse && d == 0) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
-      } else {
-        float* to = ws + (chain ? Sh::PART : 0);
-        *reinterpret_cast<float4*>(to + q * DP + d) = sum;
-        if (d == 0) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, mw, 0.f);
-      }
-    }
-    if (chain && !ends) {
-      opened = true;
-      if (threadIdx.x == 0) meta[0] = b, meta[1] = unit;
+      sum = make_float4(0, 0, 0, 0);
+      l = 0.f;
+      first = true;
     }
   }
-  if (!p.whole && threadIdx.x == 0) {
-    int n = 0;   // blocks that the opened unit goes on in
-    if (opened) {
+  if (!p.whole && warp == 0) {
+    // The unit that goes on in the next blocks, if it began here: how many they are.
+    const int r = 31 - __clz(have);
+    const int2 u = make_int2(__shfl_sync(0xffffffffu, of.x, r), __shfl_sync(0xffffffffu, of.y, r));
+    const unsigned mine = __shfl_sync(0xffffffffu, same, r);
+    int n = 0;
+    if (!(u.y & 1) && (__ffs(mine) - 1 & 1)) {
       // the steps up to its last one, and the block that has that one: the last k with
       // total * k / blocks < those steps
-      const Spot s = locate<Sh::T>(c, a.window, units, before, c1 - 1);
+      const Spot s = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, c1 - 1);
       const long long upto = c1 + (s.steps - 1 - s.step);
-      n = (int)((upto * blocks + total - 1) / total - 1 - blockIdx.x);
+      n = (int)(quot(upto * blocks + total - 1, total) - 1 - blockIdx.x);
     }
-    meta[2] = n;
+    if (lane == 0) meta[0] = u.x, meta[1] = u.y >> 1, meta[2] = n;
   }
 }
 
@@ -663,7 +733,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) k_kv_attention(const __grid_con
 template <class T, int DP, int NT>
 __global__ void __launch_bounds__(DP) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
                                                 const __grid_constant__ Plan p) {
-  typedef Shape<DP, NT> Sh;
+  typedef Shape<T, DP, NT> Sh;
   __shared__ float4 sums[4][DP / 4];
   __shared__ float st[4][3];
   const int q = blockIdx.y, i = blockIdx.x, k0 = threadIdx.x / (DP / 4), d4 = threadIdx.x % (DP / 4);
@@ -707,8 +777,20 @@ int padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 int eights(int dim, int group) { return group > 8 && dim <= 128 ? 2 : 1; }
 long long steps_of(int dim, long long tokens) { return (tokens + (dim > 128 ? 15 : 31)) / (dim > 128 ? 16 : 32); }
 
+// Strides of page and slot in the largest power of two that divides both; false where the last
+// place's offset does not fit 32 bits in it.
+bool units_of(const KvCache& c, const long long (&stride)[3], unsigned (&unit)[2], unsigned* bytes) {
+  const long long st[2] = {c.pages > 1 ? stride[0] : 0, c.page_size > 1 ? stride[1] : 0};
+  int shift = 4;
+  while (shift < 30 && !((st[0] | st[1]) >> shift & 1) && (st[0] | st[1])) ++shift;
+  *bytes = 1u << shift;
+  const unsigned __int128 last = (unsigned __int128)(c.pages - 1) * (st[0] >> shift) + (unsigned __int128)(c.page_size - 1) * (st[1] >> shift);
+  for (int i = 0; i < 2; ++i) unit[i] = (unsigned)(st[i] >> shift);
+  return last <= 0xffffffffu;
+}
+
 template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cudaStream_t s) {
-  typedef Shape<DP, NT> Sh;
+  typedef Shape<T, DP, NT> Sh;
   static PerDevice<int> sms;
   int dev = 0, n_sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -727,14 +809,22 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   const int es = sizeof(T);
   p.pairs = !((uintptr_t)a.out & (2 * es - 1)) && a.ldo % 2 == 0;
   p.scale = a.scale * 1.4426950408889634f;
+  if (!units_of(c, c.k_stride, p.k_unit, &p.k_bytes) || !units_of(c, c.v_stride, p.v_unit, &p.v_bytes)) return cudaErrorNotSupported;
+  for (int i = 0; i < 2; ++i) {
+    const bool one = (i ? c.page_size : c.pages) == 1;
+    const long long ks = one ? 0 : c.k_scale_stride[i], vs = one ? 0 : c.v_scale_stride[i];
+    if (ks > 0xffffffffll || vs > 0xffffffffll) return cudaErrorNotSupported;
+    p.ks[i] = (unsigned)ks;
+    p.vs[i] = (unsigned)vs;
+  }
   long long tokens = (long long)c.table_pages * c.page_size;
   if (a.window) tokens = std::min(tokens, (long long)a.window);
   const long long units = (long long)c.seqs * c.heads * p.tiles, steps = steps_of(c.head_dim, tokens);
   p.whole = steps <= WHOLE_STEPS;
-  // blocks: one to an SM; fewer where there are not two steps to a warp, or no more units
+  // blocks: one to an SM; fewer where there are not two steps to a warp, and one to a unit where blocks take whole ones
   long long grid = std::min(n_sms, GRID_MAX);
-  grid = std::min(grid, p.whole ? units : (units * steps + 2 * WARPS - 1) / (2 * WARPS));
-  e = launch_pdl(k_kv_attention<T, DP, NT>, (unsigned)grid, 32 * WARPS, Sh::SMEM, s, c, a, p);
+  grid = std::min(grid, p.whole ? units : (units * steps + 2 * Sh::WARPS - 1) / (2 * Sh::WARPS));
+  e = launch_pdl(k_kv_attention<T, DP, NT>, (unsigned)grid, 32 * Sh::WARPS, Sh::SMEM, s, c, a, p);
   if (e != cudaSuccess) return e;
   e = launched();
   if (e != cudaSuccess || p.whole) return e;
