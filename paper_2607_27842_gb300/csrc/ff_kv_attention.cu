@@ -66,8 +66,8 @@ template <class E, int DP, int NT> struct Shape {
 struct Plan {
   unsigned div_m, div_s;   // token / page_size
   int group, tiles;        // query heads of a key head, units that share them
-  int whole;               // blocks take whole units
-  int pairs;               // results may be stored in pairs
+  int whole;               // blocks take whole units; 2: one each
+  int pairs, vectors;      // results may be stored in pairs, queries loaded four at a time
   float scale;             // softmax scale times log2(e)
   // strides of page and slot of keys and values in units of 2^shift bytes, by which every place's
   // offset fits 32 bits; of their scales in floats
@@ -156,15 +156,17 @@ __device__ __forceinline__ long long quot(long long a, long long b) {
   return (a | b) >> 32 ? div64(a, b) : (long long)((unsigned)a / (unsigned)b);
 }
 
-// Sequences in a thread's share of them, and the steps of all shares before each one's (the line's
-// length behind them).
-template <int WARPS> __device__ __forceinline__ int share(int seqs) { return (seqs + 32 * WARPS - 1) / (32 * WARPS); }
-template <int T, int WARPS>
-__device__ __forceinline__ void line_up(const KvCache& c, int window, int units, long long* before, long long* warp_sum) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = share<WARPS>(c.seqs);
+// The line, as every warp finds it on its own: a lane has a share of adjacent sequences.
+struct Line {
+  long long before, total;   // steps of the shares before this lane's, and of all
+  int per;                   // sequences to a share
+};
+template <int T> __device__ __forceinline__ Line line_up(const KvCache& c, int window, int units) {
+  const int lane = threadIdx.x & 31, per = (c.seqs + 31) / 32;
   long long n = 0;
+#pragma unroll 4
   for (int i = 0; i < per; ++i)
-    if (tid * per + i < c.seqs) n += steps_seen<T>(c, window, tid * per + i);
+    if (lane * per + i < c.seqs) n += steps_seen<T>(c, window, lane * per + i);
   n *= units;
   long long sum = n;
 #pragma unroll
@@ -172,25 +174,15 @@ __device__ __forceinline__ void line_up(const KvCache& c, int window, int units,
     const long long v = __shfl_up_sync(0xffffffffu, sum, o);
     if (lane >= o) sum += v;
   }
-  if (lane == 31) warp_sum[warp] = sum;
-  __syncthreads();
-  long long base = 0;
-#pragma unroll
-  for (int w = 0; w < WARPS; ++w) base += w < warp ? warp_sum[w] : 0;
-  before[tid] = base + sum - n;
-  if (tid == 32 * WARPS - 1) before[32 * WARPS] = base + sum;
-  __syncthreads();
+  return {sum - n, __shfl_sync(0xffffffffu, sum, 31), per};
 }
 // The spot of step `at` of the line (below its length), by a whole warp.
-template <int T, int WARPS>
-__device__ __noinline__ Spot locate(const KvCache& c, int window, int tiles, const long long* before, long long at) {
-  const int lane = threadIdx.x & 31;
-  // the last share that starts at or before `at`: among every WARPS-th, then behind that one
-  int lo = WARPS * (__popc(__ballot_sync(0xffffffffu, before[lane * WARPS] <= at)) - 1);
-  lo += __popc(__ballot_sync(0xffffffffu, lane < WARPS && before[lo + min(lane, WARPS - 1)] <= at)) - 1;
-  at -= before[lo];
+template <int T> __device__ __noinline__ Spot locate(const KvCache& c, int window, int tiles, Line line, long long at) {
+  // the last share that starts at or before `at`
+  const int lo = __popc(__ballot_sync(0xffffffffu, line.before <= at)) - 1;
+  at -= __shfl_sync(0xffffffffu, line.before, lo);
   const int units = c.heads * tiles;
-  for (int b = lo * share<WARPS>(c.seqs); b < c.seqs; ++b) {
+  for (int b = lo * line.per; b < c.seqs; ++b) {
     const int steps = steps_seen<T>(c, window, b);
     if (at < (long long)steps * units) {
       const int unit = (int)quot(at, steps), head = unit / tiles;
@@ -226,11 +218,6 @@ __device__ __forceinline__ void store_row(T* out, int pairs, int col, int dim, f
     if (col + 1 < dim) out[col + 1] = from_f<T>(y);
   }
 }
-// The largest of the lanes in `mask`, each group of lanes on its own.
-__device__ __forceinline__ float ordered_max(unsigned mask, float x) {
-  const unsigned u = __float_as_uint(x), key = u >> 31 ? ~u : u | 0x80000000u, top = __reduce_max_sync(mask, key);
-  return __uint_as_float(top >> 31 ? top & 0x7fffffffu : ~top);
-}
 // 2^(mw - m - 15) / l, by which sums become results; 0 for a row of no tokens
 __device__ __forceinline__ float closing(float m, float l, float mw) {
   return l == 0.f ? 0.f : ex2(mw - m - 15.f) / l;
@@ -246,32 +233,48 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   typedef Shape<T, DP, NT> Sh;
   constexpr int WARPS = Sh::WARPS, TERMS = sizeof(T) == 4 ? 2 : 1;   // fp16 terms of queries and of weights
   extern __shared__ __align__(16) char smem[];
-  __shared__ long long before[32 * WARPS + 1], warp_sum[WARPS];
   // partial results of the block's units, in the line's order: what a warp has of a unit that began
   // before its stretch, then of one that goes on behind it
   __shared__ int2 part_of[2 * WARPS];             // sequence (-1: none), 2 * unit + whether its last step is in
-  __shared__ float4 part_by[2 * WARPS][Sh::NQ];   // factors of sums and softmax sum, the unit's maxima
+  __shared__ long long part_upto[WARPS];          // the line's steps up to the end of a unit that goes on
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, j = lane & 3;
   const int dim = c.head_dim;
-  if (threadIdx.x < 2 * WARPS) part_of[threadIdx.x] = make_int2(-1, 0);
+  if (lane < 2) part_of[2 * warp + lane] = make_int2(-1, 0);
+  __syncwarp();
   pdl_trigger();
   pdl_wait();
 
-  line_up<Sh::T, WARPS>(c, a.window, c.heads * p.tiles, before, warp_sum);
-  const long long total = before[32 * WARPS];
-  // blocks that have a share: with a step to every warp
-  const long long blocks = max(1ll, min((long long)gridDim.x, (total + WARPS - 1) / WARPS));
-  auto edge = [&](long long i) {   // of block i: its first step of the line
-    long long at = quot(total * min(i, blocks), blocks);
-    if (p.whole && at < total) {
-      const Spot s = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, at);
-      if (s.step) at += s.steps - s.step;
-    }
-    return at;
+  // This warp's steps of the line: w1 - w0 from `at` on, in a block's c0 .. c1.
+  Spot at;
+  long long w0, w1, c1 = 0, total = 1, blocks = 1;
+  auto stretch = [&](long long c0, long long n) {
+    // (rounded up: the first warp has steps where any has)
+    w0 = c0 + (n * warp + WARPS - 1) / WARPS;
+    w1 = c0 + (n * (warp + 1) + WARPS - 1) / WARPS;
   };
-  const long long c0 = edge(blockIdx.x), c1 = edge(blockIdx.x + 1ll);
-  // (rounded up: the first warp has steps where any has)
-  const long long w0 = c0 + ((c1 - c0) * warp + WARPS - 1) / WARPS, w1 = c0 + ((c1 - c0) * (warp + 1) + WARPS - 1) / WARPS;
+  if (p.whole == 2) {   // a block to a unit
+    const int unit = blockIdx.x, per = c.heads * p.tiles, b = unit / per, u = unit - b * per;
+    const int steps = steps_seen<Sh::T>(c, a.window, b);
+    stretch(0, steps);
+    at = {b, u / p.tiles, u % p.tiles, (int)w0, steps};
+  } else {
+    const Line line = line_up<Sh::T>(c, a.window, c.heads * p.tiles);
+    total = line.total;
+    // blocks that have a share: with a step to every warp
+    blocks = p.whole ? gridDim.x : max(1ll, min((long long)gridDim.x, (total + WARPS - 1) / WARPS));
+    auto edge = [&](long long i) {   // of block i: its first step of the line
+      long long e = i >= blocks ? total : quot(total * i, blocks);
+      if (p.whole && e < total) {
+        const Spot s = locate<Sh::T>(c, a.window, p.tiles, line, e);
+        if (s.step) e += s.steps - s.step;
+      }
+      return e;
+    };
+    const long long c0 = edge(blockIdx.x);
+    c1 = edge(blockIdx.x + 1ll);
+    stretch(c0, c1 - c0);
+    if (w0 < w1) at = locate<Sh::T>(c, a.window, p.tiles, line, w0);
+  }
 
   char* ring = smem + warp * Sh::RING;
   float* part0 = reinterpret_cast<float*>(smem + WARPS * Sh::RING) + warp * Sh::PART;
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
   if (w0 < w1) {
-    Spot in = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, w0), at = in;
+    Spot in = at;
     int to_issue = (int)min((long long)0x7fffffff, w1 - w0), to_do = to_issue;
     Seen in_seen = seen(c, a.window, in.b);
 
@@ -361,6 +364,40 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     unsigned qf[NT][TERMS][DP / 16][2];
     float qs[NT][2];                         // of queries 2j, 2j + 1: what a product is multiplied by
     float m[NT][2], l[NT][2], mw[NT][2], o[NT][DP / 16][4];
+    // Queries of the unit at `at`, as they are in memory: of query g of the tile four adjacent columns
+    // for each 16 of the sum.
+    auto load_queries = [&] {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int qi = at.tile * Sh::NQ + nt * 8 + g;
+        const T* q = reinterpret_cast<const T*>(a.q) + at.b * a.ldq + (long long)(at.head * p.group + qi) * dim;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          const int col = 16 * (j + 4 * (s / 4)) + 4 * (s % 4);
+          const bool in = qi < p.group && col < dim;
+          if constexpr (TERMS == 1) {
+            uint2 v = make_uint2(0, 0);
+            if (in) {
+              if (p.vectors) {
+                v = *reinterpret_cast<const uint2*>(q + col);
+              } else {
+                const unsigned short* h = reinterpret_cast<const unsigned short*>(q + col);
+                v = make_uint2(h[0] | (unsigned)h[1] << 16, h[2] | (unsigned)h[3] << 16);
+              }
+            }
+            qf[nt][0][s][0] = v.x, qf[nt][0][s][1] = v.y;
+          } else {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (in) {
+              const unsigned* w = reinterpret_cast<const unsigned*>(q + col);
+              v = p.vectors ? *reinterpret_cast<const uint4*>(w) : make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            qf[nt][0][s][0] = v.x, qf[nt][1][s][0] = v.y, qf[nt][0][s][1] = v.z, qf[nt][1][s][1] = v.w;
+          }
+        }
+      }
+    };
+    load_queries();
     int stage = 0;
     bool begun = at.step == 0, fresh = true;   // whether this warp has the unit's first step; its queries come next
     // (the first rounds only fill the ring: one copy of the code that does)
@@ -371,21 +408,21 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       if (on) {
       if (fresh) {
         fresh = false;
-        const int head = at.head, tile = at.tile;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          // query g of the tile: four adjacent columns for each 16 of the sum
-          const int qi = tile * Sh::NQ + nt * 8 + g;
-          const T* q = reinterpret_cast<const T*>(a.q) + at.b * a.ldq + (long long)(head * p.group + qi) * dim;
-          float x[DP / 16][4], top = 0.f;
+          auto raw = [&](int s, int h) {   // columns 2 h, 2 h + 1 of the four
+            if constexpr (TERMS == 1) {
+              const f32x2 v = bf2u(qf[nt][0][s][h]);
+              return make_float2(lo_f(v), hi_f(v));
+            } else {
+              return make_float2(__uint_as_float(qf[nt][0][s][h]), __uint_as_float(qf[nt][1][s][h]));
+            }
+          };
+          float top = 0.f;
 #pragma unroll
           for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int col = 16 * (j + 4 * (s / 4)) + 4 * (s % 4) + e;
-              x[s][e] = qi < p.group && col < dim ? to_f(q[col]) : 0.f;
-              top = max_abs(top, x[s][e]);
-            }
+            for (int h = 0; h < 2; ++h) top = max_abs(top, max_abs(raw(s, h).x, raw(s, h).y));
           top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, 2));
           // a power of two brings the largest to 2^14 .. 2^15: the terms below lose nothing above
@@ -398,7 +435,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
           for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float u = x[s][2 * h] * up, v = x[s][2 * h + 1] * up;
+              const float2 x = raw(s, h);
+              const float u = x.x * up, v = x.y * up;
               qf[nt][0][s][h] = half2_bits(u, v);
               if constexpr (TERMS == 2) {
                 const float2 hi = __half22float2(*reinterpret_cast<const __half2*>(&qf[nt][0][s][h]));
@@ -637,12 +675,16 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
             if (g == 0)
               *reinterpret_cast<float4*>(part + Sh::NQ * DP + 4 * (nt * 8 + 2 * j + e)) = make_float4(m[nt][e], l[nt][e], mw[nt][e], 0.f);
           }
-        if (lane == 0) part_of[2 * warp + which] = make_int2(at.b, 2 * (head * p.tiles + tile) + ends);
+        if (lane == 0) {
+          part_of[2 * warp + which] = make_int2(at.b, 2 * (head * p.tiles + tile) + ends);
+          part_upto[warp] = w1 + (at.steps - 1 - at.step);
+        }
       }
       begun = true;
       fresh = true;
       if (to_do > 0) {
-        if (ends) next_unit<Sh::T>(c, a.window, p.tiles, at);
+        next_unit<Sh::T>(c, a.window, p.tiles, at);
+        load_queries();
       }
     }
   }
@@ -656,76 +698,73 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       for (int i = threadIdx.x; i < a.q_heads; i += 32 * WARPS) a.lse[(long long)b * a.q_heads + i] = __int_as_float(0xff800000);
   }
 
-  float* ws = reinterpret_cast<float*>(a.ws) + (long long)blockIdx.x * 2 * Sh::PART;
-  int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART) + 4 * blockIdx.x;
   __syncthreads();
-  // Partial results join in every thread's registers; lane r holds which unit the r-th is of.
+  // Lane r holds which unit the r-th partial result is of.  A unit's join: a warp to a query, a lane
+  // to a partial result for the factors that bring it to the unit's maxima, then to its columns.
   const int2 of = lane < 2 * WARPS ? part_of[lane] : make_int2(-1, 0);
   const unsigned have = __ballot_sync(0xffffffffu, of.x >= 0);
-  if (have == 0) {
-    if (!p.whole && threadIdx.x == 0) meta[2] = 0;
-    return;
-  }
   auto part = [&](int r) { return r & 1 ? reinterpret_cast<const float*>(smem + (r >> 1) * Sh::RING)
                                         : reinterpret_cast<const float*>(smem + WARPS * Sh::RING) + (r >> 1) * Sh::PART; };
-  // factors that bring a unit's partial results to its maxima: a warp to a query, a lane to each
-  const unsigned same = __match_any_sync(0xffffffffu, (unsigned long long)(unsigned)of.x << 32 | (unsigned)(of.y >> 1));
-  for (int q = warp; q < Sh::NQ; q += WARPS) {
-    const float4 v = of.x >= 0 ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
-    const float m = ordered_max(same, v.x), mw = ordered_max(same, v.z);
-    if (lane < 2 * WARPS) part_by[lane][q] = make_float4(ex2(v.z - mw), v.y * ex2(v.x - m), m, mw);
-  }
-  __syncthreads();
-  const unsigned last_of = have & ~__ballot_sync(0xffffffffu, of.x >= 0 && same >> lane >> 1 != 0);   // of their units
-  for (int x = threadIdx.x; x < Sh::NQ * (DP / 4); x += 32 * WARPS) {
-    const int q = x / (DP / 4), d = 4 * (x - q * (DP / 4));
-    float4 sum = make_float4(0, 0, 0, 0);
-    float l = 0.f;
-    bool first = true, here = false;   // whether the unit began in this block
-    for (unsigned left = have; left; left &= left - 1) {
-      const int r = __ffs(left) - 1;
-      const float4 by = part_by[r][q], v = *reinterpret_cast<const float4*>(part(r) + q * DP + d);
-      sum = make_float4(fmaf(v.x, by.x, sum.x), fmaf(v.y, by.x, sum.y), fmaf(v.z, by.x, sum.z), fmaf(v.w, by.x, sum.w));
-      l += by.y;
-      if (first) here = r & 1;
-      first = false;
-      if (!(last_of >> r & 1)) continue;
-      const int2 u = part_of[r];
-      const int unit = u.y >> 1, head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
-      if (qi < p.group) {
-        if (here && (u.y & 1)) {
-          const int qh = head * p.group + qi;
-          T* out = reinterpret_cast<T*>(a.out) + u.x * a.ldo + (long long)qh * dim;
-          const float f = closing(by.z, l, by.w);
+  int goes_on = 0;   // blocks behind this one that its last unit goes on in, if it began here
+  for (unsigned left = have; left;) {
+    const int r0 = __ffs(left) - 1;
+    const int b = __shfl_sync(0xffffffffu, of.x, r0), unit = __shfl_sync(0xffffffffu, of.y, r0) >> 1;
+    const bool mine = of.x == b && of.y >> 1 == unit;
+    const unsigned all = __ballot_sync(0xffffffffu, mine);
+    left &= ~all;
+    const bool here = r0 & 1, ends = __ballot_sync(0xffffffffu, mine && (of.y & 1));
+    if (here && !ends && !p.whole) {
+      // the block that has the unit's last step: the last k with total * k / blocks < the steps up to it
+      goes_on = (int)(quot(part_upto[r0 >> 1] * blocks + total - 1, total) - 1 - blockIdx.x);
+      if (threadIdx.x == 0) {
+        int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART) + 4 * blockIdx.x;
+        meta[0] = b, meta[1] = unit;
+      }
+    }
+    const int head = unit / p.tiles, first = (unit - head * p.tiles) * Sh::NQ;
+    for (int q = warp; q < min(Sh::NQ, p.group - first); q += WARPS) {
+      const float4 v = mine ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
+      float m = v.x, mw = v.z;
+#pragma unroll
+      for (int k = 16; k; k >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+        mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, k));
+      }
+      const float by = ex2(v.z - mw);
+      float l = v.y * ex2(v.x - m);
+#pragma unroll
+      for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+      const int qh = head * p.group + first + q;
+      T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * dim;
+      float* to = reinterpret_cast<float*>(a.ws) + (2ll * blockIdx.x + here) * Sh::PART;
+      const bool done = here && ends;
+      const float f = done ? closing(m, l, mw) : 1.f;
+      for (int d = 4 * lane; d - 4 * lane < DP; d += 128) {
+        const bool in = d < DP;
+        float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+        for (unsigned rest = all; rest; rest &= rest - 1) {
+          const int r = __ffs(rest) - 1;
+          const float w = __shfl_sync(0xffffffffu, by, r);
+          const float4 x = in ? *reinterpret_cast<const float4*>(part(r) + q * DP + d) : make_float4(0, 0, 0, 0);
+          sum = make_float4(fmaf(x.x, w, sum.x), fmaf(x.y, w, sum.y), fmaf(x.z, w, sum.z), fmaf(x.w, w, sum.w));
+        }
+        if (!in) continue;
+        if (done) {
           store_row(out, p.pairs, d, dim, sum.x * f, sum.y * f);
           store_row(out, p.pairs, d + 2, dim, sum.z * f, sum.w * f);
-          if (a.lse && d == 0) a.lse[(long long)u.x * a.q_heads + qh] = lse_of(by.z, l);
         } else {
-          float* to = ws + (here ? Sh::PART : 0);
           *reinterpret_cast<float4*>(to + q * DP + d) = sum;
-          if (d == 0) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(by.z, l, by.w, 0.f);
         }
       }
-      sum = make_float4(0, 0, 0, 0);
-      l = 0.f;
-      first = true;
+      if (lane == 0) {
+        if (!done) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, mw, 0.f);
+        else if (a.lse) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
+      }
     }
   }
-  if (!p.whole && warp == 0) {
-    // The unit that goes on in the next blocks, if it began here: how many they are.
-    const int r = 31 - __clz(have);
-    const int2 u = make_int2(__shfl_sync(0xffffffffu, of.x, r), __shfl_sync(0xffffffffu, of.y, r));
-    const unsigned mine = __shfl_sync(0xffffffffu, same, r);
-    int n = 0;
-    if (!(u.y & 1) && (__ffs(mine) - 1 & 1)) {
-      // the steps up to its last one, and the block that has that one: the last k with
-      // total * k / blocks < those steps
-      const Spot s = locate<Sh::T, WARPS>(c, a.window, p.tiles, before, c1 - 1);
-      const long long upto = c1 + (s.steps - 1 - s.step);
-      n = (int)(quot(upto * blocks + total - 1, total) - 1 - blockIdx.x);
-    }
-    if (lane == 0) meta[0] = u.x, meta[1] = u.y >> 1, meta[2] = n;
-  }
+  if (!p.whole && threadIdx.x == 0)
+    reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART)[4 * blockIdx.x + 2] = goes_on;
 }
 
 // Units of several blocks: block (i, q) joins query q of the unit that block i of the first kernel
@@ -808,6 +847,7 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   p.tiles = (p.group + Sh::NQ - 1) / Sh::NQ;
   const int es = sizeof(T);
   p.pairs = !((uintptr_t)a.out & (2 * es - 1)) && a.ldo % 2 == 0;
+  p.vectors = !((uintptr_t)a.q & (4 * es - 1)) && a.ldq % 4 == 0;
   p.scale = a.scale * 1.4426950408889634f;
   if (!units_of(c, c.k_stride, p.k_unit, &p.k_bytes) || !units_of(c, c.v_stride, p.v_unit, &p.v_bytes)) return cudaErrorNotSupported;
   for (int i = 0; i < 2; ++i) {
@@ -820,10 +860,10 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   long long tokens = (long long)c.table_pages * c.page_size;
   if (a.window) tokens = std::min(tokens, (long long)a.window);
   const long long units = (long long)c.seqs * c.heads * p.tiles, steps = steps_of(c.head_dim, tokens);
-  p.whole = steps <= WHOLE_STEPS;
+  p.whole = steps > WHOLE_STEPS ? 0 : units > n_sms ? 1 : 2;
   // blocks: one to an SM; fewer where there are not two steps to a warp, and one to a unit where blocks take whole ones
   long long grid = std::min(n_sms, GRID_MAX);
-  grid = std::min(grid, p.whole ? units : (units * steps + 2 * Sh::WARPS - 1) / (2 * Sh::WARPS));
+  grid = p.whole == 2 ? units : std::min(grid, p.whole ? units : (units * steps + 2 * Sh::WARPS - 1) / (2 * Sh::WARPS));
   e = launch_pdl(k_kv_attention<T, DP, NT>, (unsigned)grid, 32 * Sh::WARPS, Sh::SMEM, s, c, a, p);
   if (e != cudaSuccess) return e;
   e = launched();
