@@ -3,9 +3,11 @@
 // sees is read once for all query heads of its key head.
 //
 // The work is a line of steps: a unit is one key head of one sequence with up to 8 or 16 of
-// its query heads, a step T of its tokens; the units of a sequence follow one another, then
-// the next sequence's.  Every warp of the grid takes an equal stretch of the line,
-// whatever the lengths are, and goes over it on its own: tokens come by asynchronous
+// its query heads, a step T of its tokens.  Units of a sequence whose number divides the
+// warps go together, one to a warp (or to several, which share out the steps): their places are
+// adjacent in memory, as are their scales.  The line has the steps of one such group, of the
+// sequence's next one, then of the next sequence's; every block takes an equal stretch of it,
+// whatever the lengths are, and every warp goes over its own on its own: tokens come by asynchronous
 // copies a step or two ahead, eight lanes to 128 adjacent bytes, into a ring that only this warp
 // knows; e4m3 becomes fp16 in registers, exactly; products are mma.sync m16n8k16 with tokens or columns as the 16 and
 // query heads as the 8, because a token's few query heads would fill 4 of tcgen05's 128
@@ -45,11 +47,13 @@ constexpr int WHOLE_STEPS = 32;
 
 // Shapes of a variant: columns of a head rounded up to DP, NT times 8 query heads.
 template <class E, int DP, int NT> struct Shape {
-  // warps of a block: 16 where their registers (128 to a thread) hold a warp's sums
-  static constexpr int WARPS = DP <= 128 && NT == 1 && sizeof(E) == 2 ? 16 : 8;
+  // warps of a block: as many as have the registers for their sums and queries.  A spilled register
+  // in the loop goes through the 20 KB of L1 that the rings leave: 64 x 8192 tokens took 221 us with
+  // 16 warps of 128 registers (80 bytes spilled), 189 with 12 of 168, 206 with 8.
+  static constexpr int WARPS = NT > 1 || DP == 256 || sizeof(E) == 4 ? 8 : DP == 64 ? 16 : 12;
   static constexpr int MT = DP == 256 ? 1 : 2;                 // groups of 16 tokens in a step
   static constexpr int T = 16 * MT;
-  static constexpr int STAGES = (DP == 64 ? 2 : 1) * (WARPS == 16 ? 1 : 2);
+  static constexpr int STAGES = (DP == 64 ? 2 : 1) * (WARPS > 8 ? 1 : 2);
   static constexpr int NK = DP / 64;                           // 16-byte vectors of a key to a lane
   static constexpr int ROWS = 512 / DP;                        // tokens of a copy by all lanes
   static constexpr int VB = DP >= 128 ? 16 : 8;                // bytes of a value's vector
@@ -66,6 +70,7 @@ template <class E, int DP, int NT> struct Shape {
 struct Plan {
   unsigned div_m, div_s;   // token / page_size
   int group, tiles;        // query heads of a key head, units that share them
+  int together, split;     // units that go together, warps to each of them
   int whole;               // blocks take whole units; 2: one each
   int pairs, vectors;      // results may be stored in pairs, queries loaded four at a time
   float scale;             // softmax scale times log2(e)
@@ -110,10 +115,6 @@ __device__ __forceinline__ void cp_async16s(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void cp_async16s(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void cp_async4s(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-
 // Where the 16 bytes from column 16 * chunk of token `row` lie in a stage's keys or values: lines of
 // 128 bytes (half a token, a token or two) whose vectors change places from line to line, so
 // that neither products' reads (eight lanes: two tokens by four vectors for keys, four tokens
@@ -140,10 +141,10 @@ __device__ __forceinline__ Seen seen(const KvCache& c, int window, int b) {
   return {window && len > window ? len - window : 0, len};
 }
 
-// Where a step of the line is: sequence, key head, tile of its query heads, step, and how many
-// steps the sequence has.
+// Where a step of the line is: sequence, unit (as locate() finds it: group of units), step, and how
+// many steps the sequence has.
 struct Spot {
-  int b, head, tile, step, steps;
+  int b, unit, step, steps;
 };
 template <int T> __device__ __forceinline__ int steps_seen(const KvCache& c, int window, int b) {
   const Seen s = seen(c, window, b);
@@ -161,13 +162,13 @@ struct Line {
   long long before, total;   // steps of the shares before this lane's, and of all
   int per;                   // sequences to a share
 };
-template <int T> __device__ __forceinline__ Line line_up(const KvCache& c, int window, int units) {
+template <int T> __device__ __forceinline__ Line line_up(const KvCache& c, int window, int groups) {
   const int lane = threadIdx.x & 31, per = (c.seqs + 31) / 32;
   long long n = 0;
 #pragma unroll 4
   for (int i = 0; i < per; ++i)
     if (lane * per + i < c.seqs) n += steps_seen<T>(c, window, lane * per + i);
-  n *= units;
+  n *= groups;
   long long sum = n;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -177,29 +178,27 @@ template <int T> __device__ __forceinline__ Line line_up(const KvCache& c, int w
   return {sum - n, __shfl_sync(0xffffffffu, sum, 31), per};
 }
 // The spot of step `at` of the line (below its length), by a whole warp.
-template <int T> __device__ __noinline__ Spot locate(const KvCache& c, int window, int tiles, Line line, long long at) {
+template <int T> __device__ __noinline__ Spot locate(const KvCache& c, int window, int groups, Line line, long long at) {
   // the last share that starts at or before `at`
   const int lo = __popc(__ballot_sync(0xffffffffu, line.before <= at)) - 1;
   at -= __shfl_sync(0xffffffffu, line.before, lo);
-  const int units = c.heads * tiles;
   for (int b = lo * line.per; b < c.seqs; ++b) {
     const int steps = steps_seen<T>(c, window, b);
-    if (at < (long long)steps * units) {
-      const int unit = (int)quot(at, steps), head = unit / tiles;
-      return {b, head, unit - head * tiles, (int)(at - (long long)unit * steps), steps};
+    if (at < (long long)steps * groups) {
+      const int group = (int)quot(at, steps);
+      return {b, group, (int)(at - (long long)group * steps), steps};
     }
-    at -= (long long)steps * units;
+    at -= (long long)steps * groups;
   }
-  return {c.seqs - 1, 0, 0, 0, 1};   // (lengths that change meanwhile: no address out of range)
+  return {c.seqs - 1, 0, 0, 1};   // (lengths that change meanwhile: no address out of range)
 }
 
-// The unit behind the one at s that has steps.
-template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, int window, int tiles, Spot& s) {
+// The warp's next unit that has steps: of the sequence's next group, or of the next sequence.
+template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, const Plan& p, int window, int u, Spot& s) {
   s.step = 0;
-  if (++s.tile < tiles) return;
-  s.tile = 0;
-  if (++s.head < c.heads) return;
-  s.head = 0;
+  s.unit += p.together;
+  if (s.unit < c.heads * p.tiles) return;
+  s.unit = u;
   do {
     if (s.b + 1 >= c.seqs) return;   // (as above: the line has an end before)
     s.steps = steps_seen<T>(c, window, ++s.b);
@@ -245,27 +244,27 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   pdl_wait();
 
   // This warp's steps of the line: w1 - w0 from `at` on, in a block's c0 .. c1.
+  const int sp = warp / p.together, u = warp - sp * p.together, groups = c.heads * p.tiles / p.together;
   Spot at;
   long long w0, w1, c1 = 0, total = 1, blocks = 1;
   auto stretch = [&](long long c0, long long n) {
-    // (rounded up: the first warp has steps where any has)
-    w0 = c0 + (n * warp + WARPS - 1) / WARPS;
-    w1 = c0 + (n * (warp + 1) + WARPS - 1) / WARPS;
+    // (rounded up: the first warp of a unit has steps where any has)
+    w0 = c0 + (sp < p.split ? quot(n * sp + p.split - 1, p.split) : n);
+    w1 = c0 + (sp < p.split ? quot(n * (sp + 1) + p.split - 1, p.split) : n);
   };
   if (p.whole == 2) {   // a block to a unit
-    const int unit = blockIdx.x, per = c.heads * p.tiles, b = unit / per, u = unit - b * per;
-    const int steps = steps_seen<Sh::T>(c, a.window, b);
+    const int b = blockIdx.x / groups, steps = steps_seen<Sh::T>(c, a.window, b);
     stretch(0, steps);
-    at = {b, u / p.tiles, u % p.tiles, (int)w0, steps};
+    at = {b, (int)blockIdx.x - b * groups, (int)w0, steps};
   } else {
-    const Line line = line_up<Sh::T>(c, a.window, c.heads * p.tiles);
+    const Line line = line_up<Sh::T>(c, a.window, groups);
     total = line.total;
     // blocks that have a share: with a step to every warp
-    blocks = p.whole ? gridDim.x : max(1ll, min((long long)gridDim.x, (total + WARPS - 1) / WARPS));
+    blocks = p.whole ? gridDim.x : max(1ll, min((long long)gridDim.x, quot(total + p.split - 1, p.split)));
     auto edge = [&](long long i) {   // of block i: its first step of the line
       long long e = i >= blocks ? total : quot(total * i, blocks);
       if (p.whole && e < total) {
-        const Spot s = locate<Sh::T>(c, a.window, p.tiles, line, e);
+        const Spot s = locate<Sh::T>(c, a.window, groups, line, e);
         if (s.step) e += s.steps - s.step;
       }
       return e;
@@ -273,7 +272,10 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     const long long c0 = edge(blockIdx.x);
     c1 = edge(blockIdx.x + 1ll);
     stretch(c0, c1 - c0);
-    if (w0 < w1) at = locate<Sh::T>(c, a.window, p.tiles, line, w0);
+    if (w0 < w1) {
+      at = locate<Sh::T>(c, a.window, groups, line, w0);
+      at.unit = at.unit * p.together + u;
+    }
   }
 
   char* ring = smem + warp * Sh::RING;
@@ -299,14 +301,17 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     const int col = 16 * (lane % (DP / 16)), sub = lane / (DP / 16), n_col = min(16, max(0, dim - col));
     const char *kb, *vb;   // of the unit's key head
     const float *ksb, *vsb;
-    auto heads_of = [&](int head) {
+    auto heads_of = [&](int unit) {
+      const int head = unit / p.tiles;
       kb = reinterpret_cast<const char*>(c.k) + head * c.k_stride[2];
       vb = reinterpret_cast<const char*>(c.v) + head * c.v_stride[2];
       ksb = c.k_scale + head * c.k_scale_stride[2];
       vsb = c.v_scale + head * c.v_scale_stride[2];
     };
-    heads_of(in.head);
+    heads_of(in.unit);
     unsigned in_page = 0, in_slot = 0, in_mask = 0;
+    float ks_in = 0.f, vs_in = 0.f;   // scales of this lane's token of the last step that was issued, and
+    char* scales_to = ring;           // where they go when they have come
     // Copies of a step's tokens from base + unit * (their offsets) to dst; `all`: no token of it is masked
     // and no column is missing.
     auto copy = [&](auto all, uint32_t dst, const char* base, unsigned unit, unsigned at) {
@@ -333,9 +338,12 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         const unsigned kat = in_page * p.k_unit[0] + in_slot * p.k_unit[1];
         if (in_mask == 0xffffffffu && dim == DP) copy(std::true_type(), st, kb, p.k_bytes, kat);
         else copy(std::false_type(), st, kb, p.k_bytes, kat);
-        if (lane < Sh::T)
-          cp_async4s(st + Sh::T * DP * 2 + 4 * lane,
-                     ksb + ((unsigned long long)in_page * p.ks[0] + (unsigned long long)in_slot * p.ks[1]), there ? 4 : 0);
+        ks_in = vs_in = 0.f;
+        scales_to = ring + stage_in * Sh::STAGE + Sh::T * DP * 2 + 4 * lane;
+        if (there) {
+          ks_in = ksb[(unsigned long long)in_page * p.ks[0] + (unsigned long long)in_slot * p.ks[1]];
+          vs_in = vsb[(unsigned long long)in_page * p.vs[0] + (unsigned long long)in_slot * p.vs[1]];
+        }
         if (lane == 0) *reinterpret_cast<unsigned*>(ring + stage_in * Sh::STAGE + Sh::T * DP * 2 + Sh::T * 8) = in_mask;
       }
       cp_commit();
@@ -346,15 +354,12 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         const unsigned vat = in_page * p.v_unit[0] + in_slot * p.v_unit[1];
         if (in_mask == 0xffffffffu && dim == DP) copy(std::true_type(), st, vb, p.v_bytes, vat);
         else copy(std::false_type(), st, vb, p.v_bytes, vat);
-        if (lane < Sh::T)
-          cp_async4s(st + Sh::T * DP + 4 * (Sh::T + lane),
-                     vsb + ((unsigned long long)in_page * p.vs[0] + (unsigned long long)in_slot * p.vs[1]), in_mask >> lane & 1 ? 4 : 0);
         stage_in = stage_in + 1 == Sh::STAGES ? 0 : stage_in + 1;
         if (--to_issue > 0) {
           if (++in.step == in.steps) {
-            next_unit<Sh::T>(c, a.window, p.tiles, in);
+            next_unit<Sh::T>(c, p, a.window, u, in);
             in_seen = seen(c, a.window, in.b);
-            heads_of(in.head);
+            heads_of(in.unit);
           }
           entry = look_up();
         }
@@ -369,8 +374,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     auto load_queries = [&] {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int qi = at.tile * Sh::NQ + nt * 8 + g;
-        const T* q = reinterpret_cast<const T*>(a.q) + at.b * a.ldq + (long long)(at.head * p.group + qi) * dim;
+        const int head = at.unit / p.tiles, qi = (at.unit - head * p.tiles) * Sh::NQ + nt * 8 + g;
+        const T* q = reinterpret_cast<const T*>(a.q) + at.b * a.ldq + (long long)(head * p.group + qi) * dim;
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s) {
           const int col = 16 * (j + 4 * (s / 4)) + 4 * (s % 4);
@@ -403,6 +408,10 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     // (the first rounds only fill the ring: one copy of the code that does)
     for (int round = -Sh::STAGES; to_do > 0; ++round) {
       const bool on = round >= 0;
+      if (lane < Sh::T) {
+        *reinterpret_cast<float*>(scales_to) = kv_scale(ks_in);
+        *reinterpret_cast<float*>(scales_to + 4 * Sh::T) = kv_scale(vs_in);
+      }
       unsigned mask = 0;
       float s[Sh::MT][NT][4];
       if (on) {
@@ -491,7 +500,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int k = 16 * mt + 8 * r + g;
-          const float ks = kv_scale(sc[k]);
+          const float ks = sc[k];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -521,7 +530,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int k = 16 * mt + 8 * r + g;
-          sv[mt][r] = kv_scale(sc[Sh::T + k]);
+          sv[mt][r] = sc[Sh::T + k];
           const float lsv = lg2(sv[mt][r]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -636,7 +645,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         continue;
       }
       // the unit, or this warp's part of it, is over
-      const int head = at.head, tile = at.tile;
+      const int head = at.unit / p.tiles, tile = at.unit - head * p.tiles;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -676,14 +685,14 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
               *reinterpret_cast<float4*>(part + Sh::NQ * DP + 4 * (nt * 8 + 2 * j + e)) = make_float4(m[nt][e], l[nt][e], mw[nt][e], 0.f);
           }
         if (lane == 0) {
-          part_of[2 * warp + which] = make_int2(at.b, 2 * (head * p.tiles + tile) + ends);
+          part_of[2 * warp + which] = make_int2(at.b, 2 * at.unit + ends);
           part_upto[warp] = w1 + (at.steps - 1 - at.step);
         }
       }
       begun = true;
       fresh = true;
       if (to_do > 0) {
-        next_unit<Sh::T>(c, a.window, p.tiles, at);
+        next_unit<Sh::T>(c, p, a.window, u, at);
         load_queries();
       }
     }
@@ -699,30 +708,35 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   }
 
   __syncthreads();
-  // Lane r holds which unit the r-th partial result is of.  A unit's join: a warp to a query, a lane
-  // to a partial result for the factors that bring it to the unit's maxima, then to its columns.
-  const int2 of = lane < 2 * WARPS ? part_of[lane] : make_int2(-1, 0);
-  const unsigned have = __ballot_sync(0xffffffffu, of.x >= 0);
-  auto part = [&](int r) { return r & 1 ? reinterpret_cast<const float*>(smem + (r >> 1) * Sh::RING)
-                                        : reinterpret_cast<const float*>(smem + WARPS * Sh::RING) + (r >> 1) * Sh::PART; };
-  int goes_on = 0;   // blocks behind this one that its last unit goes on in, if it began here
-  for (unsigned left = have; left;) {
-    const int r0 = __ffs(left) - 1;
-    const int b = __shfl_sync(0xffffffffu, of.x, r0), unit = __shfl_sync(0xffffffffu, of.y, r0) >> 1;
-    const bool mine = of.x == b && of.y >> 1 == unit;
-    const unsigned all = __ballot_sync(0xffffffffu, mine);
-    left &= ~all;
-    const bool here = r0 & 1, ends = __ballot_sync(0xffffffffu, mine && (of.y & 1));
-    if (here && !ends && !p.whole) {
-      // the block that has the unit's last step: the last k with total * k / blocks < the steps up to it
-      goes_on = (int)(quot(part_upto[r0 >> 1] * blocks + total - 1, total) - 1 - blockIdx.x);
-      if (threadIdx.x == 0) {
-        int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART) + 4 * blockIdx.x;
-        meta[0] = b, meta[1] = unit;
+  // A warp joins one query of the units that one place of the groups had: lane r holds which unit the
+  // r-th of their partial results is of, and the factor that brings it to the unit's maxima; then
+  // a lane has four columns.
+  const int queries = min(Sh::NQ, p.group), n_parts = 2 * p.split;
+  float* ws = reinterpret_cast<float*>(a.ws) + (long long)blockIdx.x * p.together * 2 * Sh::PART;
+  int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * p.together * 2 * Sh::PART) + 4 * blockIdx.x;
+  int goes_on = 0;   // blocks behind this one that its last group goes on in, if it began here
+  for (int item = warp; item < p.together * queries; item += WARPS) {
+    const int place = item / queries, q = item - place * queries;
+    auto of_warp = [&](int r) { return (r >> 1) * p.together + place; };
+    auto part = [&](int r) {
+      return r & 1 ? reinterpret_cast<const float*>(smem + of_warp(r) * Sh::RING)
+                   : reinterpret_cast<const float*>(smem + WARPS * Sh::RING) + of_warp(r) * Sh::PART;
+    };
+    const int2 of = lane < n_parts ? part_of[2 * of_warp(lane) + (lane & 1)] : make_int2(-1, 0);
+    for (unsigned left = __ballot_sync(0xffffffffu, of.x >= 0); left;) {
+      const int r0 = __ffs(left) - 1;
+      const int b = __shfl_sync(0xffffffffu, of.x, r0), unit = __shfl_sync(0xffffffffu, of.y, r0) >> 1;
+      const bool mine = of.x == b && of.y >> 1 == unit;
+      const unsigned all = __ballot_sync(0xffffffffu, mine);
+      left &= ~all;
+      const bool here = r0 & 1, ends = __ballot_sync(0xffffffffu, mine && (of.y & 1));
+      if (item == 0 && here && !ends && !p.whole) {
+        // the block that has the group's last step: the last k with total * k / blocks < the steps up to it
+        goes_on = (int)(quot(part_upto[of_warp(r0)] * blocks + total - 1, total) - 1 - blockIdx.x);
+        if (lane == 0) meta[0] = b, meta[1] = unit;
       }
-    }
-    const int head = unit / p.tiles, first = (unit - head * p.tiles) * Sh::NQ;
-    for (int q = warp; q < min(Sh::NQ, p.group - first); q += WARPS) {
+      const int head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
+      if (qi >= p.group) continue;
       const float4 v = mine ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
       float m = v.x, mw = v.z;
 #pragma unroll
@@ -734,9 +748,9 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       float l = v.y * ex2(v.x - m);
 #pragma unroll
       for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
-      const int qh = head * p.group + first + q;
+      const int qh = head * p.group + qi;
       T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * dim;
-      float* to = reinterpret_cast<float*>(a.ws) + (2ll * blockIdx.x + here) * Sh::PART;
+      float* to = ws + (2 * place + here) * Sh::PART;
       const bool done = here && ends;
       const float f = done ? closing(m, l, mw) : 1.f;
       for (int d = 4 * lane; d - 4 * lane < DP; d += 128) {
@@ -763,26 +777,26 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       }
     }
   }
-  if (!p.whole && threadIdx.x == 0)
-    reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * 2 * Sh::PART)[4 * blockIdx.x + 2] = goes_on;
+  if (!p.whole && threadIdx.x == 0) meta[2] = goes_on;
 }
 
-// Units of several blocks: block (i, q) joins query q of the unit that block i of the first kernel
-// began, over the parts in the line's order, four at a time side by side.
+// Units of several blocks: block (i, y) joins a query of a unit of the group that block i of the first
+// kernel began, over the parts in the line's order, four at a time side by side.
 template <class T, int DP, int NT>
 __global__ void __launch_bounds__(DP) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
                                                 const __grid_constant__ Plan p) {
   typedef Shape<T, DP, NT> Sh;
   __shared__ float4 sums[4][DP / 4];
   __shared__ float st[4][3];
-  const int q = blockIdx.y, i = blockIdx.x, k0 = threadIdx.x / (DP / 4), d4 = threadIdx.x % (DP / 4);
+  const int queries = min(Sh::NQ, p.group), place = blockIdx.y / queries, q = blockIdx.y - place * queries;
+  const int i = blockIdx.x, k0 = threadIdx.x / (DP / 4), d4 = threadIdx.x % (DP / 4);
   pdl_trigger();
   pdl_wait();
   const float* ws = reinterpret_cast<const float*>(a.ws);
-  const int* meta = reinterpret_cast<const int*>(ws + (long long)gridDim.x * 2 * Sh::PART) + 4 * i;
+  const int* meta = reinterpret_cast<const int*>(ws + (long long)gridDim.x * p.together * 2 * Sh::PART) + 4 * i;
   const int n = meta[2];
   if (n == 0) return;
-  const int b = meta[0], unit = meta[1], head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
+  const int b = meta[0], unit = meta[1] + place, head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
   if (qi >= p.group) return;
   float4 sum = make_float4(0, 0, 0, 0);
   float m = NONE, mw = NONE, l = 0.f;
@@ -795,7 +809,7 @@ __global__ void __launch_bounds__(DP) k_kv_join(const __grid_constant__ KvCache 
   };
 #pragma unroll 4
   for (int k = k0; k <= n; k += 4) {
-    const float* part = ws + (2ll * (i + k) + (k ? 0 : 1)) * Sh::PART;
+    const float* part = ws + (2ll * ((i + k) * p.together + place) + (k ? 0 : 1)) * Sh::PART;
     const float4 s = *reinterpret_cast<const float4*>(part + Sh::NQ * DP + 4 * q);
     add(*reinterpret_cast<const float4*>(part + q * DP + 4 * d4), s.x, s.y, s.z);
   }
@@ -815,6 +829,13 @@ __global__ void __launch_bounds__(DP) k_kv_join(const __grid_constant__ KvCache 
 int padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 int eights(int dim, int group) { return group > 8 && dim <= 128 ? 2 : 1; }
 long long steps_of(int dim, long long tokens) { return (tokens + (dim > 128 ? 15 : 31)) / (dim > 128 ? 16 : 32); }
+
+// Units that go together: as many of a sequence's as divide them and use seven of eight warps.
+int together(int units, int warps) {
+  int n = std::min(units, warps);
+  while (units % n || 8 * n * (warps / n) < 7 * warps) --n;
+  return n;
+}
 
 // Strides of page and slot in the largest power of two that divides both; false where the last
 // place's offset does not fit 32 bits in it.
@@ -861,14 +882,16 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   if (a.window) tokens = std::min(tokens, (long long)a.window);
   const long long units = (long long)c.seqs * c.heads * p.tiles, steps = steps_of(c.head_dim, tokens);
   p.whole = steps > WHOLE_STEPS ? 0 : units > n_sms ? 1 : 2;
+  p.together = p.whole ? 1 : together(c.heads * p.tiles, Sh::WARPS);
+  p.split = Sh::WARPS / p.together;
   // blocks: one to an SM; fewer where there are not two steps to a warp, and one to a unit where blocks take whole ones
   long long grid = std::min(n_sms, GRID_MAX);
-  grid = p.whole == 2 ? units : std::min(grid, p.whole ? units : (units * steps + 2 * Sh::WARPS - 1) / (2 * Sh::WARPS));
+  grid = p.whole == 2 ? units : std::min(grid, p.whole ? units : (units / p.together * steps + 2 * p.split - 1) / (2 * p.split));
   e = launch_pdl(k_kv_attention<T, DP, NT>, (unsigned)grid, 32 * Sh::WARPS, Sh::SMEM, s, c, a, p);
   if (e != cudaSuccess) return e;
   e = launched();
   if (e != cudaSuccess || p.whole) return e;
-  e = launch_pdl(k_kv_join<T, DP, NT>, dim3((unsigned)grid, Sh::NQ), DP, 0, s, c, a, p);
+  e = launch_pdl(k_kv_join<T, DP, NT>, dim3((unsigned)grid, p.together * std::min(Sh::NQ, p.group)), DP, 0, s, c, a, p);
   return e != cudaSuccess ? e : launched();
 }
 template <class T> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cudaStream_t s) {
@@ -885,7 +908,9 @@ template <class T> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cud
 size_t kv_attention_workspace(int seqs, int q_heads, int heads, int dim, long long tokens) {
   (void)seqs;
   if (steps_of(dim, tokens) <= WHOLE_STEPS) return 0;
-  return GRID_MAX * (2 * 8 * (size_t)eights(dim, q_heads / heads) * (padded(dim) + 4) * 4 + 16);
+  const int group = q_heads / heads, queries = 8 * eights(dim, group), units = heads * ((group + queries - 1) / queries);
+  const size_t most = std::max({together(units, 8), together(units, 12), together(units, 16)});   // (by a block's warps)
+  return GRID_MAX * (most * 2 * queries * (padded(dim) + 4) * 4 + 16);
 }
 
 cudaError_t launch_kv_attention(DType dt, const KvCache& c, const KvAttnArgs& a, cudaStream_t s) {
