@@ -67,10 +67,21 @@ template <class E, int DP, int NT> struct Shape {
   static_assert(STAGE % 16 == 0 && PART % 4 == 0, "whole vectors");
 };
 
+// Division of numbers below 2^31 by one that the host knows: a product's upper half.
+struct Div {
+  unsigned m, s;
+  __host__ void by(unsigned d) {
+    for (s = 0; (1ull << s) < d; ++s) {}
+    m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+  }
+  __device__ __forceinline__ int of(unsigned n) const { return (int)((__umulhi(m, n) + n) >> s); }
+};
+
 struct Plan {
-  unsigned div_m, div_s;   // token / page_size
+  Div page, split_by, tiles_by, blocks_by, together_by, groups_by;   // page_size, split, ..., the grid
   int group, tiles;        // query heads of a key head, units that share them
-  int together, split;     // units that go together, warps to each of them
+  int together, split, groups;   // units that go together, warps to each of them, groups of a sequence
+  int join_queries, grid;  // queries to a block of the second kernel, blocks of the first
   int whole;               // blocks take whole units; 2: one each
   int pairs, vectors;      // results may be stored in pairs, queries loaded four at a time
   float scale;             // softmax scale times log2(e)
@@ -151,10 +162,13 @@ template <int T> __device__ __forceinline__ int steps_seen(const KvCache& c, int
   return (s.end - s.first + T - 1) / T;
 }
 
-// a / b for a >= 0, b > 0 (lines are mostly short enough for 32 bits, which divide in a fifth of the time)
-__device__ __noinline__ long long div64(long long a, long long b) { return a / b; }
+// a / b for a >= 0, b > 0
+__device__ __noinline__ long long quot64(long long a, long long b) { return a / b; }
 __device__ __forceinline__ long long quot(long long a, long long b) {
-  return (a | b) >> 32 ? div64(a, b) : (long long)((unsigned)a / (unsigned)b);
+  return (a | b) >> 31 ? quot64(a, b) : (int)((unsigned)a / (unsigned)b);
+}
+__device__ __forceinline__ long long quot(long long a, long long b, const Div& by) {
+  return a >> 31 ? quot64(a, b) : by.of((unsigned)a);
 }
 
 // The line, as every warp finds it on its own: a lane has a share of adjacent sequences.
@@ -185,7 +199,7 @@ template <int T> __device__ __noinline__ Spot locate(const KvCache& c, int windo
   for (int b = lo * line.per; b < c.seqs; ++b) {
     const int steps = steps_seen<T>(c, window, b);
     if (at < (long long)steps * groups) {
-      const int group = (int)quot(at, steps);
+      const int group = groups == 1 ? 0 : (int)quot(at, steps);
       return {b, group, (int)(at - (long long)group * steps), steps};
     }
     at -= (long long)steps * groups;
@@ -244,25 +258,25 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   pdl_wait();
 
   // This warp's steps of the line: w1 - w0 from `at` on, in a block's c0 .. c1.
-  const int sp = warp / p.together, u = warp - sp * p.together, groups = c.heads * p.tiles / p.together;
+  const int sp = p.together_by.of(warp), u = warp - sp * p.together, groups = p.groups;
   Spot at;
   long long w0, w1, c1 = 0, total = 1, blocks = 1;
   auto stretch = [&](long long c0, long long n) {
     // (rounded up: the first warp of a unit has steps where any has)
-    w0 = c0 + (sp < p.split ? quot(n * sp + p.split - 1, p.split) : n);
-    w1 = c0 + (sp < p.split ? quot(n * (sp + 1) + p.split - 1, p.split) : n);
+    w0 = c0 + (sp < p.split ? quot(n * sp + p.split - 1, p.split, p.split_by) : n);
+    w1 = c0 + (sp < p.split ? quot(n * (sp + 1) + p.split - 1, p.split, p.split_by) : n);
   };
   if (p.whole == 2) {   // a block to a unit
-    const int b = blockIdx.x / groups, steps = steps_seen<Sh::T>(c, a.window, b);
+    const int b = p.groups_by.of(blockIdx.x), steps = steps_seen<Sh::T>(c, a.window, b);
     stretch(0, steps);
     at = {b, (int)blockIdx.x - b * groups, (int)w0, steps};
   } else {
     const Line line = line_up<Sh::T>(c, a.window, groups);
     total = line.total;
     // blocks that have a share: with a step to every warp
-    blocks = p.whole ? gridDim.x : max(1ll, min((long long)gridDim.x, quot(total + p.split - 1, p.split)));
+    blocks = p.whole ? gridDim.x : max(1ll, min((long long)gridDim.x, quot(total + p.split - 1, p.split, p.split_by)));
     auto edge = [&](long long i) {   // of block i: its first step of the line
-      long long e = i >= blocks ? total : quot(total * i, blocks);
+      long long e = i >= blocks ? total : blocks == gridDim.x ? quot(total * i, blocks, p.blocks_by) : quot(total * i, blocks);
       if (p.whole && e < total) {
         const Spot s = locate<Sh::T>(c, a.window, groups, line, e);
         if (s.step) e += s.steps - s.step;
@@ -290,7 +304,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 
     // Page of this lane's token of the step at `in`, looked up one step before its copies.
     auto token = [&] { return in_seen.first + in.step * Sh::T + (lane & (Sh::T - 1)); };
-    auto page_of = [&](int t) { return (int)((__umulhi(p.div_m, (unsigned)t) + (unsigned)t) >> p.div_s); };
+    auto page_of = [&](int t) { return p.page.of((unsigned)t); };
     auto look_up = [&] {
       const int t = token();
       return t < in_seen.end ? c.table[in.b * c.ld_table + page_of(t)] : -1;
@@ -302,7 +316,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     const char *kb, *vb;   // of the unit's key head
     const float *ksb, *vsb;
     auto heads_of = [&](int unit) {
-      const int head = unit / p.tiles;
+      const int head = p.tiles_by.of(unit);
       kb = reinterpret_cast<const char*>(c.k) + head * c.k_stride[2];
       vb = reinterpret_cast<const char*>(c.v) + head * c.v_stride[2];
       ksb = c.k_scale + head * c.k_scale_stride[2];
@@ -374,7 +388,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     auto load_queries = [&] {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int head = at.unit / p.tiles, qi = (at.unit - head * p.tiles) * Sh::NQ + nt * 8 + g;
+        const int head = p.tiles_by.of(at.unit), qi = (at.unit - head * p.tiles) * Sh::NQ + nt * 8 + g;
         const T* q = reinterpret_cast<const T*>(a.q) + at.b * a.ldq + (long long)(head * p.group + qi) * dim;
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s) {
@@ -645,7 +659,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         continue;
       }
       // the unit, or this warp's part of it, is over
-      const int head = at.unit / p.tiles, tile = at.unit - head * p.tiles;
+      const int head = p.tiles_by.of(at.unit), tile = at.unit - head * p.tiles;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -715,8 +729,11 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   float* ws = reinterpret_cast<float*>(a.ws) + (long long)blockIdx.x * p.together * 2 * Sh::PART;
   int* meta = reinterpret_cast<int*>(reinterpret_cast<float*>(a.ws) + (long long)gridDim.x * p.together * 2 * Sh::PART) + 4 * blockIdx.x;
   int goes_on = 0;   // blocks behind this one that its last group goes on in, if it began here
-  for (int item = warp; item < p.together * queries; item += WARPS) {
+  // (units take turns where there are more warps than queries: the nth is of warps `turn` = n mod `turns`)
+  const int items = p.together * queries, turns = max(1, WARPS / items), turn = warp / items;
+  for (int item = turns > 1 ? warp - turn * items : warp; item < items && turn < turns * (turns > 1 ? 1 : WARPS); item += turns > 1 ? items : WARPS) {
     const int place = item / queries, q = item - place * queries;
+    int nth = 0;
     auto of_warp = [&](int r) { return (r >> 1) * p.together + place; };
     auto part = [&](int r) {
       return r & 1 ? reinterpret_cast<const float*>(smem + of_warp(r) * Sh::RING)
@@ -730,13 +747,13 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       const unsigned all = __ballot_sync(0xffffffffu, mine);
       left &= ~all;
       const bool here = r0 & 1, ends = __ballot_sync(0xffffffffu, mine && (of.y & 1));
-      if (item == 0 && here && !ends && !p.whole) {
+      if (warp == 0 && item == 0 && here && !ends && !p.whole) {
         // the block that has the group's last step: the last k with total * k / blocks < the steps up to it
         goes_on = (int)(quot(part_upto[of_warp(r0)] * blocks + total - 1, total) - 1 - blockIdx.x);
         if (lane == 0) meta[0] = b, meta[1] = unit;
       }
-      const int head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
-      if (qi >= p.group) continue;
+      const int head = p.tiles_by.of(unit), qi = (unit - head * p.tiles) * Sh::NQ + q;
+      if (qi >= p.group || (turns > 1 && nth++ % turns != turn)) continue;
       const float4 v = mine ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
       float m = v.x, mw = v.z;
 #pragma unroll
@@ -780,50 +797,97 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
   if (!p.whole && threadIdx.x == 0) meta[2] = goes_on;
 }
 
-// Units of several blocks: block (i, y) joins a query of a unit of the group that block i of the first
-// kernel began, over the parts in the line's order, four at a time side by side.
+// Units of several blocks: block (x, y) joins some queries of a unit of the y-th group that goes over
+// several blocks (no more than there are groups), over the parts in the line's order: their maxima and factors first, then a thread has
+// four columns of a query over every `lanes`-th part.
+constexpr int JOIN = 512;
 template <class T, int DP, int NT>
-__global__ void __launch_bounds__(DP) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
-                                                const __grid_constant__ Plan p) {
+__global__ void __launch_bounds__(JOIN) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
+                                                  const __grid_constant__ Plan p) {
   typedef Shape<T, DP, NT> Sh;
-  __shared__ float4 sums[4][DP / 4];
-  __shared__ float st[4][3];
-  const int queries = min(Sh::NQ, p.group), place = blockIdx.y / queries, q = blockIdx.y - place * queries;
-  const int i = blockIdx.x, k0 = threadIdx.x / (DP / 4), d4 = threadIdx.x % (DP / 4);
+  __shared__ float by[Sh::NQ][GRID_MAX], stat[Sh::NQ][3];   // factors; m, l, mw
+  __shared__ float4 sums[JOIN];
+  const int chunks = (min(Sh::NQ, p.group) + p.join_queries - 1) / p.join_queries;
+  const int place = blockIdx.x / chunks, q0 = (blockIdx.x - place * chunks) * p.join_queries;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_trigger();
   pdl_wait();
   const float* ws = reinterpret_cast<const float*>(a.ws);
-  const int* meta = reinterpret_cast<const int*>(ws + (long long)gridDim.x * p.together * 2 * Sh::PART) + 4 * i;
-  const int n = meta[2];
-  if (n == 0) return;
-  const int b = meta[0], unit = meta[1] + place, head = unit / p.tiles, qi = (unit - head * p.tiles) * Sh::NQ + q;
-  if (qi >= p.group) return;
-  float4 sum = make_float4(0, 0, 0, 0);
-  float m = NONE, mw = NONE, l = 0.f;
-  auto add = [&](float4 v, float vm, float vl, float vmw) {
-    const float mn = fmaxf(m, vm), mwn = fmaxf(mw, vmw), f = ex2(mw - mwn), fk = ex2(vmw - mwn);
-    l = l * ex2(m - mn) + vl * ex2(vm - mn);
-    sum = make_float4(sum.x * f + v.x * fk, sum.y * f + v.y * fk, sum.z * f + v.z * fk, sum.w * f + v.w * fk);
-    m = mn;
-    mw = mwn;
-  };
-#pragma unroll 4
-  for (int k = k0; k <= n; k += 4) {
-    const float* part = ws + (2ll * ((i + k) * p.together + place) + (k ? 0 : 1)) * Sh::PART;
-    const float4 s = *reinterpret_cast<const float4*>(part + Sh::NQ * DP + 4 * q);
-    add(*reinterpret_cast<const float4*>(part + q * DP + 4 * d4), s.x, s.y, s.z);
+  const int* metas = reinterpret_cast<const int*>(ws + (long long)p.grid * p.together * 2 * Sh::PART);
+  // the block that began it: the y-th one that says so
+  int opens[GRID_MAX / 32], i = -1;
+#pragma unroll
+  for (int e = 0; e < GRID_MAX / 32; ++e) opens[e] = lane + 32 * e < p.grid ? metas[4 * (lane + 32 * e) + 2] : 0;
+  int left = blockIdx.y;
+#pragma unroll
+  for (int e = 0; e < GRID_MAX / 32; ++e) {
+    unsigned some = __ballot_sync(0xffffffffu, opens[e] > 0);
+    const int n = __popc(some);
+    if (i < 0 && left < n) {
+      for (; left; --left) some &= some - 1;
+      i = 32 * e + __ffs(some) - 1;
+    }
+    left -= n;
   }
-  sums[k0][d4] = sum;
-  if (d4 == 0) st[k0][0] = m, st[k0][1] = l, st[k0][2] = mw;
+  if (i < 0) return;
+  const int* meta = metas + 4 * i;
+  const int n = meta[2] + 1;
+  const int b = meta[0], unit = meta[1] + place, head = p.tiles_by.of(unit), first = (unit - head * p.tiles) * Sh::NQ;
+  const int queries = min(min(Sh::NQ, p.group - first) - q0, p.join_queries);
+  if (queries <= 0) return;
+  auto part = [&](int k) { return ws + (2ll * ((i + k) * p.together + place) + (k ? 0 : 1)) * Sh::PART; };
+  for (int q = warp; q < queries; q += JOIN / 32) {   // a warp to a query
+    float4 v[GRID_MAX / 32];   // (all of them under way at once)
+    float m = NONE, mw = NONE, l = 0.f;
+#pragma unroll
+    for (int e = 0; e < GRID_MAX / 32; ++e) {
+      v[e] = make_float4(NONE, 0.f, NONE, 0.f);
+      if (lane + 32 * e < n) v[e] = *reinterpret_cast<const float4*>(part(lane + 32 * e) + Sh::NQ * DP + 4 * (q0 + q));
+    }
+#pragma unroll
+    for (int e = 0; e < GRID_MAX / 32; ++e) {
+      m = fmaxf(m, v[e].x);
+      mw = fmaxf(mw, v[e].z);
+    }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+      mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, k));
+    }
+#pragma unroll
+    for (int e = 0; e < GRID_MAX / 32; ++e) {
+      if (lane + 32 * e < n) by[q][lane + 32 * e] = ex2(v[e].z - mw);
+      l += v[e].y * ex2(v[e].x - m);
+    }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+    if (lane == 0) stat[q][0] = m, stat[q][1] = l, stat[q][2] = mw;
+  }
+  __syncthreads();
+  const int width = queries * (DP / 4), lanes = JOIN / width, x = tid % width, k0 = tid / width;
+  const int q = x / (DP / 4), d = 4 * (x - q * (DP / 4));
+  float4 sum = make_float4(0, 0, 0, 0);
+  if (k0 < lanes) {
+#pragma unroll 5
+    for (int k = k0; k < n; k += lanes) {
+      const float4 v = *reinterpret_cast<const float4*>(part(k) + (q0 + q) * DP + d);
+      const float w = by[q][k];
+      sum = make_float4(fmaf(v.x, w, sum.x), fmaf(v.y, w, sum.y), fmaf(v.z, w, sum.z), fmaf(v.w, w, sum.w));
+    }
+    sums[tid] = sum;
+  }
   __syncthreads();
   if (k0) return;
-  for (int k = 1; k < 4; ++k) add(sums[k][d4], st[k][0], st[k][1], st[k][2]);
-  const int qh = head * p.group + qi;
+  for (int k = 1; k < lanes; ++k) {
+    const float4 v = sums[k * width + x];
+    sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+  }
+  const int qh = head * p.group + first + q0 + q;
   T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * c.head_dim;
-  const float f = closing(m, l, mw);
-  store_row(out, p.pairs, 4 * d4, c.head_dim, sum.x * f, sum.y * f);
-  store_row(out, p.pairs, 4 * d4 + 2, c.head_dim, sum.z * f, sum.w * f);
-  if (a.lse && d4 == 0) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
+  const float f = closing(stat[q][0], stat[q][1], stat[q][2]);
+  store_row(out, p.pairs, d, c.head_dim, sum.x * f, sum.y * f);
+  store_row(out, p.pairs, d + 2, c.head_dim, sum.z * f, sum.w * f);
+  if (a.lse && d == 0) a.lse[(long long)b * a.q_heads + qh] = lse_of(stat[q][0], stat[q][1]);
 }
 
 int padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
@@ -862,10 +926,10 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   });
   if (e != cudaSuccess) return e;
   Plan p = {};
-  while ((1ll << p.div_s) < c.page_size) ++p.div_s;
-  p.div_m = (unsigned)(((1ull << 32) * ((1ull << p.div_s) - c.page_size)) / c.page_size + 1);
+  p.page.by(c.page_size);
   p.group = a.q_heads / c.heads;
   p.tiles = (p.group + Sh::NQ - 1) / Sh::NQ;
+  p.tiles_by.by(p.tiles);
   const int es = sizeof(T);
   p.pairs = !((uintptr_t)a.out & (2 * es - 1)) && a.ldo % 2 == 0;
   p.vectors = !((uintptr_t)a.q & (4 * es - 1)) && a.ldq % 4 == 0;
@@ -884,14 +948,28 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   p.whole = steps > WHOLE_STEPS ? 0 : units > n_sms ? 1 : 2;
   p.together = p.whole ? 1 : together(c.heads * p.tiles, Sh::WARPS);
   p.split = Sh::WARPS / p.together;
+  p.split_by.by(p.split);
+  p.together_by.by(p.together);
+  p.groups = c.heads * p.tiles / p.together;
+  p.groups_by.by(p.groups);
   // blocks: one to an SM; fewer where there are not two steps to a warp, and one to a unit where blocks take whole ones
   long long grid = std::min(n_sms, GRID_MAX);
   grid = p.whole == 2 ? units : std::min(grid, p.whole ? units : (units / p.together * steps + 2 * p.split - 1) / (2 * p.split));
+  p.blocks_by.by((unsigned)grid);
+  p.grid = (int)grid;
+  // queries to a block of the second kernel: all of them where a unit has a few parts, fewer where
+  // a few sequences have all blocks, so that at most four parts follow one another
+  const int queries = std::min(Sh::NQ, p.group);
+  const long long parts = grid / ((long long)c.seqs * p.groups);
+  p.join_queries = queries;
+  while (p.join_queries > 1 && 4 * (JOIN / (p.join_queries * (DP / 4))) < parts) --p.join_queries;
   e = launch_pdl(k_kv_attention<T, DP, NT>, (unsigned)grid, 32 * Sh::WARPS, Sh::SMEM, s, c, a, p);
   if (e != cudaSuccess) return e;
   e = launched();
   if (e != cudaSuccess || p.whole) return e;
-  e = launch_pdl(k_kv_join<T, DP, NT>, dim3((unsigned)grid, p.together * std::min(Sh::NQ, p.group)), DP, 0, s, c, a, p);
+  e = launch_pdl(k_kv_join<T, DP, NT>, dim3(p.together * ((queries + p.join_queries - 1) / p.join_queries),
+                                             (unsigned)std::min(grid, (long long)c.seqs * p.groups)),
+                 JOIN, 0, s, c, a, p);
   return e != cudaSuccess ? e : launched();
 }
 template <class T> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cudaStream_t s) {
