@@ -10,21 +10,34 @@ namespace ff {
 namespace {
 
 // Eight elements of a head, the share of one lane: in 16-byte vectors, or one by one
-// where rows start off them.
-template <class T, bool VEC> __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-  if constexpr (!VEC) {
+// where rows start off them.  As they are in memory, so that loads wait for nothing.
+template <class T, bool VEC> struct Eight {
+  T r[8];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f(p[i]);
-  } else if constexpr (sizeof(T) == 2) {
-    ld16(p, v);
-  } else {
-    float a[4], b[4];
-    ld16(p, a);
-    ld16(p + 4, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
+    for (int i = 0; i < 8; ++i) r[i] = p[i];
   }
-}
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f(r[i]);
+  }
+};
+template <class T> struct Eight<T, true> {
+  uint4 r[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      unpack16(r[0], v);
+    } else {
+      const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+    }
+  }
+};
 template <class T, bool VEC> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   if constexpr (!VEC) {
 #pragma unroll
@@ -38,62 +51,79 @@ template <class T, bool VEC> __device__ __forceinline__ void store8(T* p, const 
   }
 }
 
-// Sequence and token of a row of the call; false where the row has none.
-struct Token {
-  int b, t;
+// Where a row's token lies: page (-1: nowhere) and slot; of_none: the row is of no sequence.
+struct Place {
+  int page, slot;
+  bool of_none;
 };
-__device__ __forceinline__ bool token_of(const KvCache& c, const int* row_start, long long row, Token* o) {
-  if (!row_start) {
-    *o = {(int)row, kv_len(c, (int)row) - 1};
-    return true;
+__device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start, long long row, const Div& page_size) {
+  int b = (int)row, back = 1;   // rows from this one to the sequence's last
+  if (row_start) {
+    // the last sequence that starts at or before the row (empty ones end where they start)
+    int lo = 0, hi = c.seqs;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (row_start[mid] <= row) lo = mid + 1;
+      else hi = mid;
+    }
+    b = lo - 1;
+    const int end = b < 0 ? 0 : row_start[b + 1];
+    if (row >= end) return {-1, 0, true};
+    back = end - (int)row;
   }
-  // the last sequence that starts at or before the row (empty ones end where they start)
-  int lo = 0, hi = c.seqs;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (row_start[mid] <= row) lo = mid + 1;
-    else hi = mid;
-  }
-  const int b = lo - 1;
-  if (b < 0) return false;
-  const int end = row_start[b + 1];
-  if (row >= end) return false;
-  *o = {b, (int)(kv_len(c, b) - (end - row))};
-  return true;
+  const int t = kv_len(c, b) - back;
+  if (t < 0) return {-1, 0, false};
+  const int n = page_size.of((unsigned)t), page = c.table[b * c.ld_table + n];
+  return {(unsigned)page < (unsigned)c.pages ? page : -1, t - n * c.page_size, false};
 }
 
-// L lanes to a head of one row.
-template <class T, bool VEC, int L>
-__global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r) {
+// L lanes to a head of a row, U such heads to a lane, all loads of which are under way before the
+// first is used.  Bound by memory.
+template <class T, bool VEC, int L, int U>
+__global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
+                                                  const Div heads, const Div page_size) {
+  constexpr int G = 256 / L;
   const int lane = threadIdx.x % L, col = 8 * lane;
-  const long long item = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const long long row = item / c.heads;
-  const int head = (int)(item - row * c.heads);
   pdl_trigger();
   pdl_wait();
-  Token tk;
-  int page = -1;
-  if (row < r.rows && token_of(c, r.row_start, row, &tk) && tk.t >= 0) page = kv_page(c, tk.b, tk.t);
-  const int slot = page < 0 ? 0 : tk.t % c.page_size;
+  Eight<T, VEC> x[U][2];
+  int head[U];
+  long long row[U];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (page >= 0 && col < c.head_dim)
-      load8<T, VEC>(reinterpret_cast<const T*>(kv ? r.v : r.k) + row * (kv ? r.ldv : r.ldk) + (long long)head * c.head_dim + col, x);
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_abs(m, x[i]);
-#pragma unroll
-    for (int o = L / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (page < 0 || col >= c.head_dim) continue;
-    const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
-    const long long* st = kv ? c.v_stride : c.k_stride;
-    uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + page * st[0] + slot * st[1] + head * st[2] + col;
-    *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
-                                              to_e4m3x4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
-    const long long* ss = kv ? c.v_scale_stride : c.k_scale_stride;
-    if (lane == 0) (kv ? c.v_scale : c.k_scale)[page * ss[0] + slot * ss[1] + head * ss[2]] = s;
+  for (int u = 0; u < U; ++u) {
+    const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
+    row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
+    head[u] = (int)(item - row[u] * c.heads);
+    const bool in = row[u] < r.rows && col < c.head_dim;
+    const long long at = (long long)head[u] * c.head_dim + col;
+    if (in) {
+      x[u][0].load(reinterpret_cast<const T*>(r.k) + row[u] * r.ldk + at);
+      x[u][1].load(reinterpret_cast<const T*>(r.v) + row[u] * r.ldv + at);
+    }
   }
+  Place p[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) p[u] = row[u] < r.rows ? place_of(c, r.row_start, row[u], page_size) : Place{-1, 0, true};
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const bool in = row[u] < r.rows && col < c.head_dim;
+      float v[8], m = 0.f;
+      x[u][kv].get(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max_abs(m, in ? v[i] : 0.f);
+#pragma unroll
+      for (int o = L / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if (p[u].page < 0 || col >= c.head_dim) continue;
+      const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
+      const long long* st = kv ? c.v_stride : c.k_stride;
+      uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + p[u].page * st[0] + p[u].slot * st[1] + head[u] * st[2] + col;
+      *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                                                to_e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+      const long long* ss = kv ? c.v_scale_stride : c.k_scale_stride;
+      if (lane == 0) (kv ? c.v_scale : c.k_scale)[p[u].page * ss[0] + p[u].slot * ss[1] + head[u] * ss[2]] = s;
+    }
 }
 
 // four e4m3 bytes as floats
@@ -104,42 +134,69 @@ __device__ __forceinline__ void from_e4m3x4(uint32_t u, float* v) {
   v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
 }
 
-template <class T, bool VEC, int L>
-__global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r) {
+template <class T, bool VEC, int L, int U>
+__global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
+                                                 const Div heads, const Div page_size) {
+  constexpr int G = 256 / L;
   const int lane = threadIdx.x % L, col = 8 * lane;
-  const long long item = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const long long row = item / c.heads;
-  const int head = (int)(item - row * c.heads);
   pdl_trigger();
   pdl_wait();
-  Token tk;
-  if (row >= r.rows || col >= c.head_dim || !token_of(c, r.row_start, row, &tk)) return;
-  const int page = tk.t < 0 ? -1 : kv_page(c, tk.b, tk.t);
-  const int slot = page < 0 ? 0 : tk.t % c.page_size;
+  if (col >= c.head_dim) return;
+  Place p[U];
+  int head[U];
+  long long row[U];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (page >= 0) {
+  for (int u = 0; u < U; ++u) {
+    const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
+    row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
+    head[u] = (int)(item - row[u] * c.heads);
+    p[u] = row[u] < r.rows ? place_of(c, r.row_start, row[u], page_size) : Place{-1, 0, true};
+  }
+  uint2 q[U][2];
+  float s[U][2];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      q[u][kv] = make_uint2(0, 0);
+      s[u][kv] = 0.f;
+      if (p[u].page < 0) continue;
       const long long* st = kv ? c.v_stride : c.k_stride;
-      const uint8_t* q = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + page * st[0] + slot * st[1] + head * st[2] + col;
+      q[u][kv] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + p[u].page * st[0] +
+                                                 p[u].slot * st[1] + head[u] * st[2] + col);
       const long long* ss = kv ? c.v_scale_stride : c.k_scale_stride;
-      const float s = kv_scale((kv ? c.v_scale : c.k_scale)[page * ss[0] + slot * ss[1] + head * ss[2]]);
-      const uint2 u = *reinterpret_cast<const uint2*>(q);
-      from_e4m3x4(u.x, x);
-      from_e4m3x4(u.y, x + 4);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= s;
+      s[u][kv] = (kv ? c.v_scale : c.k_scale)[p[u].page * ss[0] + p[u].slot * ss[1] + head[u] * ss[2]];
     }
-    store8<T, VEC>(reinterpret_cast<T*>(kv ? r.v : r.k) + row * (kv ? r.ldv : r.ldk) + (long long)head * c.head_dim + col, x);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (p[u].of_none) continue;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[8];
+      from_e4m3x4(q[u][kv].x, x);
+      from_e4m3x4(q[u][kv].y, x + 4);
+      const float f = kv_scale(s[u][kv]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= f;
+      store8<T, VEC>(reinterpret_cast<T*>(kv ? r.v : r.k) + row[u] * (kv ? r.ldv : r.ldk) + (long long)head[u] * c.head_dim + col, x);
+    }
   }
 }
 
-template <class T, bool VEC, bool WRITE, int L> cudaError_t kv_rows_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  const long long grid = (r.rows * c.heads + 256 / L - 1) / (256 / L);
+template <class T, bool VEC, bool WRITE, int L, int U> cudaError_t kv_rows_u(const KvCache& c, const KvRows& r, cudaStream_t s) {
+  const long long per = 256 / L * U, grid = (r.rows * c.heads + per - 1) / per;
   if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  const cudaError_t e = WRITE ? launch_pdl(k_kv_write<T, VEC, L>, (unsigned)grid, 256, 0, s, c, r)
-                              : launch_pdl(k_kv_read<T, VEC, L>, (unsigned)grid, 256, 0, s, c, r);
+  Div heads, page_size;
+  heads.by(c.heads);
+  page_size.by(c.page_size);
+  const cudaError_t e = WRITE ? launch_pdl(k_kv_write<T, VEC, L, U>, (unsigned)grid, 256, 0, s, c, r, heads, page_size)
+                              : launch_pdl(k_kv_read<T, VEC, L, U>, (unsigned)grid, 256, 0, s, c, r, heads, page_size);
   return e != cudaSuccess ? e : launched();
+}
+template <class T, bool VEC, bool WRITE, int L> cudaError_t kv_rows_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
+  // several heads to a lane where two blocks of them for every SM remain
+  constexpr int U = WRITE && sizeof(T) == 4 ? 2 : 4;
+  return r.rows * c.heads >= 152ll * 2 * U * (256 / L) ? kv_rows_u<T, VEC, WRITE, L, U>(c, r, s) : kv_rows_u<T, VEC, WRITE, L, 1>(c, r, s);
 }
 template <class T, bool VEC, bool WRITE> cudaError_t kv_rows_v(const KvCache& c, const KvRows& r, cudaStream_t s) {
   return c.head_dim <= 64 ? kv_rows_l<T, VEC, WRITE, 8>(c, r, s)

@@ -53,16 +53,20 @@ struct BlockNormsArgs {
 };
 cudaError_t launch_block_norms(DType dt, long long rows, int C, const BlockNormsArgs& a, cudaStream_t s);
 
+// Division of numbers below 2^31 by one that the host knows: a product's upper half.
+struct Div {
+  unsigned m, s;
+  void by(unsigned d) {
+    for (s = 0; (1ull << s) < d; ++s) {}
+    m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+  }
+  __device__ __forceinline__ int of(unsigned n) const { return (int)((__umulhi(m, n) + n) >> s); }
+};
+
 // Tokens of sequence b: what the table can hold at most.
 __device__ __forceinline__ int kv_len(const KvCache& c, int b) {
   const long long most = (long long)c.table_pages * c.page_size;
   return (int)max(0ll, min((long long)c.lens[b], most));
-}
-
-// Page of token t of sequence b, -1 where there is none.  t lies in the table.
-__device__ __forceinline__ int kv_page(const KvCache& c, int b, int t) {
-  const int p = c.table[b * c.ld_table + t / c.page_size];
-  return (unsigned)p < (unsigned)c.pages ? p : -1;
 }
 
 // What a scale stands for: infinities are NaN (featfix_ops.h).

@@ -67,16 +67,6 @@ template <class E, int DP, int NT> struct Shape {
   static_assert(STAGE % 16 == 0 && PART % 4 == 0, "whole vectors");
 };
 
-// Division of numbers below 2^31 by one that the host knows: a product's upper half.
-struct Div {
-  unsigned m, s;
-  __host__ void by(unsigned d) {
-    for (s = 0; (1ull << s) < d; ++s) {}
-    m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
-  }
-  __device__ __forceinline__ int of(unsigned n) const { return (int)((__umulhi(m, n) + n) >> s); }
-};
-
 struct Plan {
   Div page, split_by, tiles_by, blocks_by, together_by, groups_by;   // page_size, split, ..., the grid
   int group, tiles;        // query heads of a key head, units that share them
