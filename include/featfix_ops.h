@@ -227,8 +227,8 @@ FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_d
  * k, v are e4m3 bytes; place (page, slot, head) starts stride[0] * page +
  * stride[1] * slot + stride[2] * head bytes behind the pointer (multiples of 16, at
  * least head_dim; pointers are 16-byte aligned), its scale that many floats behind
- * k_scale / v_scale (at least 1): heads inside or outside of a page's tokens, with or
- * without gaps.  head_dim is a multiple of 8, at most 256.
+ * k_scale / v_scale (at least 1), strides below 2^32: heads inside or outside of a
+ * page's tokens, with or without gaps.  head_dim is a multiple of 8, at most 256.
  *
  * Token t of sequence b is in page table[b * ld_table + t / page_size] (t <
  * table_pages * page_size, at most 2^31 - 256), slot t % page_size, for t < lens[b]; lens count the
@@ -283,7 +283,9 @@ FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int 
  * apart where dtype is f32 and as one where it is bf16, probabilities the same: relative
  * errors of 2^-22 and 2^-11, below dtype's own rounding.  The workspace (16-byte aligned) may
  * hold anything; calls that may run at the same time need one each.  The same inputs
- * give the same bits.                                                         */
+ * give the same bits.  The largest power of two that divides the page's and the slot's stride
+ * times 2^32 must pass the last place's offset (FEATFIX_ERR_UNSUPPORTED: pools from 64 GB on,
+ * of places 16 bytes off any rounder stride).                                 */
 FEATFIX_API featfix_status featfix_op_kv_attention(int dtype, const featfix_kv_cache* cache, const void* dev_q,
                                        long long ld_q, int q_heads, float scale, int window, void* dev_out,
                                        long long ld_out, float* dev_lse, void* dev_workspace, size_t ws_bytes,

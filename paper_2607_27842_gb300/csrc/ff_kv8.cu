@@ -17,7 +17,11 @@ template <class T, bool VEC> struct Eight {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = p[i];
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = from_f<T>(0.f);
+  }
+  __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_f(r[i]);
   }
@@ -28,9 +32,16 @@ template <class T> struct Eight<T, true> {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = reinterpret_cast<const uint4*>(p)[i];
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void get(float* v) const {
     if constexpr (sizeof(T) == 2) {
-      unpack16(r[0], v);
+      float u[8];
+      unpack16(r[0], u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = u[i];
     } else {
       const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
 #pragma unroll
@@ -77,16 +88,43 @@ __device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start
   return {(unsigned)page < (unsigned)c.pages ? page : -1, t - n * c.page_size, false};
 }
 
-// L lanes to a head of a row, U such heads to a lane, all loads of which are under way before the
-// first is used.  Bound by memory.
+// Where a place starts (strides are below 2^32: products of 32 bits).
+__device__ __forceinline__ unsigned long long place_at(const long long (&st)[3], const Place& p, int head) {
+  return (unsigned long long)(unsigned)p.page * (unsigned)st[0] + (unsigned long long)(unsigned)p.slot * (unsigned)st[1] +
+         (unsigned long long)(unsigned)head * (unsigned)st[2];
+}
+
+// Largest magnitude of a lane's sixteen elements: bf16 in pairs, as they are in memory.
+template <class T, bool VEC> __device__ __forceinline__ float amax16(const Eight<T, VEC> (&e)[2], const float (&v)[16]) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w[4] = {e[i].r[0].x, e[i].r[0].y, e[i].r[0].z, e[i].r[0].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[k]));
+    }
+    return max_abs(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  } else {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max_abs(m, v[i]);
+    return m;
+  }
+}
+
+// L lanes to a head of a row, sixteen columns to a lane, U such heads to a lane, all loads of which are
+// under way before the first is used.  Bound by instruction issue before it was by memory: hence sixteen
+// columns (eight: 14566 x 16 heads of 128 in bf16 49 us, half of its instructions addresses and the
+// maximum's exchange) and 32-bit strides.
 template <class T, bool VEC, int L, int U>
 __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
                                                   const Div heads, const Div page_size) {
   constexpr int G = 256 / L;
-  const int lane = threadIdx.x % L, col = 8 * lane;
+  const int lane = threadIdx.x % L, col = 16 * lane, n = min(2, max(0, c.head_dim - col) / 8);   // eights of this lane
   pdl_trigger();
   pdl_wait();
-  Eight<T, VEC> x[U][2];
+  Eight<T, VEC> x[U][2][2];
   int head[U];
   long long row[U];
 #pragma unroll
@@ -94,11 +132,15 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
     const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
     row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
     head[u] = (int)(item - row[u] * c.heads);
-    const bool in = row[u] < r.rows && col < c.head_dim;
-    const long long at = (long long)head[u] * c.head_dim + col;
-    if (in) {
-      x[u][0].load(reinterpret_cast<const T*>(r.k) + row[u] * r.ldk + at);
-      x[u][1].load(reinterpret_cast<const T*>(r.v) + row[u] * r.ldv + at);
+    const int at = head[u] * c.head_dim + col;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x[u][0][i].zero();
+      x[u][1][i].zero();
+      if (row[u] < r.rows && i < n) {
+        x[u][0][i].load(reinterpret_cast<const T*>(r.k) + row[u] * r.ldk + at + 8 * i);
+        x[u][1][i].load(reinterpret_cast<const T*>(r.v) + row[u] * r.ldv + at + 8 * i);
+      }
     }
   }
   Place p[U];
@@ -108,21 +150,25 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-      const bool in = row[u] < r.rows && col < c.head_dim;
-      float v[8], m = 0.f;
-      x[u][kv].get(v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max_abs(m, in ? v[i] : 0.f);
+      float v[16];
+      x[u][kv][0].get(v);
+      x[u][kv][1].get(v + 8);
+      float m = amax16<T, VEC>(x[u][kv], v);
 #pragma unroll
       for (int o = L / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (p[u].page < 0 || col >= c.head_dim) continue;
+      if (p[u].page < 0 || n == 0) continue;
       const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
-      const long long* st = kv ? c.v_stride : c.k_stride;
-      uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + p[u].page * st[0] + p[u].slot * st[1] + head[u] * st[2] + col;
-      *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                                                to_e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
-      const long long* ss = kv ? c.v_scale_stride : c.k_scale_stride;
-      if (lane == 0) (kv ? c.v_scale : c.k_scale)[p[u].page * ss[0] + p[u].slot * ss[1] + head[u] * ss[2]] = s;
+      uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col;
+      const f32x2 i2 = f2u(inv, inv);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 a = fmul2(f2u(v[4 * i], v[4 * i + 1]), i2), b = fmul2(f2u(v[4 * i + 2], v[4 * i + 3]), i2);
+        w[i] = to_e4m3x4(lo_f(a), hi_f(a), lo_f(b), hi_f(b));
+      }
+      if (n == 2) *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+      else *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+      if (lane == 0) (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p[u], head[u])] = s;
     }
 }
 
@@ -161,11 +207,9 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache
       q[u][kv] = make_uint2(0, 0);
       s[u][kv] = 0.f;
       if (p[u].page < 0) continue;
-      const long long* st = kv ? c.v_stride : c.k_stride;
-      q[u][kv] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + p[u].page * st[0] +
-                                                 p[u].slot * st[1] + head[u] * st[2] + col);
-      const long long* ss = kv ? c.v_scale_stride : c.k_scale_stride;
-      s[u][kv] = (kv ? c.v_scale : c.k_scale)[p[u].page * ss[0] + p[u].slot * ss[1] + head[u] * ss[2]];
+      q[u][kv] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) +
+                                                 place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col);
+      s[u][kv] = (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p[u], head[u])];
     }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -195,12 +239,14 @@ template <class T, bool VEC, bool WRITE, int L, int U> cudaError_t kv_rows_u(con
 }
 template <class T, bool VEC, bool WRITE, int L> cudaError_t kv_rows_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
   // several heads to a lane where two blocks of them for every SM remain
-  constexpr int U = WRITE && sizeof(T) == 4 ? 2 : 4;
-  return r.rows * c.heads >= 152ll * 2 * U * (256 / L) ? kv_rows_u<T, VEC, WRITE, L, U>(c, r, s) : kv_rows_u<T, VEC, WRITE, L, 1>(c, r, s);
+  constexpr int U = !WRITE ? 4 : sizeof(T) == 2 ? 2 : 1;
+  if (U > 1 && r.rows * c.heads >= 152ll * 2 * U * (256 / L)) return kv_rows_u<T, VEC, WRITE, L, U>(c, r, s);
+  return kv_rows_u<T, VEC, WRITE, L, 1>(c, r, s);
 }
 template <class T, bool VEC, bool WRITE> cudaError_t kv_rows_v(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  return c.head_dim <= 64 ? kv_rows_l<T, VEC, WRITE, 8>(c, r, s)
-         : c.head_dim <= 128 ? kv_rows_l<T, VEC, WRITE, 16>(c, r, s) : kv_rows_l<T, VEC, WRITE, 32>(c, r, s);
+  constexpr int L = WRITE ? 4 : 8;   // lanes to 64 columns
+  return c.head_dim <= 64 ? kv_rows_l<T, VEC, WRITE, L>(c, r, s)
+         : c.head_dim <= 128 ? kv_rows_l<T, VEC, WRITE, 2 * L>(c, r, s) : kv_rows_l<T, VEC, WRITE, 4 * L>(c, r, s);
 }
 template <class T, bool WRITE> cudaError_t kv_rows(const KvCache& c, const KvRows& r, cudaStream_t s) {
   const auto al = [](const void* p, long long ld) { return !((uintptr_t)p & 15) && ld % (16 / (int)sizeof(T)) == 0; };

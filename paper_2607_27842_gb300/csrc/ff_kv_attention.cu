@@ -925,12 +925,10 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   p.vectors = !((uintptr_t)a.q & (4 * es - 1)) && a.ldq % 4 == 0;
   p.scale = a.scale * 1.4426950408889634f;
   if (!units_of(c, c.k_stride, p.k_unit, &p.k_bytes) || !units_of(c, c.v_stride, p.v_unit, &p.v_bytes)) return cudaErrorNotSupported;
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2; ++i) {   // (strides of one page or slot say nothing)
     const bool one = (i ? c.page_size : c.pages) == 1;
-    const long long ks = one ? 0 : c.k_scale_stride[i], vs = one ? 0 : c.v_scale_stride[i];
-    if (ks > 0xffffffffll || vs > 0xffffffffll) return cudaErrorNotSupported;
-    p.ks[i] = (unsigned)ks;
-    p.vs[i] = (unsigned)vs;
+    p.ks[i] = one ? 0 : (unsigned)c.k_scale_stride[i];
+    p.vs[i] = one ? 0 : (unsigned)c.v_scale_stride[i];
   }
   long long tokens = (long long)c.table_pages * c.page_size;
   if (a.window) tokens = std::min(tokens, (long long)a.window);

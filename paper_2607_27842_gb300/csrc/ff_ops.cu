@@ -39,7 +39,7 @@ constexpr int PAGE_MAX = 1 << 24;
 bool strides_ok(const featfix_kv_cache& c, const long long (&st)[3], long long width, int unit) {
   const int n[3] = {c.pages, c.page_size, c.heads};
   for (int i = 0; i < 3; ++i)
-    if (n[i] > 1 && (st[i] < width || st[i] % unit || st[i] > (1ll << 46) / n[i])) return false;
+    if (n[i] > 1 && (st[i] < width || st[i] % unit || st[i] > 0xffffffffll)) return false;
   return true;
 }
 bool cache_ok(const featfix_kv_cache* c) {
