@@ -49,16 +49,13 @@ template <class T> struct Eight<T, true> {
     }
   }
 };
-template <class T, bool VEC> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
-  if constexpr (!VEC) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = from_f<T>(v[i]);
-  } else if constexpr (sizeof(T) == 2) {
+// As many elements as 16 bytes hold, in a vector or one by one.
+template <class T, bool VEC> __device__ __forceinline__ void store_vec(T* p, const float (&v)[VecN<T>::n]) {
+  if constexpr (VEC) {
     st16(p, v);
   } else {
-    const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-    st16(p, a);
-    st16(p + 4, b);
+#pragma unroll
+    for (int i = 0; i < VecN<T>::n; ++i) p[i] = from_f<T>(v[i]);
   }
 }
 
@@ -67,22 +64,40 @@ struct Place {
   int page, slot;
   bool of_none;
 };
-__device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start, long long row, const Div& page_size) {
+// First rows and lengths of the sequences, by a block in shared memory where there are not too many: one
+// wait for memory instead of one for every halving of the search and one for the length (8000 rows of 19
+// sequences 8.4 -> 6 us).
+constexpr int SEQS_HELD = 512;
+struct Sequences {
+  int start[SEQS_HELD + 1], len[SEQS_HELD];
+};
+__device__ __forceinline__ bool hold(const KvCache& c, const int* row_start, Sequences& q) {
+  if (!row_start || c.seqs > SEQS_HELD) return false;
+  for (int i = threadIdx.x; i <= c.seqs; i += blockDim.x) {
+    q.start[i] = row_start[i];
+    if (i < c.seqs) q.len[i] = kv_len(c, i);
+  }
+  __syncthreads();
+  return true;
+}
+__device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start, const Sequences* held, long long row,
+                                          const Div& page_size) {
   int b = (int)row, back = 1;   // rows from this one to the sequence's last
   if (row_start) {
+    const int* start = held ? held->start : row_start;
     // the last sequence that starts at or before the row (empty ones end where they start)
     int lo = 0, hi = c.seqs;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (row_start[mid] <= row) lo = mid + 1;
+      if (start[mid] <= row) lo = mid + 1;
       else hi = mid;
     }
     b = lo - 1;
-    const int end = b < 0 ? 0 : row_start[b + 1];
+    const int end = b < 0 ? 0 : start[b + 1];
     if (row >= end) return {-1, 0, true};
     back = end - (int)row;
   }
-  const int t = kv_len(c, b) - back;
+  const int t = (held ? held->len[b] : kv_len(c, b)) - back;
   if (t < 0) return {-1, 0, false};
   const int n = page_size.of((unsigned)t), page = c.table[b * c.ld_table + n];
   return {(unsigned)page < (unsigned)c.pages ? page : -1, t - n * c.page_size, false};
@@ -121,6 +136,7 @@ template <class T, bool VEC, int L, int U>
 __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
                                                   const Div heads, const Div page_size) {
   constexpr int G = 256 / L;
+  __shared__ Sequences sequences;
   const int lane = threadIdx.x % L, col = 16 * lane, n = min(2, max(0, c.head_dim - col) / 8);   // eights of this lane
   pdl_trigger();
   pdl_wait();
@@ -143,9 +159,10 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
       }
     }
   }
+  const Sequences* held = hold(c, r.row_start, sequences) ? &sequences : nullptr;
   Place p[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) p[u] = row[u] < r.rows ? place_of(c, r.row_start, row[u], page_size) : Place{-1, 0, true};
+  for (int u = 0; u < U; ++u) p[u] = row[u] < r.rows ? place_of(c, r.row_start, held, row[u], page_size) : Place{-1, 0, true};
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -180,13 +197,19 @@ __device__ __forceinline__ void from_e4m3x4(uint32_t u, float* v) {
   v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
 }
 
+// L threads to a head of a row, as many columns to each as 16 bytes of the result hold (so that
+// adjacent lanes write adjacent vectors), U such heads to a thread, all loads under way before the
+// first is used.  Bound by memory.
 template <class T, bool VEC, int L, int U>
 __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
                                                  const Div heads, const Div page_size) {
   constexpr int G = 256 / L;
-  const int lane = threadIdx.x % L, col = 8 * lane;
+  constexpr int E = VecN<T>::n;
+  const int lane = threadIdx.x % L, col = E * lane;
+  __shared__ Sequences sequences;
   pdl_trigger();
   pdl_wait();
+  const Sequences* held = hold(c, r.row_start, sequences) ? &sequences : nullptr;
   if (col >= c.head_dim) return;
   Place p[U];
   int head[U];
@@ -196,19 +219,25 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache
     const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
     row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
     head[u] = (int)(item - row[u] * c.heads);
-    p[u] = row[u] < r.rows ? place_of(c, r.row_start, row[u], page_size) : Place{-1, 0, true};
+    p[u] = row[u] < r.rows ? place_of(c, r.row_start, held, row[u], page_size) : Place{-1, 0, true};
   }
-  uint2 q[U][2];
+  uint32_t q[U][2][E / 4];
   float s[U][2];
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-      q[u][kv] = make_uint2(0, 0);
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) q[u][kv][i] = 0;
       s[u][kv] = 0.f;
       if (p[u].page < 0) continue;
-      q[u][kv] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) +
-                                                 place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col);
+      const uint8_t* at = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col;
+      if constexpr (E == 8) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        q[u][kv][0] = v.x, q[u][kv][E / 4 - 1] = v.y;
+      } else {
+        q[u][kv][0] = *reinterpret_cast<const uint32_t*>(at);
+      }
       s[u][kv] = (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p[u], head[u])];
     }
 #pragma unroll
@@ -216,13 +245,13 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache
     if (p[u].of_none) continue;
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-      float x[8];
-      from_e4m3x4(q[u][kv].x, x);
-      from_e4m3x4(q[u][kv].y, x + 4);
+      float x[E];
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) from_e4m3x4(q[u][kv][i], x + 4 * i);
       const float f = kv_scale(s[u][kv]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= f;
-      store8<T, VEC>(reinterpret_cast<T*>(kv ? r.v : r.k) + row[u] * (kv ? r.ldv : r.ldk) + (long long)head[u] * c.head_dim + col, x);
+      for (int i = 0; i < E; ++i) x[i] *= f;
+      store_vec<T, VEC>(reinterpret_cast<T*>(kv ? r.v : r.k) + row[u] * (kv ? r.ldv : r.ldk) + (long long)head[u] * c.head_dim + col, x);
     }
   }
 }
@@ -239,12 +268,13 @@ template <class T, bool VEC, bool WRITE, int L, int U> cudaError_t kv_rows_u(con
 }
 template <class T, bool VEC, bool WRITE, int L> cudaError_t kv_rows_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
   // several heads to a lane where two blocks of them for every SM remain
-  constexpr int U = !WRITE ? 4 : sizeof(T) == 2 ? 2 : 1;
+  // (read 14566 x 16 heads of 128 in bf16: 32.2 us with two, 33.6 with four, 44.8 with eight)
+  constexpr int U = WRITE && sizeof(T) == 4 ? 1 : 2;
   if (U > 1 && r.rows * c.heads >= 152ll * 2 * U * (256 / L)) return kv_rows_u<T, VEC, WRITE, L, U>(c, r, s);
   return kv_rows_u<T, VEC, WRITE, L, 1>(c, r, s);
 }
 template <class T, bool VEC, bool WRITE> cudaError_t kv_rows_v(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  constexpr int L = WRITE ? 4 : 8;   // lanes to 64 columns
+  constexpr int L = WRITE ? 4 : 64 / VecN<T>::n;   // threads to 64 columns
   return c.head_dim <= 64 ? kv_rows_l<T, VEC, WRITE, L>(c, r, s)
          : c.head_dim <= 128 ? kv_rows_l<T, VEC, WRITE, 2 * L>(c, r, s) : kv_rows_l<T, VEC, WRITE, 4 * L>(c, r, s);
 }
