@@ -64,40 +64,27 @@ struct Place {
   int page, slot;
   bool of_none;
 };
-// First rows and lengths of the sequences, by a block in shared memory where there are not too many: one
-// wait for memory instead of one for every halving of the search and one for the length (8000 rows of 19
-// sequences 8.4 -> 6 us).
-constexpr int SEQS_HELD = 512;
-struct Sequences {
-  int start[SEQS_HELD + 1], len[SEQS_HELD];
-};
-__device__ __forceinline__ bool hold(const KvCache& c, const int* row_start, Sequences& q) {
-  if (!row_start || c.seqs > SEQS_HELD) return false;
-  for (int i = threadIdx.x; i <= c.seqs; i += blockDim.x) {
-    q.start[i] = row_start[i];
-    if (i < c.seqs) q.len[i] = kv_len(c, i);
-  }
-  __syncthreads();
-  return true;
-}
-__device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start, const Sequences* held, long long row,
-                                          const Div& page_size) {
+// (by a whole warp)
+__device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start, long long row, const Div& page_size) {
   int b = (int)row, back = 1;   // rows from this one to the sequence's last
   if (row_start) {
-    const int* start = held ? held->start : row_start;
-    // the last sequence that starts at or before the row (empty ones end where they start)
-    int lo = 0, hi = c.seqs;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (start[mid] <= row) lo = mid + 1;
-      else hi = mid;
+    // the last sequence that starts at or before the row (empty ones end where they start), by 32 starts at
+    // a time: one wait for memory up to 31 sequences, two up to 1023
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = c.seqs + 1;
+    while (n > 1) {
+      const int step = (n + 31) / 32, at = lane * step;
+      const int k = __popc(__ballot_sync(0xffffffffu, at < n && row_start[lo + min(at, n - 1)] <= row));
+      if (k == 0) return {-1, 0, true};
+      lo += (k - 1) * step;
+      n = min(step, n - (k - 1) * step);
     }
-    b = lo - 1;
-    const int end = b < 0 ? 0 : start[b + 1];
-    if (row >= end) return {-1, 0, true};
-    back = end - (int)row;
+    if (lo == c.seqs) return {-1, 0, true};
+    b = lo;
+    back = row_start[b + 1] - (int)row;
+    if (back <= 0) return {-1, 0, true};   // (starts that do not rise)
   }
-  const int t = (held ? held->len[b] : kv_len(c, b)) - back;
+  const int t = kv_len(c, b) - back;
   if (t < 0) return {-1, 0, false};
   const int n = page_size.of((unsigned)t), page = c.table[b * c.ld_table + n];
   return {(unsigned)page < (unsigned)c.pages ? page : -1, t - n * c.page_size, false};
@@ -128,54 +115,46 @@ template <class T, bool VEC> __device__ __forceinline__ float amax16(const Eight
   }
 }
 
-// L lanes to a head of a row, sixteen columns to a lane, U such heads to a lane, all loads of which are
-// under way before the first is used.  Bound by instruction issue before it was by memory: hence sixteen
-// columns (eight: 14566 x 16 heads of 128 in bf16 49 us, half of its instructions addresses and the
-// maximum's exchange) and 32-bit strides.
-template <class T, bool VEC, int L, int U>
+// A warp to a row, or to an equal part of its heads: a row's place is looked up once, while its first
+// columns are under way.  L lanes to a head, sixteen columns to a lane.  Bound by instruction issue
+// before it was by memory: hence sixteen columns (eight, and a look-up for every head: 14566 x 16 heads of
+// 128 in bf16 49 us) and 32-bit strides.
+template <class T, bool VEC, int L>
 __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
-                                                  const Div heads, const Div page_size) {
-  constexpr int G = 256 / L;
-  __shared__ Sequences sequences;
-  const int lane = threadIdx.x % L, col = 16 * lane, n = min(2, max(0, c.head_dim - col) / 8);   // eights of this lane
+                                                  const Div parts_by, int parts, int per, const Div page_size) {
+  const int lane = threadIdx.x & 31, col = 16 * (lane % L), n = min(2, max(0, c.head_dim - col) / 8);   // eights of this lane
+  const long long warp = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long row = warp >> 31 ? warp / parts : parts_by.of((unsigned)warp);
+  const int first = (int)(warp - row * parts) * per, end = min(c.heads, first + per);
   pdl_trigger();
   pdl_wait();
-  Eight<T, VEC> x[U][2][2];
-  int head[U];
-  long long row[U];
+  if (row >= r.rows) return;
+  const T* from[2] = {reinterpret_cast<const T*>(r.k) + row * r.ldk + col, reinterpret_cast<const T*>(r.v) + row * r.ldv + col};
+  Place p = {-1, 0, true};
+  for (int h0 = first; h0 < end; h0 += 32 / L) {
+    const int head = h0 + lane / L;
+    const bool in = head < end && n > 0;
+    Eight<T, VEC> x[2][2];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
-    row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
-    head[u] = (int)(item - row[u] * c.heads);
-    const int at = head[u] * c.head_dim + col;
+    for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[u][0][i].zero();
-      x[u][1][i].zero();
-      if (row[u] < r.rows && i < n) {
-        x[u][0][i].load(reinterpret_cast<const T*>(r.k) + row[u] * r.ldk + at + 8 * i);
-        x[u][1][i].load(reinterpret_cast<const T*>(r.v) + row[u] * r.ldv + at + 8 * i);
+      for (int i = 0; i < 2; ++i) {
+        x[kv][i].zero();
+        if (in && i < n) x[kv][i].load(from[kv] + head * c.head_dim + 8 * i);
       }
-    }
-  }
-  const Sequences* held = hold(c, r.row_start, sequences) ? &sequences : nullptr;
-  Place p[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) p[u] = row[u] < r.rows ? place_of(c, r.row_start, held, row[u], page_size) : Place{-1, 0, true};
-#pragma unroll
-  for (int u = 0; u < U; ++u)
+    if (h0 == first) p = place_of(c, r.row_start, row, page_size);
+    if (p.page < 0) return;
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       float v[16];
-      x[u][kv][0].get(v);
-      x[u][kv][1].get(v + 8);
-      float m = amax16<T, VEC>(x[u][kv], v);
+      x[kv][0].get(v);
+      x[kv][1].get(v + 8);
+      float m = amax16<T, VEC>(x[kv], v);
 #pragma unroll
       for (int o = L / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (p[u].page < 0 || n == 0) continue;
+      if (!in) continue;
       const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
-      uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col;
+      uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p, head) + col;
       const f32x2 i2 = f2u(inv, inv);
       uint32_t w[4];
 #pragma unroll
@@ -185,8 +164,9 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
       }
       if (n == 2) *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
       else *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
-      if (lane == 0) (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p[u], head[u])] = s;
+      if (col == 0) (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p, head)] = s;
     }
+  }
 }
 
 // four e4m3 bytes as floats
@@ -197,90 +177,104 @@ __device__ __forceinline__ void from_e4m3x4(uint32_t u, float* v) {
   v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
 }
 
-// L threads to a head of a row, as many columns to each as 16 bytes of the result hold (so that
-// adjacent lanes write adjacent vectors), U such heads to a thread, all loads under way before the
-// first is used.  Bound by memory.
-template <class T, bool VEC, int L, int U>
+// A warp to a row, or to an equal part of its vectors (as many columns as 16 bytes of the result hold, so
+// that adjacent lanes write adjacent vectors): a row's place is looked up once.  U vectors of k and of v
+// are under way at a time.  Bound by memory.
+template <class T, bool VEC, int U>
 __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
-                                                 const Div heads, const Div page_size) {
-  constexpr int G = 256 / L;
+                                                 const Div parts_by, int parts, int per, const Div dim_by, const Div page_size) {
   constexpr int E = VecN<T>::n;
-  const int lane = threadIdx.x % L, col = E * lane;
-  __shared__ Sequences sequences;
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long row = warp >> 31 ? warp / parts : parts_by.of((unsigned)warp);
+  const int first = (int)(warp - row * parts) * per + lane, all = c.heads * (c.head_dim / E), end = min(all, first - lane + per);
   pdl_trigger();
   pdl_wait();
-  const Sequences* held = hold(c, r.row_start, sequences) ? &sequences : nullptr;
-  if (col >= c.head_dim) return;
-  Place p[U];
-  int head[U];
-  long long row[U];
+  if (row >= r.rows) return;
+  const Place p = place_of(c, r.row_start, row, page_size);
+  if (p.of_none) return;
+  const uint8_t* from[2] = {reinterpret_cast<const uint8_t*>(c.k) + place_at(c.k_stride, p, 0),
+                            reinterpret_cast<const uint8_t*>(c.v) + place_at(c.v_stride, p, 0)};
+  const float* scale[2] = {c.k_scale + place_at(c.k_scale_stride, p, 0), c.v_scale + place_at(c.v_scale_stride, p, 0)};
+  const unsigned step[2] = {(unsigned)c.k_stride[2], (unsigned)c.v_stride[2]};
+  const unsigned scale_step[2] = {(unsigned)c.k_scale_stride[2], (unsigned)c.v_scale_stride[2]};
+  T* to[2] = {reinterpret_cast<T*>(r.k) + row * r.ldk, reinterpret_cast<T*>(r.v) + row * r.ldv};
+  for (int i = first; i < end; i += 32 * U) {
+    uint32_t q[U][2][E / 4];
+    float s[U][2];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const long long item = ((long long)blockIdx.x * U + u) * G + threadIdx.x / L;
-    row[u] = item >> 31 ? item / c.heads : heads.of((unsigned)item);
-    head[u] = (int)(item - row[u] * c.heads);
-    p[u] = row[u] < r.rows ? place_of(c, r.row_start, held, row[u], page_size) : Place{-1, 0, true};
-  }
-  uint32_t q[U][2][E / 4];
-  float s[U][2];
+    for (int u = 0; u < U; ++u) {
+      const int at = (i + 32 * u) * E, head = dim_by.of((unsigned)at), col = at - head * c.head_dim;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+      for (int kv = 0; kv < 2; ++kv) {
+        s[u][kv] = 0.f;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-#pragma unroll
-      for (int i = 0; i < E / 4; ++i) q[u][kv][i] = 0;
-      s[u][kv] = 0.f;
-      if (p[u].page < 0) continue;
-      const uint8_t* at = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p[u], head[u]) + col;
-      if constexpr (E == 8) {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
-        q[u][kv][0] = v.x, q[u][kv][E / 4 - 1] = v.y;
-      } else {
-        q[u][kv][0] = *reinterpret_cast<const uint32_t*>(at);
+        for (int k = 0; k < E / 4; ++k) q[u][kv][k] = 0;
+        if (p.page < 0 || i + 32 * u >= end) continue;
+        const uint8_t* b = from[kv] + (unsigned long long)(unsigned)head * step[kv] + col;
+        if constexpr (E == 8) {
+          const uint2 v = *reinterpret_cast<const uint2*>(b);
+          q[u][kv][0] = v.x, q[u][kv][E / 4 - 1] = v.y;
+        } else {
+          q[u][kv][0] = *reinterpret_cast<const uint32_t*>(b);
+        }
+        s[u][kv] = scale[kv][(unsigned long long)(unsigned)head * scale_step[kv]];
       }
-      s[u][kv] = (kv ? c.v_scale : c.k_scale)[place_at(kv ? c.v_scale_stride : c.k_scale_stride, p[u], head[u])];
     }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (p[u].of_none) continue;
+    for (int u = 0; u < U; ++u) {
+      if (i + 32 * u >= end) break;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      float x[E];
+      for (int kv = 0; kv < 2; ++kv) {
+        float x[E];
 #pragma unroll
-      for (int i = 0; i < E / 4; ++i) from_e4m3x4(q[u][kv][i], x + 4 * i);
-      const float f = kv_scale(s[u][kv]);
+        for (int k = 0; k < E / 4; ++k) from_e4m3x4(q[u][kv][k], x + 4 * k);
+        const float f = kv_scale(s[u][kv]);
 #pragma unroll
-      for (int i = 0; i < E; ++i) x[i] *= f;
-      store_vec<T, VEC>(reinterpret_cast<T*>(kv ? r.v : r.k) + row[u] * (kv ? r.ldv : r.ldk) + (long long)head[u] * c.head_dim + col, x);
+        for (int k = 0; k < E; ++k) x[k] *= f;
+        store_vec<T, VEC>(to[kv] + (i + 32 * u) * E, x);
+      }
     }
   }
 }
 
-template <class T, bool VEC, bool WRITE, int L, int U> cudaError_t kv_rows_u(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  const long long per = 256 / L * U, grid = (r.rows * c.heads + per - 1) / per;
+// Steps of a row's loop that go to a warp: as many as leave WARPS_HELD warps to an SM.
+constexpr int WARPS_HELD = 128;   // (14566 x 16 heads of 128 in bf16, read: 31.9 us with 64, 29.9 with 128, 30.6 with 256)
+long long steps_to_warp(long long rows, long long steps) {
+  return std::max(1ll, std::min(steps, rows * steps / (152ll * WARPS_HELD)));
+}
+template <class T, bool VEC, int L> cudaError_t kv_write_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
+  const long long steps = (c.heads + 32 / L - 1) / (32 / L), n = steps_to_warp(r.rows, steps), parts = (steps + n - 1) / n;
+  const long long grid = (r.rows * parts + 7) / 8;
   if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  Div heads, page_size;
-  heads.by(c.heads);
+  Div parts_by, page_size;
+  parts_by.by((unsigned)parts);
   page_size.by(c.page_size);
-  const cudaError_t e = WRITE ? launch_pdl(k_kv_write<T, VEC, L, U>, (unsigned)grid, 256, 0, s, c, r, heads, page_size)
-                              : launch_pdl(k_kv_read<T, VEC, L, U>, (unsigned)grid, 256, 0, s, c, r, heads, page_size);
+  const cudaError_t e = launch_pdl(k_kv_write<T, VEC, L>, (unsigned)grid, 256, 0, s, c, r, parts_by, (int)parts, (int)(32 / L * n), page_size);
   return e != cudaSuccess ? e : launched();
 }
-template <class T, bool VEC, bool WRITE, int L> cudaError_t kv_rows_l(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  // several heads to a lane where two blocks of them for every SM remain
-  // (read 14566 x 16 heads of 128 in bf16: 32.2 us with two, 33.6 with four, 44.8 with eight)
-  constexpr int U = WRITE && sizeof(T) == 4 ? 1 : 2;
-  if (U > 1 && r.rows * c.heads >= 152ll * 2 * U * (256 / L)) return kv_rows_u<T, VEC, WRITE, L, U>(c, r, s);
-  return kv_rows_u<T, VEC, WRITE, L, 1>(c, r, s);
+template <class T, bool VEC> cudaError_t kv_write(const KvCache& c, const KvRows& r, cudaStream_t s) {
+  return c.head_dim <= 64 ? kv_write_l<T, VEC, 4>(c, r, s)
+         : c.head_dim <= 128 ? kv_write_l<T, VEC, 8>(c, r, s) : kv_write_l<T, VEC, 16>(c, r, s);
 }
-template <class T, bool VEC, bool WRITE> cudaError_t kv_rows_v(const KvCache& c, const KvRows& r, cudaStream_t s) {
-  constexpr int L = WRITE ? 4 : 64 / VecN<T>::n;   // threads to 64 columns
-  return c.head_dim <= 64 ? kv_rows_l<T, VEC, WRITE, L>(c, r, s)
-         : c.head_dim <= 128 ? kv_rows_l<T, VEC, WRITE, 2 * L>(c, r, s) : kv_rows_l<T, VEC, WRITE, 4 * L>(c, r, s);
+template <class T, bool VEC> cudaError_t kv_read(const KvCache& c, const KvRows& r, cudaStream_t s) {
+  constexpr int U = 2;
+  const long long all = (long long)c.heads * (c.head_dim / VecN<T>::n), steps = (all + 32 * U - 1) / (32 * U);
+  const long long n = steps_to_warp(r.rows, steps), parts = (steps + n - 1) / n;
+  const long long grid = (r.rows * parts + 7) / 8;
+  if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+  Div parts_by, dim_by, page_size;
+  parts_by.by((unsigned)parts);
+  dim_by.by(c.head_dim);
+  page_size.by(c.page_size);
+  const cudaError_t e = launch_pdl(k_kv_read<T, VEC, U>, (unsigned)grid, 256, 0, s, c, r, parts_by, (int)parts, (int)(32 * U * n), dim_by, page_size);
+  return e != cudaSuccess ? e : launched();
 }
 template <class T, bool WRITE> cudaError_t kv_rows(const KvCache& c, const KvRows& r, cudaStream_t s) {
   const auto al = [](const void* p, long long ld) { return !((uintptr_t)p & 15) && ld % (16 / (int)sizeof(T)) == 0; };
-  return al(r.k, r.ldk) && al(r.v, r.ldv) ? kv_rows_v<T, true, WRITE>(c, r, s) : kv_rows_v<T, false, WRITE>(c, r, s);
+  const bool vec = al(r.k, r.ldk) && al(r.v, r.ldv);
+  if constexpr (WRITE) return vec ? kv_write<T, true>(c, r, s) : kv_write<T, false>(c, r, s);
+  else return vec ? kv_read<T, true>(c, r, s) : kv_read<T, false>(c, r, s);
 }
 
 }  // namespace
