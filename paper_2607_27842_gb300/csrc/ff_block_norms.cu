@@ -65,15 +65,16 @@ template <class T, int NB, bool Q8>
 __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
     k_block_norms(long long rows, int C, int W, long long per, int chunks, const __grid_constant__ BlockNormsArgs a) {
   extern __shared__ __align__(16) float factors[];   // p, q, s: pieces of two halves, a lane's four columns each
-  __shared__ float2 red[2][8];
+  __shared__ __align__(16) float sums[2][2][64];   // of a slot's warps (8 places to a slot, 0 where it has fewer): squares, means
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1), slot = warp / W, slots = 8 / W;
   const int c0 = w * NB * 256 + 8 * lane;
-  const int wide = (C + 255) / 256 * 256;
+  const int wide = W * NB * 256;   // columns of the lanes
+  const bool ragged = C != wide;   // some lanes have pieces behind the row's end
   // (sample, chunk of its rows) of this block
   const long long sample = blockIdx.x / chunks, first = sample * a.rpb + (blockIdx.x - sample * chunks) * per;
   const long long end = min(rows, min((sample + 1) * a.rpb, first + per));
-  float *fp = factors, *fq = fp + ((a.gate || a.weight_after) ? wide : 0), *fs = fq + ((a.scale || a.weight) ? wide : 0);
-  const bool has_p = fq != fp, has_q = fs != fq, has_s = a.shift != nullptr;
+  float *fp = factors, *fq = fp + wide, *fs = fq + wide;
+  const bool has_s = a.shift != nullptr;
   bool in[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) in[i] = c0 + 256 * i < C;
@@ -96,17 +97,17 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
 #pragma unroll
   for (int i = 0; i < NB; ++i) fy[i].zero(), fx[i].zero();
   if (first + slot < end) load_row();
-  for (int c = threadIdx.x; c < C; c += 256) {
+  for (int c = threadIdx.x; c < wide; c += 256) {
     const int at = (c & ~255) + (c & 4) * 32 + (c & 248) / 2 + (c & 3);
-    auto weight = [&](const void* m) { return m ? to_f(reinterpret_cast<const T*>(m)[c]) : 1.f; };
-    if (has_p) fp[at] = (a.gate ? a.gate[sample * a.gate_stride + c] : 1.f) * weight(a.weight_after);
-    if (has_q) fq[at] = (a.scale ? 1.f + a.scale[sample * a.scale_stride + c] : 1.f) * weight(a.weight);
-    if (has_s) fs[at] = a.shift[sample * a.shift_stride + c];
+    const bool there = c < C;
+    auto weight = [&](const void* m) { return m && there ? to_f(reinterpret_cast<const T*>(m)[c]) : 1.f; };
+    fp[at] = (a.gate && there ? a.gate[sample * a.gate_stride + c] : 1.f) * weight(a.weight_after);
+    fq[at] = (a.scale && there ? 1.f + a.scale[sample * a.scale_stride + c] : 1.f) * weight(a.weight);
+    if (has_s) fs[at] = there ? a.shift[sample * a.shift_stride + c] : 0.f;
   }
+  if (threadIdx.x < 64) sums[0][0][threadIdx.x] = sums[0][1][threadIdx.x] = sums[1][0][threadIdx.x] = sums[1][1][threadIdx.x] = 0.f;
   __syncthreads();
-  // (pieces behind the row's end have no place there)
   auto factor = [&](const float* f, int i, f32x2 (&v)[4]) {
-    if (!in[i]) return;
     const ulonglong2* p = reinterpret_cast<const ulonglong2*>(f + (w * NB + i) * 256 + 4 * lane);
     const ulonglong2 l = p[0], h = p[32];
     v[0] = l.x, v[1] = l.y, v[2] = h.x, v[3] = h.y;
@@ -143,19 +144,19 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
     }
     ss = warp_sum(lo_f(sum) + hi_f(sum));
     if (W > 1) {
-      if (lane == 0) red[which][warp] = make_float2(mean, ss);
+      float *of = &sums[which][0][8 * slot], *means = &sums[which][1][8 * slot];
+      if (lane == 0) {
+        of[w] = ss;
+        if (a.centered) means[w] = mean;
+      }
       slot_sync(slot, W);
-      ss = 0.f;
+      const float4 s0 = reinterpret_cast<const float4*>(of)[0], s1 = reinterpret_cast<const float4*>(of)[1];
+      ss = ((s0.x + s0.y) + (s0.z + s0.w)) + ((s1.x + s1.y) + (s1.z + s1.w));
       if (a.centered) {
         float m = 0.f;
-        for (int k = 0; k < W; ++k) m = fmaf(red[which][warp - w + k].x, held(k), m);
+        for (int k = 0; k < W; ++k) m = fmaf(means[k], held(k), m);
         mean = m * per_col;
-        for (int k = 0; k < W; ++k) {
-          const float2 o = red[which][warp - w + k];
-          ss += fmaf((o.x - mean) * (o.x - mean), held(k), o.y);
-        }
-      } else {
-        for (int k = 0; k < W; ++k) ss += red[which][warp - w + k].y;
+        for (int k = 0; k < W; ++k) ss = fmaf((means[k] - mean) * (means[k] - mean), held(k), ss);
       }
     }
     return make_float2(mean, rsqrtf(fmaf(ss, per_col, a.eps)));
@@ -190,15 +191,11 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
     if (a.norm_after) by = normed(h, norm(h, 0));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      f32x2 p[4] = {by, by, by, by};
-      if (has_p) {
-        factor(fp, i, p);
+      f32x2 p[4];
+      factor(fp, i, p);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = fmul2(by, p[k]);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) h[i][k] = ffma2(rs, res[i][k], fmul2(h[i][k], p[k]));
-      if (!in[i]) h[i][0] = h[i][1] = h[i][2] = h[i][3] = 0;
+      for (int k = 0; k < 4; ++k) h[i][k] = ffma2(rs, res[i][k], fmul2(h[i][k], fmul2(by, p[k])));
+      if (ragged && !in[i]) h[i][0] = h[i][1] = h[i][2] = h[i][3] = 0;
       if (a.sum && in[i]) Cols<T>::store(sm + 256 * i, h[i]);
     }
     sm += a.ldsum * slots;
@@ -206,15 +203,16 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
     by = normed(h, norm(h, 1));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      f32x2 q[4] = {by, by, by, by}, s[4] = {0, 0, 0, 0};
-      if (has_q) {
-        factor(fq, i, q);
+      f32x2 q[4], s[4];
+      factor(fq, i, q);
+      if (has_s) {
+        factor(fs, i, s);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = fmul2(by, q[k]);
+        for (int k = 0; k < 4; ++k) h[i][k] = ffma2(h[i][k], fmul2(by, q[k]), s[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[i][k] = fmul2(h[i][k], fmul2(by, q[k]));
       }
-      if (has_s) factor(fs, i, s);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) h[i][k] = ffma2(h[i][k], q[k], s[k]);
     }
     if constexpr (!Q8) {
 #pragma unroll
@@ -468,10 +466,10 @@ template <class T, bool Q8> cudaError_t norms_any(long long rows, int C, const B
 
 template <class T, int NB, bool Q8> cudaError_t norms_nb(int W, long long rows, int C, BlockNormsArgs a, cudaStream_t s) {
   const auto kernel = k_block_norms<T, NB, Q8>;
-  const int wide = (C + 255) / 256 * 256, slots = 8 / W;
+  const int wide = W * NB * 256, slots = 8 / W;
   const bool modulated = a.gate || a.scale || a.shift;
   if (!modulated) a.rpb = (int)rows;
-  const size_t smem = 4ull * wide * ((a.gate || a.weight_after) + (a.scale || a.weight) + (a.shift != nullptr));
+  const size_t smem = 4ull * wide * (2 + (a.shift != nullptr));
   // (the limit of the widest row: another call of the process may come between it and the launch)
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * (NB * 2048 < BLOCK_NORMS_COLS_MAX ? NB * 2048 : BLOCK_NORMS_COLS_MAX));
   if (e != cudaSuccess) return e;
