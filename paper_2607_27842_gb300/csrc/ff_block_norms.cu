@@ -247,15 +247,15 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
 
 // Rows on any boundary and of any width, element by element: NB adjacent 128-column blocks to a warp,
 // adjacent rows one after the other.  With KEEP the factors stay in registers until the sample changes.
-template <class T, int NB, bool VEC, bool Q8, bool KEEP>
+template <class T, int NB, bool Q8, bool KEEP>
 __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long rows, int C, int W, long long per,
                                                                    const __grid_constant__ BlockNormsArgs a) {
   __shared__ float2 red[2][8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp & (W - 1), slot = warp / W;
-  const int c0 = w * NB * 128 + at<VEC>(lane), left = C - c0;   // columns from the lane's first on
+  const int c0 = w * NB * 128 + lane, left = C - c0;   // columns from the lane's first on
   const int held = min(C, (w + 1) * NB * 128) - w * NB * 128;   // columns of the warp; none where not positive
   const long long r0 = ((long long)blockIdx.x * (8 / W) + slot) * per, r1 = min(rows, r0 + per);
-  Four<T, VEC> fy[NB], fx[NB];
+  Four<T, false> fy[NB], fx[NB];
   f32x2 p[KEEP ? NB : 1][2], q[KEEP ? NB : 1][2], s[KEEP ? NB : 1][2];
   long long sample = -1;
   pdl_trigger();
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
   // the three factors of a lane's four columns of block i, for this row's sample
   auto times = [&](f32x2 (&v)[2], const void* weight, int i) {
     if (!weight) return;
-    Four<T, VEC> f;
+    Four<T, false> f;
     f32x2 u[2];
     f.load(reinterpret_cast<const T*>(weight) + c0 + 128 * i, left - 128 * i);
     f.get(u);
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
     m += sample * stride + c0 + 128 * i;
     float e[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = (VEC ? k : 32 * k) < left - 128 * i ? m[VEC ? k : 32 * k] : 0.f;
+    for (int k = 0; k < 4; ++k) e[k] = 32 * k < left - 128 * i ? m[32 * k] : 0.f;
     v[0] = f2u(e[0], e[1]);
     v[1] = f2u(e[2], e[3]);
   };
@@ -311,7 +311,6 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
   };
   // a pair of columns, 0 past the row's end
   auto within = [&](f32x2 v, int i, int k) -> f32x2 {
-    if (VEC) return 128 * i < left ? v : 0;
     return 128 * i + 64 * k + 32 < left ? v : 128 * i + 64 * k < left ? f2u(lo_f(v), 0.f) : 0;
   };
   // mean (0 where the norm has none) and 1 / root mean square of a row's columns, the which-th of the
@@ -404,7 +403,7 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
       if constexpr (!KEEP) make_p(i, p[0]);
 #pragma unroll
       for (int k = 0; k < 2; ++k) h[i][k] = ffma2(rs, res[i][k], fmul2(h[i][k], fmul2(by, p[KEEP ? i : 0][k])));
-      if (a.sum && 128 * i < left) Four<T, VEC>::store(sm + 128 * i, left - 128 * i, h[i]);
+      if (a.sum && 128 * i < left) Four<T, false>::store(sm + 128 * i, left - 128 * i, h[i]);
     }
     sm += a.ldsum;
     if (!Q8 && !a.out) continue;
@@ -418,22 +417,18 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
     if constexpr (!Q8) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
-        if (128 * i < left) Four<T, VEC>::store(o + 128 * i, left - 128 * i, h[i]);
+        if (128 * i < left) Four<T, false>::store(o + 128 * i, left - 128 * i, h[i]);
       o += a.ldo;
     } else {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         // columns past the row's end hold no magnitude
         float m = 0.f;
-        if (VEC) {
-          if (128 * i < left) m = amax4(h[i]);
-        } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (128 * i + 32 * k < left) m = max_abs(m, k & 1 ? hi_f(h[i][k / 2]) : lo_f(h[i][k / 2]));
-        }
+        for (int k = 0; k < 4; ++k)
+          if (128 * i + 32 * k < left) m = max_abs(m, k & 1 ? hi_f(h[i][k / 2]) : lo_f(h[i][k / 2]));
         const float sc = q8_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
-        if (128 * i < left) ff::store8<VEC>(o8 + 128 * i, left - 128 * i, h[i], q8_inv(sc));
+        if (128 * i < left) ff::store8<false>(o8 + 128 * i, left - 128 * i, h[i], q8_inv(sc));
         if (lane == 0 && 128 * i < held) sp[i * a.q8.lds] = sc;
       }
       o8 += a.q8.ldq;
@@ -451,7 +446,7 @@ template <class T, int NB, bool Q8> cudaError_t norms_any_nb(int W, long long ro
   // two blocks to an SM go over all rows where factors stay in registers; else a row to a slot
   const long long most = KEEP ? 152 * 2 : (rows + slots - 1) / slots, per = (rows + most * slots - 1) / (most * slots);
   const long long grid = (rows + per * slots - 1) / (per * slots);
-  const cudaError_t e = launch_pdl(k_block_norms_any<T, NB, false, Q8, KEEP>, (unsigned)grid, 256, 0, s, rows, C, W, per, a);
+  const cudaError_t e = launch_pdl(k_block_norms_any<T, NB, Q8, KEEP>, (unsigned)grid, 256, 0, s, rows, C, W, per, a);
   return e != cudaSuccess ? e : launched();
 }
 template <class T, bool Q8> cudaError_t norms_any(long long rows, int C, const BlockNormsArgs& a, cudaStream_t s) {
@@ -487,10 +482,13 @@ template <class T, bool Q8> cudaError_t norms(long long rows, int C, const Block
   if (C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
     return norms_any<T, Q8>(rows, C, a, s);
   const int pieces = (C + 255) / 256;
-  // Warps to a row: two pieces to a warp (three where they leave fewer lanes idle), fewer while the rows
-  // alone leave the SMs without 8 warps each.
+  // Warps to a row: four pieces to a warp (fp32: two; three where they leave fewer lanes idle), fewer while
+  // the rows alone leave the SMs without 8 warps each.  14566 x 2048 with modulation and 8-bit output
+  // 38.0 us with four, 45.8 with two (three blocks to an SM instead of two), 41.8 with eight (one block);
+  // fp32 93.6, 88.6 and 87.4.
+  constexpr int PREF = sizeof(T) == 2 ? 4 : 2;
   int W = 1;
-  while (W < 8 && (pieces > 2 * W || (rows * W < 152 * 8 && pieces > W))) W *= 2;
+  while (W < 8 && (pieces > PREF * W || (rows * W < 152 * 8 && pieces > W))) W *= 2;
   if (W > 1 && pieces <= 3 * (W / 2) && rows * (W / 2) >= 152 * 8) W /= 2;
   const int nb = (pieces + W - 1) / W;
   return nb <= 1 ? norms_nb<T, 1, Q8>(W, rows, C, a, s) : nb <= 2 ? norms_nb<T, 2, Q8>(W, rows, C, a, s)
