@@ -479,7 +479,9 @@ template <class T, int NB, bool Q8> cudaError_t norms_nb(int W, long long rows, 
 }
 template <class T, bool Q8> cudaError_t norms(long long rows, int C, const BlockNormsArgs& a, cudaStream_t s) {
   const auto al = [](const void* p, long long ld) { return !((uintptr_t)p & 15) && ld % (16 / (int)sizeof(T)) == 0; };
-  if (C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
+  // (a row to a slot, and weights alone: nothing to reuse from shared memory, 1 x 2048 3.3 instead of 3.65 us)
+  const bool few = rows <= 2 * 152 && C <= 2048 && !a.gate && !a.scale && !a.shift;
+  if (few || C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
     return norms_any<T, Q8>(rows, C, a, s);
   const int pieces = (C + 255) / 256;
   // Warps to a row: four pieces to a warp (fp32: two; three where they leave fewer lanes idle), fewer while

@@ -71,8 +71,9 @@ struct Plan {
   Div page, split_by, tiles_by, blocks_by, together_by, groups_by;   // page_size, split, ..., the grid
   int group, tiles;        // query heads of a key head, units that share them
   int together, split, groups;   // units that go together, warps to each of them, groups of a sequence
+  int units;               // of all sequences, where whole is 2 (and a group is a unit)
   int join_queries, grid;  // queries to a block of the second kernel, blocks of the first
-  int whole;               // blocks take whole units; 2: one each
+  int whole;               // blocks take whole units; 2: the same number each, at most one to a warp
   int pairs, vectors;      // results may be stored in pairs, queries loaded four at a time
   float scale;             // softmax scale times log2(e)
   // strides of page and slot of keys and values in units of 2^shift bytes, by which every place's
@@ -256,10 +257,13 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     w0 = c0 + (sp < p.split ? quot(n * sp + p.split - 1, p.split, p.split_by) : n);
     w1 = c0 + (sp < p.split ? quot(n * (sp + 1) + p.split - 1, p.split, p.split_by) : n);
   };
-  if (p.whole == 2) {   // a block to a unit
-    const int b = p.groups_by.of(blockIdx.x), steps = steps_seen<Sh::T>(c, a.window, b);
+  if (p.whole == 2) {   // some units to a block, as many warps to each
+    // (to the kernel these warps go together; the units need not be of one sequence)
+    const long long unit = (long long)blockIdx.x * p.together + u;
+    const int b = unit < p.units ? p.groups_by.of((unsigned)unit) : 0;
+    const int steps = unit < p.units ? steps_seen<Sh::T>(c, a.window, b) : 0;
     stretch(0, steps);
-    at = {b, (int)blockIdx.x - b * groups, (int)w0, steps};
+    at = {b, (int)unit - b * groups, (int)w0, steps};
   } else {
     const Line line = line_up<Sh::T>(c, a.window, groups);
     total = line.total;
@@ -933,16 +937,19 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   long long tokens = (long long)c.table_pages * c.page_size;
   if (a.window) tokens = std::min(tokens, (long long)a.window);
   const long long units = (long long)c.seqs * c.heads * p.tiles, steps = steps_of(c.head_dim, tokens);
-  p.whole = steps > WHOLE_STEPS ? 0 : units > n_sms ? 1 : 2;
-  p.together = p.whole ? 1 : together(c.heads * p.tiles, Sh::WARPS);
+  const long long to_block = (units + n_sms - 1) / n_sms;   // units, where every SM takes the same number of whole ones
+  p.whole = steps > WHOLE_STEPS ? 0 : to_block > Sh::WARPS ? 1 : 2;
+  p.together = p.whole == 2 ? (int)to_block : p.whole ? 1 : together(c.heads * p.tiles, Sh::WARPS);
   p.split = Sh::WARPS / p.together;
   p.split_by.by(p.split);
   p.together_by.by(p.together);
-  p.groups = c.heads * p.tiles / p.together;
+  p.groups = c.heads * p.tiles / (p.whole == 2 ? 1 : p.together);
+  p.units = p.whole == 2 ? (int)units : 0;
   p.groups_by.by(p.groups);
-  // blocks: one to an SM; fewer where there are not two steps to a warp, and one to a unit where blocks take whole ones
+  // blocks: one to an SM; fewer where there are not two steps to a warp
   long long grid = std::min(n_sms, GRID_MAX);
-  grid = p.whole == 2 ? units : std::min(grid, p.whole ? units : (units / p.together * steps + 2 * p.split - 1) / (2 * p.split));
+  if (p.whole == 2) grid = (units + to_block - 1) / to_block;
+  if (p.whole == 0) grid = std::min(grid, (units / p.together * steps + 2 * p.split - 1) / (2 * p.split));
   p.blocks_by.by((unsigned)grid);
   p.grid = (int)grid;
   // queries to a block of the second kernel: all of them where a unit has a few parts, fewer where
