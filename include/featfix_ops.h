@@ -298,7 +298,8 @@ FEATFIX_API featfix_status featfix_op_kv_attention(int dtype, const featfix_kv_c
  *   z = norm(h) * weight * (1 + scale[s]) + shift[s],
  *   norm(u) = u / sqrt(mean(u^2) + eps), of u - mean(u) with FEATFIX_NORM_CENTERED.
  * Weights [C] in dtype (NULL: 1), gate, scale (NULL: 1 and 0) and shift (NULL: 0) float rows
- * of their strides.  h and all statistics stay in fp32; dev_sum (nullable) receives h
+ * of their strides.  h and all statistics stay in fp32 (rows whose sum of squares passes fp32's
+ * range, |u| of about 1e19, have norm 0); dev_sum (nullable) receives h
  * rounded to dtype, dev_out z, or dev_q and dev_q_scale z in 8 bits (scales as activations
  * have them); not both, and at least one of dev_sum, dev_out and dev_q is given.  Outputs may be
  * x or y where they have one row stride.                                        */

@@ -1,6 +1,7 @@
 // The norms at the end of a block and at the beginning of the next one, with gate and
 // residual between them (formulas: featfix_op_block_norms).  Bound by memory: x and y are read
 // once into registers, and what is written is computed from there.
+#include "ff_host.h"
 #include "ff_kv8.cuh"
 #include "ff_rows8.cuh"
 
@@ -465,8 +466,16 @@ template <class T, int NB, bool Q8> cudaError_t norms_nb(int W, long long rows, 
   const bool modulated = a.gate || a.scale || a.shift;
   if (!modulated) a.rpb = (int)rows;
   const size_t smem = 4ull * wide * (2 + (a.shift != nullptr));
-  // (the limit of the widest row: another call of the process may come between it and the launch)
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * (NB * 2048 < BLOCK_NORMS_COLS_MAX ? NB * 2048 : BLOCK_NORMS_COLS_MAX));
+  // (the limit of the widest row, set once: another call of the process may come between it and a launch)
+  static PerDevice<int> limits;
+  int dev = 0, limit = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= PerDevice<int>::devices) return cudaErrorNotSupported;
+  e = limits.get(dev, &limit, [&](int& v) {
+    v = 12 * std::min(NB * 2048, BLOCK_NORMS_COLS_MAX);
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v);
+  });
   if (e != cudaSuccess) return e;
   // rows of a sample in chunks: as many blocks as the SMs hold at once, or a row to a slot
   const long long samples = (rows + a.rpb - 1) / a.rpb, held = 152ll * (NB <= 2 ? 3 : NB <= 4 ? 2 : 1);
