@@ -222,7 +222,7 @@ FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_d
  * A place of the cache holds a head of one token: head_dim e4m3 values and one
  * scale, by the rule above with the head as the block:
  *   s = max(largest |x| of the head / 448, 2^-100),   q = e4m3(x / s).
- * Scales that are NaN or infinite stand for NaN in all of the head.
+ * Scales that are NaN, infinite or negative stand for NaN in all of the head.
  *
  * k, v are e4m3 bytes; place (page, slot, head) starts stride[0] * page +
  * stride[1] * slot + stride[2] * head bytes behind the pointer (multiples of 16, at

@@ -69,7 +69,9 @@ __device__ __forceinline__ int kv_len(const KvCache& c, int b) {
   return (int)max(0ll, min((long long)c.lens[b], most));
 }
 
-// What a scale stands for: infinities are NaN (featfix_ops.h).
-__device__ __forceinline__ float kv_scale(float s) { return s < __int_as_float(0x7f800000) ? s : __int_as_float(0x7fffffff); }
+// What a scale stands for: infinities and negative numbers are NaN (featfix_ops.h).
+__device__ __forceinline__ float kv_scale(float s) {
+  return s >= 0.f && s < __int_as_float(0x7f800000) ? s : __int_as_float(0x7fffffff);
+}
 
 }  // namespace ff

@@ -71,6 +71,26 @@ def test_queries_that_are_no_numbers(cuda, dtype):
     assert ((out[2].double() - ref[2]).abs() <= eo[2]).all() and ((lse[2].double() - ref_lse[2]).abs() <= el[2]).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [-1.0, -math.inf, -1e-38, math.nan])
+def test_scales_that_no_token_has(cuda, dtype, scale):
+    """Negative scales are NaN, as infinite ones: in the head that has one, and in no other."""
+    c = Cache(30, 16, 2, 64, 3, 9)
+    c.place([130, 140, 17])
+    c.fill(11)
+    q = randn((3, 8 * 64), 22).to(TD[dtype])
+    want, _ = attend(c, q, 8)
+    (p, s), (p2, s2) = c.at(0, 77, 78), c.at(2, 16, 17)
+    c.k_scale[p, s, 1] = scale
+    c.v_scale[p2, s2, 0] = scale
+    out, _ = attend(c, q, 8)
+    assert out[0, 4 * 64:].isnan().all() and out[2, :4 * 64].isnan().all()
+    assert (out[0, :4 * 64] == want[0, :4 * 64]).all() and (out[1] == want[1]).all() and (out[2, 4 * 64:] == want[2, 4 * 64:]).all()
+    k, v = (torch.zeros((3, 128), device="cuda", dtype=TD[dtype]) for _ in range(2))
+    ff.featfix_op_kv_read(dtype, c.parts, c.table, c.lens, k, v)
+    assert not k.isnan().any() and v[2, :64].isnan().all() and not v[2, 64:].isnan().any() and not v[:2].isnan().any()
+
+
 def test_streams_and_threads_with_workspaces_of_their_own(cuda):
     """Two threads, each on a stream with its own workspace and cache, at the same time."""
     caches, qs, wants = [], [], []
