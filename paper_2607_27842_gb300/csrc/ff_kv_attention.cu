@@ -785,7 +785,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       }
     }
   }
-  if (!p.whole && threadIdx.x == 0) meta[2] = goes_on;
+  // (within the grid also where lengths changed meanwhile)
+  if (!p.whole && threadIdx.x == 0) meta[2] = max(0, min(goes_on, (int)(gridDim.x - 1 - blockIdx.x)));
 }
 
 // Units of several blocks: block (x, y) joins some queries of a unit of the y-th group that goes over
@@ -822,8 +823,10 @@ __global__ void __launch_bounds__(JOIN) k_kv_join(const __grid_constant__ KvCach
   }
   if (i < 0) return;
   const int* meta = metas + 4 * i;
-  const int n = meta[2] + 1;
-  const int b = meta[0], unit = meta[1] + place, head = p.tiles_by.of(unit), first = (unit - head * p.tiles) * Sh::NQ;
+  const int n = min(meta[2], p.grid - 1 - i) + 1;
+  // (places of the tensors also where two calls share a workspace at the same time, which they must not)
+  const int b = min((unsigned)meta[0], c.seqs - 1u), unit = min((unsigned)meta[1], (unsigned)(c.heads * p.tiles - p.together)) + place;
+  const int head = p.tiles_by.of(unit), first = (unit - head * p.tiles) * Sh::NQ;
   const int queries = min(min(Sh::NQ, p.group - first) - q0, p.join_queries);
   if (queries <= 0) return;
   auto part = [&](int k) { return ws + (2ll * ((i + k) * p.together + place) + (k ? 0 : 1)) * Sh::PART; };
