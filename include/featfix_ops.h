@@ -267,8 +267,8 @@ FEATFIX_API featfix_status featfix_op_kv_read(int dtype, const featfix_kv_cache*
                                   const int* dev_row_start, void* dev_k, long long ld_k, void* dev_v, long long ld_v,
                                   void* stream);
 
-/* Scratch bytes that featfix_op_kv_attention needs for caches of up to `tokens` tokens to
- * a sequence (table_pages * page_size), on any GPU; 0 where it needs none.      */
+/* Scratch bytes that featfix_op_kv_attention needs for up to `seqs` sequences in caches of up to
+ * `tokens` tokens to each (table_pages * page_size), on any GPU; 0 where it needs none. */
 FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int k_heads, int head_dim,
                                          long long tokens);
 

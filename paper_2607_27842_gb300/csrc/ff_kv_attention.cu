@@ -42,9 +42,14 @@ namespace {
 
 constexpr int GRID_MAX = 160;      // blocks that the workspace has room for
 constexpr float NONE = -3.0e38f;   // maximum of nothing
-// longest units, in steps, of which every block takes whole ones (no second kernel): 1000 tokens of 16 + 4
-// heads 11.1 us so and 14.2 shared out, 2000 tokens 17.4 and 14.7
-constexpr int WHOLE_STEPS = 32;
+// Blocks take whole units, and there is no second kernel, where units are short: at most WHOLE_STEPS steps
+// (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 14.2 shared out, 1 x 2000 17.4 and 14.7), and a block's
+// fit its warps (200 x 1000 tokens of 32 + 8 heads 75 and 87 us) or have WHOLE_SUM steps in all (256 x 256
+// tokens 37.5 and 41.7, 256 x 1000 114 and 105, 4096 x 32 131 and 114).
+constexpr int WHOLE_STEPS = 32, WHOLE_SUM = 160, SMS = 152;
+bool whole_units(long long units, long long steps, int warps) {
+  return steps <= WHOLE_STEPS && (units <= (long long)SMS * warps || units * steps <= SMS * WHOLE_SUM);
+}
 
 // Shapes of a variant: columns of a head rounded up to DP, NT times 8 query heads.
 template <class E, int DP, int NT> struct Shape {
@@ -938,7 +943,7 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   if (a.window) tokens = std::min(tokens, (long long)a.window);
   const long long units = (long long)c.seqs * c.heads * p.tiles, steps = steps_of(c.head_dim, tokens);
   const long long to_block = (units + n_sms - 1) / n_sms;   // units, where every SM takes the same number of whole ones
-  p.whole = steps > WHOLE_STEPS ? 0 : to_block > Sh::WARPS ? 1 : 2;
+  p.whole = !whole_units(units, steps, Sh::WARPS) ? 0 : to_block > Sh::WARPS ? 1 : 2;
   p.together = p.whole == 2 ? (int)to_block : p.whole ? 1 : together(c.heads * p.tiles, Sh::WARPS);
   p.split = Sh::WARPS / p.together;
   p.split_by.by(p.split);
@@ -979,9 +984,9 @@ template <class T> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cud
 }  // namespace
 
 size_t kv_attention_workspace(int seqs, int q_heads, int heads, int dim, long long tokens) {
-  (void)seqs;
-  if (steps_of(dim, tokens) <= WHOLE_STEPS) return 0;
   const int group = q_heads / heads, queries = 8 * eights(dim, group), units = heads * ((group + queries - 1) / queries);
+  // (by the fewest warps of a block of either type)
+  if (whole_units((long long)seqs * units, steps_of(dim, tokens), queries > 8 || dim > 128 ? 8 : 12)) return 0;
   const size_t most = std::max({together(units, 8), together(units, 12), together(units, 16)});   // (by a block's warps)
   return GRID_MAX * (most * 2 * queries * (padded(dim) + 4) * 4 + 16);
 }

@@ -21,7 +21,9 @@ pytestmark = pytest.mark.gpu
     (70, 1500, 2, 3, 64, 16, 0),        # shared out over all blocks, several sequences to a lane of the line
     (300, 90, 8, 1, 32, 8, 0),          # whole units, more than the SMs have warps
     (200, 2000, 1, 4, 128, 32, 70),     # short by the window alone
-    (1100, 40, 2, 2, 128, 16, 0)])
+    (1100, 40, 2, 2, 128, 16, 0),
+    (1200, 90, 8, 1, 32, 8, 0),         # shared out: more steps than whole units are taken for
+    (900, 70, 9, 2, 64, 16, 40), (500, 120, 5, 9, 72, 8, 0)])
 def test_many_sequences(cuda, dtype, seqs, most, heads, group, dim, page, window):
     g = torch.Generator().manual_seed(seqs)
     lens = [int(v) for v in torch.randint(0, most + 1, (seqs,), generator=g)]
