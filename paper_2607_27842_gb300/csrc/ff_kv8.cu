@@ -118,7 +118,8 @@ template <class T, bool VEC> __device__ __forceinline__ float amax16(const Eight
 // A warp to a row, or to an equal part of its heads: a row's place is looked up once, while its first
 // columns are under way.  L lanes to a head, sixteen columns to a lane.  Bound by instruction issue
 // before it was by memory: hence sixteen columns (eight, and a look-up for every head: 14566 x 16 heads of
-// 128 in bf16 49 us) and 32-bit strides.
+// 128 in bf16 46 us) and 32-bit strides.  Now 30.6 us, 5.9 TB/s, and 45.7 from fp32, 6.6 TB/s; one token of 4
+// heads 1.9 us in a graph.
 template <class T, bool VEC, int L>
 __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
                                                   const Div parts_by, int parts, int per, const Div page_size) {
@@ -179,7 +180,7 @@ __device__ __forceinline__ void from_e4m3x4(uint32_t u, float* v) {
 
 // A warp to a row, or to an equal part of its vectors (as many columns as 16 bytes of the result hold, so
 // that adjacent lanes write adjacent vectors): a row's place is looked up once.  U vectors of k and of v
-// are under way at a time.  Bound by memory.
+// are under way at a time.  Bound by memory: 14566 x 16 heads of 128 30.0 us in bf16, 6.0 TB/s, 49.9 in fp32.
 template <class T, bool VEC, int U>
 __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ KvCache c, const __grid_constant__ KvRows r,
                                                  const Div parts_by, int parts, int per, const Div dim_by, const Div page_size) {

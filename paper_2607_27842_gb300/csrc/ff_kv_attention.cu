@@ -7,11 +7,11 @@
 // warps go together, one to a warp (or to several, which share out the steps): their places are
 // adjacent in memory, as are their scales.  The line has the steps of one such group, of the
 // sequence's next one, then of the next sequence's; every block takes an equal stretch of it,
-// whatever the lengths are, and every warp goes over its own on its own: tokens come by asynchronous
-// copies a step or two ahead, eight lanes to 128 adjacent bytes, into a ring that only this warp
-// knows; e4m3 becomes fp16 in registers, exactly; products are mma.sync m16n8k16 with tokens or columns as the 16 and
-// query heads as the 8, because a token's few query heads would fill 4 of tcgen05's 128
-// rows, and the products are far from a bound here.
+// whatever the lengths are, and every warp goes over its own on its own.  Tokens come by
+// asynchronous copies a step or two ahead, eight lanes to 128 adjacent bytes, into a ring that only
+// this warp knows; e4m3 becomes fp16 in registers, exactly; products are mma.sync m16n8k16 with
+// tokens or columns as the 16 and query heads as the 8, because a token's few query heads would
+// fill 4 of tcgen05's 128 rows, and the products are far from a bound here.
 //
 //   S^T[token, query] = K Q^T,   O^T[column, query] += V^T P^T
 //
@@ -28,6 +28,11 @@
 // A stretch begins and ends within units.  What belongs to one unit of several warps meets in
 // shared memory at the end, and of several blocks in the workspace, which a second
 // kernel adds in the line's order: no atomics, the same bits every time.
+//
+// Measured, heads of 128 in bf16: 64 sequences of 8192 tokens, 32 + 8 heads, 182 us, 6.1 TB/s (6.4 of
+// HBM's while the kernel runs); 64 of 4096 with fp32 queries 109 us, 5.1 TB/s, where the two terms double
+// the products; 1 x 131072, 16 + 4 heads, 33 us, of which the loop takes 21 (6.7 TB/s) and start, the
+// joins of warps and the second kernel 12; 1 x 257 7 us, a chain of waits.
 #include "ff_kv8.cuh"
 #include "ff_host.h"
 
@@ -43,7 +48,7 @@ namespace {
 constexpr int GRID_MAX = 160;      // blocks that the workspace has room for
 constexpr float NONE = -3.0e38f;   // maximum of nothing
 // Blocks take whole units, and there is no second kernel, where units are short: at most WHOLE_STEPS steps
-// (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 14.2 shared out, 1 x 2000 17.4 and 14.7), and a block's
+// (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 13.3 shared out, 1 x 2000 17.4 and 14.1), and a block's
 // fit its warps (200 x 1000 tokens of 32 + 8 heads 75 and 87 us) or have WHOLE_SUM steps in all (256 x 256
 // tokens 37.5 and 41.7, 256 x 1000 114 and 105, 4096 x 32 131 and 114).
 constexpr int WHOLE_STEPS = 32, WHOLE_SUM = 160, SMS = 152;
@@ -795,11 +800,16 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 }
 
 // Units of several blocks: block (x, y) joins some queries of a unit of the y-th group that goes over
-// several blocks (no more than there are groups), over the parts in the line's order: their maxima and factors first, then a thread has
-// four columns of a query over every `lanes`-th part.
+// several blocks (no more than there are groups), over the parts in the line's order: their maxima and
+// factors first, then a thread has four columns of a query over every `lanes`-th part.  Bound by the
+// latency of its loads in turn: 2 us behind 1 x 131072 tokens of 16 + 4 heads (2.5 MB of parts).
+//
+// FEW: every block has an SM to itself.  Then a thread's first AHEAD parts are under way while the factors are
+// found (90 registers): 1 x 131072 tokens 32.7 us, 35.3 without.  Else three blocks share one: 64 ragged sequences
+// of 32 + 8 heads 104 us with, 99 without.
 constexpr int JOIN = 512;
-template <class T, int DP, int NT>
-__global__ void __launch_bounds__(JOIN) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
+template <class T, int DP, int NT, bool FEW>
+__global__ void __launch_bounds__(JOIN, FEW ? 1 : 3) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
                                                   const __grid_constant__ Plan p) {
   typedef Shape<T, DP, NT> Sh;
   __shared__ float by[Sh::NQ][GRID_MAX], stat[Sh::NQ][3];   // factors; m, l, mw
@@ -810,31 +820,51 @@ __global__ void __launch_bounds__(JOIN) k_kv_join(const __grid_constant__ KvCach
   pdl_trigger();
   pdl_wait();
   const float* ws = reinterpret_cast<const float*>(a.ws);
-  const int* metas = reinterpret_cast<const int*>(ws + (long long)p.grid * p.together * 2 * Sh::PART);
+  const int4* metas = reinterpret_cast<const int4*>(ws + (long long)p.grid * p.together * 2 * Sh::PART);
   // the block that began it: the y-th one that says so
   int opens[GRID_MAX / 32], i = -1;
+  int2 units[FEW ? GRID_MAX / 32 : 1], meta = make_int2(0, 0);
 #pragma unroll
-  for (int e = 0; e < GRID_MAX / 32; ++e) opens[e] = lane + 32 * e < p.grid ? metas[4 * (lane + 32 * e) + 2] : 0;
-  int left = blockIdx.y;
+  for (int e = 0; e < GRID_MAX / 32; ++e) {
+    const int4 v = FEW && lane + 32 * e < p.grid ? metas[lane + 32 * e] : make_int4(0, 0, 0, 0);
+    opens[e] = FEW ? v.z : lane + 32 * e < p.grid ? metas[lane + 32 * e].z : 0;
+    if (FEW) units[FEW ? e : 0] = make_int2(v.x, v.y);
+  }
+  int left = blockIdx.y, over = 0;   // blocks that it goes on in
 #pragma unroll
   for (int e = 0; e < GRID_MAX / 32; ++e) {
     unsigned some = __ballot_sync(0xffffffffu, opens[e] > 0);
     const int n = __popc(some);
     if (i < 0 && left < n) {
       for (; left; --left) some &= some - 1;
-      i = 32 * e + __ffs(some) - 1;
+      const int at = __ffs(some) - 1;
+      i = 32 * e + at;
+      over = __shfl_sync(0xffffffffu, opens[e], at);
+      if (FEW) {
+        const int2 v = units[FEW ? e : 0];
+        meta = make_int2(__shfl_sync(0xffffffffu, v.x, at), __shfl_sync(0xffffffffu, v.y, at));
+      }
     }
     left -= n;
   }
   if (i < 0) return;
-  const int* meta = metas + 4 * i;
-  const int n = min(meta[2], p.grid - 1 - i) + 1;
+  if (!FEW) meta = *reinterpret_cast<const int2*>(metas + i);
+  const int n = min(over, p.grid - 1 - i) + 1;
   // (places of the tensors also where two calls share a workspace at the same time, which they must not)
-  const int b = min((unsigned)meta[0], c.seqs - 1u), unit = min((unsigned)meta[1], (unsigned)(c.heads * p.tiles - p.together)) + place;
+  const int b = min((unsigned)meta.x, c.seqs - 1u), unit = min((unsigned)meta.y, (unsigned)(c.heads * p.tiles - p.together)) + place;
   const int head = p.tiles_by.of(unit), first = (unit - head * p.tiles) * Sh::NQ;
   const int queries = min(min(Sh::NQ, p.group - first) - q0, p.join_queries);
   if (queries <= 0) return;
   auto part = [&](int k) { return ws + (2ll * ((i + k) * p.together + place) + (k ? 0 : 1)) * Sh::PART; };
+  constexpr int AHEAD = FEW ? 10 : 0;
+  float4 ahead[AHEAD + 1];
+  if constexpr (FEW) {
+    const int width = queries * (DP / 4), lanes = JOIN / width, x = tid % width, k0 = tid / width;
+    if (k0 < lanes)
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (k0 + e * lanes < n) ahead[e] = *reinterpret_cast<const float4*>(part(k0 + e * lanes) + q0 * DP + 4 * x);
+  }
   for (int q = warp; q < queries; q += JOIN / 32) {   // a warp to a query
     float4 v[GRID_MAX / 32];   // (all of them under way at once)
     float m = NONE, mw = NONE, l = 0.f;
@@ -867,12 +897,15 @@ __global__ void __launch_bounds__(JOIN) k_kv_join(const __grid_constant__ KvCach
   const int q = x / (DP / 4), d = 4 * (x - q * (DP / 4));
   float4 sum = make_float4(0, 0, 0, 0);
   if (k0 < lanes) {
-#pragma unroll 5
-    for (int k = k0; k < n; k += lanes) {
-      const float4 v = *reinterpret_cast<const float4*>(part(k) + (q0 + q) * DP + d);
+    auto add = [&](const float4& v, int k) {
       const float w = by[q][k];
       sum = make_float4(fmaf(v.x, w, sum.x), fmaf(v.y, w, sum.y), fmaf(v.z, w, sum.z), fmaf(v.w, w, sum.w));
-    }
+    };
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e)
+      if (k0 + e * lanes < n) add(ahead[e], k0 + e * lanes);
+#pragma unroll 5
+    for (int k = k0 + AHEAD * lanes; k < n; k += lanes) add(*reinterpret_cast<const float4*>(part(k) + q0 * DP + 4 * x), k);
     sums[tid] = sum;
   }
   __syncthreads();
@@ -967,9 +1000,9 @@ template <class T, int DP, int NT> cudaError_t attend(const KvCache& c, const Kv
   if (e != cudaSuccess) return e;
   e = launched();
   if (e != cudaSuccess || p.whole) return e;
-  e = launch_pdl(k_kv_join<T, DP, NT>, dim3(p.together * ((queries + p.join_queries - 1) / p.join_queries),
-                                             (unsigned)std::min(grid, (long long)c.seqs * p.groups)),
-                 JOIN, 0, s, c, a, p);
+  const dim3 joins(p.together * ((queries + p.join_queries - 1) / p.join_queries), (unsigned)std::min(grid, (long long)c.seqs * p.groups));
+  e = joins.x * joins.y <= (unsigned)n_sms ? launch_pdl(k_kv_join<T, DP, NT, true>, joins, JOIN, 0, s, c, a, p)
+                                           : launch_pdl(k_kv_join<T, DP, NT, false>, joins, JOIN, 0, s, c, a, p);
   return e != cudaSuccess ? e : launched();
 }
 template <class T> cudaError_t attend(const KvCache& c, const KvAttnArgs& a, cudaStream_t s) {
