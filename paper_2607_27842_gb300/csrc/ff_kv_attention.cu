@@ -48,9 +48,9 @@ namespace {
 constexpr int GRID_MAX = 160;      // blocks that the workspace has room for
 constexpr float NONE = -3.0e38f;   // maximum of nothing
 // Blocks take whole units, and there is no second kernel, where units are short: at most WHOLE_STEPS steps
-// (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 13.3 shared out, 1 x 2000 17.4 and 14.1), and a block's
-// fit its warps (200 x 1000 tokens of 32 + 8 heads 75 and 87 us) or have WHOLE_SUM steps in all (256 x 256
-// tokens 37.5 and 41.7, 256 x 1000 114 and 105, 4096 x 32 131 and 114).
+// (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 13.6 shared out, 1 x 2000 17.3 and 14.0), and a block's
+// fit its warps (200 x 1000 tokens of 32 + 8 heads 73 and 86 us) or have WHOLE_SUM steps in all (256 x 256
+// tokens 36.3 and 41.6, 256 x 1000 106 and 104, 4096 x 32 130 and 115).
 constexpr int WHOLE_STEPS = 32, WHOLE_SUM = 160, SMS = 152;
 bool whole_units(long long units, long long steps, int warps) {
   return steps <= WHOLE_STEPS && (units <= (long long)SMS * warps || units * steps <= SMS * WHOLE_SUM);
@@ -61,7 +61,7 @@ template <class E, int DP, int NT> struct Shape {
   // warps of a block: as many as have the registers for their sums and queries.  A spilled register
   // in the loop goes through the 20 KB of L1 that the rings leave: 64 x 8192 tokens took 221 us with
   // 16 warps of 128 registers (80 bytes spilled), 189 with 12 of 168, 206 with 8; 64 x 4096 in fp32 123 with
-  // 8 and 109 with 12.
+  // 8 and 109 with 12, though 88 bytes spill.
   static constexpr int WARPS = NT > 1 || DP == 256 ? 8 : DP == 64 && sizeof(E) == 2 ? 16 : 12;
   static constexpr int MT = DP == 256 ? 1 : 2;                 // groups of 16 tokens in a step
   static constexpr int T = 16 * MT;
