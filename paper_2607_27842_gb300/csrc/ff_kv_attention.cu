@@ -805,7 +805,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 // latency of its loads in turn: 2 us behind 1 x 131072 tokens of 16 + 4 heads (2.5 MB of parts).
 //
 // FEW: every block has an SM to itself.  Then a thread's first AHEAD parts are under way while the factors are
-// found (90 registers): 1 x 131072 tokens 32.7 us, 35.3 without.  Else three blocks share one: 64 ragged sequences
+// found (114 registers): 1 x 131072 tokens 32.7 us, 35.3 without.  Else three blocks share one: 64 ragged sequences
 // of 32 + 8 heads 104 us with, 99 without.
 constexpr int JOIN = 512;
 template <class T, int DP, int NT, bool FEW>
