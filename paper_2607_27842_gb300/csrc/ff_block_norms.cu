@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
   };
 
   // Mean (0 where the norm has none) and 1 / root mean square of a row's columns, the which-th norm of the
-  // row; a warp finds its own mean and squares around it first.
+  // row; a warp finds its own mean and squares around it first.  A warp that writes one norm's sums has passed the
+  // other's barrier, behind which all have read the row before's.
   auto held = [&](int k) { return (float)max(0, min(C, (k + 1) * NB * 256) - k * NB * 256); };   // columns of a warp
   const float per_col = 1.f / (float)C, mine = held(w), per_mine = mine > 0.f ? 1.f / mine : 0.f;
   auto norm = [&](const f32x2 (&v)[NB][4], int which) {
@@ -182,7 +183,9 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
   T* o = reinterpret_cast<T*>(a.out) + (first + slot) * a.ldo + c0;
   uint8_t* o8 = reinterpret_cast<uint8_t*>(a.q8.q) + (first + slot) * a.q8.ldq + c0;
   float* sp = a.q8.scale + (long long)(w * NB * 2 + (lane >> 4)) * a.q8.lds + first + slot;
+  const bool alone = W > 1 && !(a.norm_after && (Q8 || a.out));   // one norm to a row: it has no other's barrier
   for (long long r = first + slot; r < end; r += slots) {
+    if (alone) slot_sync(slot, W);
     f32x2 h[NB][4], res[NB][4];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
@@ -318,9 +321,11 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
   auto within = [&](f32x2 v, int i, int k) -> f32x2 {
     return 128 * i + 64 * k + 32 < left ? v : 128 * i + 64 * k < left ? f2u(lo_f(v), 0.f) : 0;
   };
-  // mean (0 where the norm has none) and 1 / root mean square of a row's columns, the which-th of the
-  // row; a warp finds its own mean and squares around it first
-  auto norm = [&](const f32x2 (&v)[NB][2], int which) {
+  // mean (0 where the norm has none) and 1 / root mean square of a row's columns; a warp finds its own mean and
+  // squares around it first; two places take turns, so that a warp that writes one has passed the barrier behind
+  // which all others had read it
+  int turn = 0;
+  auto norm = [&](const f32x2 (&v)[NB][2]) {
     float mean = 0.f, ss;
     f32x2 sum = 0;
     if (a.centered) {
@@ -342,15 +347,17 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
     }
     ss = warp_sum(lo_f(sum) + hi_f(sum));
     if (W > 1) {
-      if (lane == 0) red[which][warp] = make_float2(mean, ss);
+      float2* of = red[turn];
+      turn ^= 1;
+      if (lane == 0) of[warp] = make_float2(mean, ss);
       slot_sync(slot, W);
       float all = 0.f, m = 0.f;
       if (a.centered) {
-        for (int k = 0; k < W; ++k) m += red[which][warp - w + k].x * (float)max(0, min(C, (k + 1) * NB * 128) - k * NB * 128);
+        for (int k = 0; k < W; ++k) m += of[warp - w + k].x * (float)max(0, min(C, (k + 1) * NB * 128) - k * NB * 128);
         m /= (float)C;
       }
       for (int k = 0; k < W; ++k) {
-        const float2 o = red[which][warp - w + k];
+        const float2 o = of[warp - w + k];
         all += o.y;
         if (a.centered) all = fmaf((o.x - m) * (o.x - m), (float)max(0, min(C, (k + 1) * NB * 128) - k * NB * 128), all);
       }
@@ -402,7 +409,7 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
     }
     if (KEEP && r + 1 < r1) load_row();
     f32x2 by = one;
-    if (a.norm_after) by = normed(h, norm(h, 0));
+    if (a.norm_after) by = normed(h, norm(h));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       if constexpr (!KEEP) make_p(i, p[0]);
@@ -412,7 +419,7 @@ __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long
     }
     sm += a.ldsum;
     if (!Q8 && !a.out) continue;
-    by = normed(h, norm(h, 1));
+    by = normed(h, norm(h));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       if constexpr (!KEEP) make_qs(i, q[0], s[0]);

@@ -181,6 +181,20 @@ def test_large_means_and_special_rows(cuda):
     assert out[~bad].isfinite().all() and qs[:, ~bad].isfinite().all() and qs[:, 3].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C,extra", [(4099, 2048, 0), (2501, 1001, 1), (700, 8192, 0), (300, 16384, 0), (305, 9001, 0)])
+@pytest.mark.parametrize("after", [False, True])
+def test_one_norm_to_a_row(cuda, dtype, rows, C, extra, after):
+    """Rows of several warps with a single norm each (the one before the block, or the one after it and the sum
+    alone): sums of adjacent rows, a thousandfold apart, do not meet."""
+    t = inputs(rows, C, TD[dtype], extra, 1, 51, ("y", "x") if after else ("y", "weight"))
+    t["y"][::2] *= 1000
+    first = run(dtype, t, after=after, result=None if after else "out", extra=extra, sum_out=after)
+    for _ in range(5):
+        again = run(dtype, t, after=after, result=None if after else "out", extra=extra, sum_out=after)
+        assert all((again[n] == first[n]).all() for n in first)
+
+
 def test_no_rows(cuda):
     x = torch.empty((0, 64), device="cuda")
     n0 = ff.featfix_launch_count()
