@@ -61,9 +61,8 @@ template <class T> struct Cols {
 // the next row's loads under way meanwhile.  Weights and modulation enter as three factors of a
 // column, h = resid_scale x + p norm(y), z = q norm(h) + s, from shared memory: read from L2 for every
 // row they are three times the bytes of x and y, and in registers (48 for 512 columns) they leave 16 warps
-// to an SM, which do not hide the two norms' latencies (14566 x 2048: 99 us).  Now 38 us there with modulation and
-// 8-bit output, 5.5 TB/s, where warps wait for shared memory and for each other's sums; 14566 x 4096 74 us,
-// 5.7 TB/s; fp32 88 us.
+// to an SM, which do not hide the two norms' latencies (14566 x 2048: 99 us).  Now 36 us there with modulation and
+// 8-bit output, 5.8 TB/s, where warps wait for shared memory and for each other's sums; 4000 x 8192 51 us; fp32 88 us.
 template <class T, int NB, bool Q8>
 __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
     k_block_norms(long long rows, int C, int W, long long per, int chunks, const __grid_constant__ BlockNormsArgs a) {
@@ -100,13 +99,61 @@ __global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
 #pragma unroll
   for (int i = 0; i < NB; ++i) fy[i].zero(), fx[i].zero();
   if (first + slot < end) load_row();
-  for (int c = threadIdx.x; c < wide; c += 256) {
-    const int at = (c & ~255) + (c & 4) * 32 + (c & 248) / 2 + (c & 3);
+  // Factors of eight adjacent columns at a time: every load of them is under way before the first is used
+  // (column by column 4000 x 8192 took 62 us, 51 so).
+  auto eight = [&](const float* m, float (&v)[8]) {
+    if (!((uintptr_t)m & 15)) {
+      const float4 l = reinterpret_cast<const float4*>(m)[0], h = reinterpret_cast<const float4*>(m)[1];
+      v[0] = l.x, v[1] = l.y, v[2] = l.z, v[3] = l.w, v[4] = h.x, v[5] = h.y, v[6] = h.z, v[7] = h.w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = m[k];
+    }
+  };
+  auto eight_of = [&](const void* m, int c, Cols<T>& v) {
+    const T* p = reinterpret_cast<const T*>(m) + c;
+    if (!((uintptr_t)p & 15)) {
+      v.load(p);
+    } else {
+      __align__(16) T e[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e[k] = p[k];
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) v.r[k] = reinterpret_cast<const uint4*>(e)[k];
+    }
+  };
+  for (int c = 8 * threadIdx.x; c < wide; c += 2048) {
     const bool there = c < C;
-    auto weight = [&](const void* m) { return m && there ? to_f(reinterpret_cast<const T*>(m)[c]) : 1.f; };
-    fp[at] = (a.gate && there ? a.gate[sample * a.gate_stride + c] : 1.f) * weight(a.weight_after);
-    fq[at] = (a.scale && there ? 1.f + a.scale[sample * a.scale_stride + c] : 1.f) * weight(a.weight);
-    if (has_s) fs[at] = there ? a.shift[sample * a.shift_stride + c] : 0.f;
+    float g[8], sc[8], sh[8];
+    Cols<T> wa, wb;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[k] = 1.f, sc[k] = sh[k] = 0.f;
+    if (a.gate && there) eight(a.gate + sample * a.gate_stride + c, g);
+    if (a.scale && there) eight(a.scale + sample * a.scale_stride + c, sc);
+    if (has_s && there) eight(a.shift + sample * a.shift_stride + c, sh);
+    if (a.weight_after && there) eight_of(a.weight_after, c, wa);
+    if (a.weight && there) eight_of(a.weight, c, wb);
+    f32x2 p[4], q[4], f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = f2u(g[2 * k], g[2 * k + 1]), q[k] = f2u(1.f + sc[2 * k], 1.f + sc[2 * k + 1]);
+    if (a.weight_after && there) {
+      wa.get(f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = fmul2(p[k], f[k]);
+    }
+    if (a.weight && there) {
+      wb.get(f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) q[k] = fmul2(q[k], f[k]);
+    }
+    const int at = (c & ~255) + (c & 248) / 2;   // the first four; the others 128 places behind
+    auto put = [&](float* to, f32x2 v0, f32x2 v1, f32x2 v2, f32x2 v3) {
+      *reinterpret_cast<ulonglong2*>(to + at) = make_ulonglong2(v0, v1);
+      *reinterpret_cast<ulonglong2*>(to + at + 128) = make_ulonglong2(v2, v3);
+    };
+    put(fp, p[0], p[1], p[2], p[3]);
+    put(fq, q[0], q[1], q[2], q[3]);
+    if (has_s) put(fs, f2u(sh[0], sh[1]), f2u(sh[2], sh[3]), f2u(sh[4], sh[5]), f2u(sh[6], sh[7]));
   }
   if (threadIdx.x < 64) sums[0][0][threadIdx.x] = sums[0][1][threadIdx.x] = sums[1][0][threadIdx.x] = sums[1][1][threadIdx.x] = 0.f;
   __syncthreads();
