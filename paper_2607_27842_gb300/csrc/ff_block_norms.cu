@@ -63,8 +63,13 @@ template <class T> struct Cols {
 // row they are three times the bytes of x and y, and in registers (48 for 512 columns) they leave 16 warps
 // to an SM, which do not hide the two norms' latencies (14566 x 2048: 99 us).  Now 36 us there with modulation and
 // 8-bit output, 5.8 TB/s, where warps wait for shared memory and for each other's sums; 4000 x 8192 51 us; fp32 88 us.
+//
+// Blocks to an SM: as many as leave a lane the registers for its pieces of the two rows.  In fp32 three blocks
+// of two pieces (80 registers, 130 bytes spilled) take 89.5 us for 14566 x 2048 and 188 for x 4096, two 85 and 151;
+// two of four pieces (350 bytes spilled) 130 for 4000 x 8192, one 91.
+template <class T, int NB> constexpr int NORMS_BLOCKS = NB * (int)sizeof(T) <= 4 ? 3 : NB * (int)sizeof(T) <= 12 ? 2 : 1;
 template <class T, int NB, bool Q8>
-__global__ void __launch_bounds__(256, NB <= 2 ? 3 : NB <= 4 ? 2 : 1)
+__global__ void __launch_bounds__(256, NORMS_BLOCKS<T, NB>)
     k_block_norms(long long rows, int C, int W, long long per, int chunks, const __grid_constant__ BlockNormsArgs a) {
   extern __shared__ __align__(16) float factors[];   // p, q, s: pieces of two halves, a lane's four columns each
   __shared__ __align__(16) float sums[2][2][64];   // of a slot's warps (8 places to a slot, 0 where it has fewer): squares, means
@@ -536,7 +541,7 @@ template <class T, int NB, bool Q8> cudaError_t norms_nb(int W, long long rows, 
   });
   if (e != cudaSuccess) return e;
   // rows of a sample in chunks: as many blocks as the SMs hold at once, or a row to a slot
-  const long long samples = (rows + a.rpb - 1) / a.rpb, held = 152ll * (NB <= 2 ? 3 : NB <= 4 ? 2 : 1);
+  const long long samples = (rows + a.rpb - 1) / a.rpb, held = 152ll * NORMS_BLOCKS<T, NB>;
   const long long of_sample = std::min<long long>(rows, a.rpb), want = std::max(1ll, held / samples);
   const long long per = std::max<long long>(slots, ((of_sample + want - 1) / want + slots - 1) / slots * slots);
   const long long chunks = (of_sample + per - 1) / per;
@@ -551,11 +556,11 @@ template <class T, bool Q8> cudaError_t norms(long long rows, int C, const Block
   if (few || C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
     return norms_any<T, Q8>(rows, C, a, s);
   const int pieces = (C + 255) / 256;
-  // Warps to a row: four pieces to a warp (fp32: two; three where they leave fewer lanes idle), fewer while
-  // the rows alone leave the SMs without 8 warps each.  14566 x 2048 with modulation and 8-bit output
-  // 38.0 us with four, 45.8 with two (three blocks to an SM instead of two), 41.8 with eight (one block);
-  // fp32 93.6, 88.6 and 87.4.
-  constexpr int PREF = sizeof(T) == 2 ? 4 : 2;
+  // Warps to a row: four pieces to a warp (three where they leave fewer lanes idle), fewer while the rows
+  // alone leave the SMs without 8 warps each.  14566 x 2048 with modulation and 8-bit output 35.8 us with four, 38.9
+  // with eight (one block to an SM), before the factors' present form 38.0 and 45.8 with two; fp32 85.3, with two
+  // 84.5, centered 79.5 and 86.5.
+  constexpr int PREF = 4;
   int W = 1;
   while (W < 8 && (pieces > PREF * W || (rows * W < 152 * 8 && pieces > W))) W *= 2;
   if (W > 1 && pieces <= 3 * (W / 2) && rows * (W / 2) >= 152 * 8) W /= 2;
