@@ -62,7 +62,7 @@ template <class T> struct Cols {
 // column, h = resid_scale x + p norm(y), z = q norm(h) + s, from shared memory: read from L2 for every
 // row they are three times the bytes of x and y, and in registers (48 for 512 columns) they leave 16 warps
 // to an SM, which do not hide the two norms' latencies (14566 x 2048: 99 us).  Now 36 us there with modulation and
-// 8-bit output, 5.8 TB/s, where warps wait for shared memory and for each other's sums; 4000 x 8192 51 us; fp32 88 us.
+// 8-bit output, 5.8 TB/s, where warps wait for shared memory and for each other's sums; 4000 x 8192 51 us; fp32 85 us.
 //
 // Blocks to an SM: as many as leave a lane the registers for its pieces of the two rows.  In fp32 three blocks
 // of two pieces (80 registers, 130 bytes spilled) take 89.5 us for 14566 x 2048 and 188 for x 4096, two 85 and 151;
