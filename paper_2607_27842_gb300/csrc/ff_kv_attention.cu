@@ -20,10 +20,11 @@
 // product 16 adjacent columns of values 2j, 2j + 1, 2j + 8, 2j + 9, whole 16-byte vectors in the
 // order of memory.  P^T turns from the one's result to the other's operand in movmatrix.
 //
-// Softmax with a running maximum m of the scores x (in powers of two).  The weights p * scale_v
-// go to fp16, times 2^(m + 15 - mw) with a running maximum mw of x + log2(scale_v): the largest
-// weight uses all of fp16's range whatever the scales are, and weights 2^-29 below it still
-// have 11 bits.  The softmax's sum takes p = exp2(x - m) in fp32.
+// Softmax with a running maximum m of the scores x (in powers of two).  Its sum l takes p = exp2(x - m) in
+// fp32.  The weights p * scale_v go to fp16, times the power of two that brings the largest of them so far,
+// w, to 2^14 .. 2^15: they use all of fp16's range whatever the scales are, and weights 2^-28 below the
+// largest still have 11 bits.  w is kept relative to m, as l is: a sum x + log2(scale_v) would lose the
+// scale in the rounding of large x (from 2^24 on more than a factor of two, past fp16's largest number).
 //
 // A stretch begins and ends within units.  What belongs to one unit of several warps meets in
 // shared memory at the end, and of several blocks in the workspace, which a second
@@ -73,7 +74,7 @@ template <class E, int DP, int NT> struct Shape {
   static constexpr int STAGE = T * DP * 2 + T * 8 + 16;        // keys, values, scales, mask
   static constexpr int RING = STAGE * STAGES;                  // of a warp
   static constexpr int NQ = 8 * NT;
-  static constexpr int PART = NQ * (DP + 4);                   // floats: sums, then m, l, mw of each query
+  static constexpr int PART = NQ * (DP + 4);                   // floats: sums, then m, l, w of each query
   static constexpr int SMEM = WARPS * (RING + PART * 4);
   static_assert(PART * 4 <= RING, "the second partial result lies in the ring");
   static_assert(STAGE % 16 == 0 && PART % 4 == 0, "whole vectors");
@@ -114,11 +115,14 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float lg2(float x) {
-  float r;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
+// Weights up to w, of exponent e = top_exp(w), are below 2^15 times raised(e) = 2^(141 - e); lowered(e) is
+// 1 / raised(e).  (Weights all below 2^-111 come from scales that no written token has.)
+__device__ __forceinline__ int top_exp(float w) { return max(15, (int)(__float_as_uint(w) >> 23)); }
+__device__ __forceinline__ float raised(int e) { return __int_as_float((268 - e) << 23); }
+__device__ __forceinline__ float lowered(int e) { return __int_as_float((e - 14) << 23); }
+// 2^(from - to): turns sums of weights raised by `from` into such raised by `to`.  (Past 2^127 the factor that it
+// goes with has become 0; below 2^-126 nothing is left of the sums beside weights of 2^14.)
+__device__ __forceinline__ float moved(int from, int to) { return __int_as_float((max(-126, min(127, from - to)) + 127) << 23); }
 __device__ __forceinline__ unsigned half2_bits(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&h);
@@ -231,10 +235,8 @@ __device__ __forceinline__ void store_row(T* out, int pairs, int col, int dim, f
     if (col + 1 < dim) out[col + 1] = from_f<T>(y);
   }
 }
-// 2^(mw - m - 15) / l, by which sums become results; 0 for a row of no tokens
-__device__ __forceinline__ float closing(float m, float l, float mw) {
-  return l == 0.f ? 0.f : ex2(mw - m - 15.f) / l;
-}
+// By which sums become results; 0 for a row of no tokens.
+__device__ __forceinline__ float closing(float l, float w) { return l == 0.f ? 0.f : lowered(top_exp(w)) / l; }
 __device__ __forceinline__ float lse_of(float m, float l) {
   return l == 0.f ? __int_as_float(0xff800000) : (m + log2f(l)) * 0.69314718055994531f;
 }
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     };
     unsigned qf[NT][TERMS][DP / 16][2];
     float qs[NT][2];                         // of queries 2j, 2j + 1: what a product is multiplied by
-    float m[NT][2], l[NT][2], mw[NT][2], o[NT][DP / 16][4];
+    float m[NT][2], l[NT][2], w[NT][2], o[NT][DP / 16][4];   // (w: see above)
     // Queries of the unit at `at`, as they are in memory: of query g of the tile four adjacent columns
     // for each 16 of the sum.
     auto load_queries = [&] {
@@ -470,8 +472,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             qs[nt][e] = __shfl_sync(0xffffffffu, down, (2 * j + e) * 4) * p.scale;
-            m[nt][e] = mw[nt][e] = NONE;
-            l[nt][e] = 0.f;
+            m[nt][e] = NONE;
+            l[nt][e] = w[nt][e] = 0.f;
           }
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i)
@@ -534,107 +536,107 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       const char* st = ring + stage * Sh::STAGE;
       const float* sc = reinterpret_cast<const float*>(st + Sh::T * DP * 2);
 
-      float sv[Sh::MT][2];   // (of masked tokens 0)
-      float top[NT][2], topw[NT][2];
+      float by[NT][2];   // exp2 of what m grows by, negative
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) top[nt][e] = topw[nt][e] = NONE;
+        for (int e = 0; e < 2; ++e) {
+          float top = m[nt][e];
+#pragma unroll
+          for (int mt = 0; mt < Sh::MT; ++mt) top = fmaxf(top, fmaxf(s[mt][nt][e], s[mt][nt][2 + e]));
+#pragma unroll
+          for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+          by[nt][e] = ex2(m[nt][e] - top);
+          m[nt][e] = top;
+        }
+      // p, its sum, and the weights p * scale_v (of masked tokens 0)
+      float topw[NT][2], sum[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) topw[nt][e] = sum[nt][e] = 0.f;
 #pragma unroll
       for (int mt = 0; mt < Sh::MT; ++mt)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int k = 16 * mt + 8 * r + g;
-          sv[mt][r] = sc[Sh::T + k];
-          const float lsv = lg2(sv[mt][r]);
+          const float sv = sc[Sh::T + 16 * mt + 8 * r + g];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float x = s[mt][nt][2 * r + e];
-              top[nt][e] = fmaxf(top[nt][e], x);
-              topw[nt][e] = fmaxf(topw[nt][e], x + lsv);
+              float& x = s[mt][nt][2 * r + e];
+              const float pr = ex2(x - m[nt][e]);
+              sum[nt][e] += pr;
+              x = pr * sv;
+              topw[nt][e] = fmaxf(topw[nt][e], x);
             }
         }
       bool grew = false;
+      int from[NT][2], to[NT][2];   // exponents that sums and weights are raised by
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
-          for (int k = 4; k < 32; k <<= 1) {
-            top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], k));
-            topw[nt][e] = fmaxf(topw[nt][e], __shfl_xor_sync(0xffffffffu, topw[nt][e], k));
-          }
-          grew |= top[nt][e] > m[nt][e] || topw[nt][e] > mw[nt][e];
+          for (int k = 4; k < 32; k <<= 1) topw[nt][e] = fmaxf(topw[nt][e], __shfl_xor_sync(0xffffffffu, topw[nt][e], k));
+          from[nt][e] = top_exp(w[nt][e]);
+          w[nt][e] = fmaxf(w[nt][e] * by[nt][e], topw[nt][e]);
+          to[nt][e] = top_exp(w[nt][e]);
+          l[nt][e] = fmaf(l[nt][e], by[nt][e], sum[nt][e]);
+          grew |= by[nt][e] != 1.f || from[nt][e] != to[nt][e];
         }
       if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float f[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float mn = fmaxf(m[nt][e], top[nt][e]), mwn = fmaxf(mw[nt][e], topw[nt][e]);
-            l[nt][e] *= ex2(m[nt][e] - mn);
-            f[e] = ex2(mw[nt][e] - mwn);
-            m[nt][e] = mn;
-            mw[nt][e] = mwn;
-          }
+          for (int e = 0; e < 2; ++e) f[e] = by[nt][e] * moved(from[nt][e], to[nt][e]);
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nt][i][e] *= f[e & 1];
         }
       }
-      float up[NT][2];   // 2^(m - mw + 15); bounded where all values are zeros
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) up[nt][e] = ex2(fminf(m[nt][e] - mw[nt][e] + 15.f, 126.f));
       unsigned pb[Sh::MT][NT][TERMS][2];
 #pragma unroll
-      for (int mt = 0; mt < Sh::MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt) {
+        const float up[2] = {raised(to[nt][0]), raised(to[nt][1])};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int mt = 0; mt < Sh::MT; ++mt)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            float w[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float pr = ex2(s[mt][nt][2 * r + e] - m[nt][e]);
-              l[nt][e] += pr;
-              w[e] = pr * up[nt][e] * sv[mt][r];
-            }
-            const unsigned hi = half2_bits(w[0], w[1]);
+            const float u = s[mt][nt][2 * r] * up[0], v = s[mt][nt][2 * r + 1] * up[1];
+            const unsigned hi = half2_bits(u, v);
             pb[mt][nt][0][r] = transposed8x8(hi);
             if constexpr (TERMS == 2) {
               const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              pb[mt][nt][1][r] = transposed8x8(half2_bits(w[0] - h.x, w[1] - h.y));
+              pb[mt][nt][1][r] = transposed8x8(half2_bits(u - h.x, v - h.y));
             }
           }
+      }
 
 #pragma unroll
       for (int mt = 0; mt < Sh::MT; ++mt)
 #pragma unroll
         for (int i = 0; i < Sh::NV; ++i) {
-          unsigned w[4][Sh::VB / 4];   // tokens 2j, 2j + 1, 2j + 8, 2j + 9: VB adjacent columns
+          unsigned vw[4][Sh::VB / 4];   // tokens 2j, 2j + 1, 2j + 8, 2j + 9: VB adjacent columns
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int row = 16 * mt + 8 * (r >> 1) + 2 * j + (r & 1), at = column<DP>(g, i * (Sh::VB / 2));
             const char* src = st + Sh::T * DP + place<DP, Sh::T>(row, at / 16) + at % 16;
             if constexpr (Sh::VB == 16) {
               const uint4 u = *reinterpret_cast<const uint4*>(src);
-              w[r][0] = u.x, w[r][1] = u.y, w[r][2] = u.z, w[r][3] = u.w;
+              vw[r][0] = u.x, vw[r][1] = u.y, vw[r][2] = u.z, vw[r][3] = u.w;
             } else {
               const uint2 u = *reinterpret_cast<const uint2*>(src);
-              w[r][0] = u.x, w[r][1] = u.y;
+              vw[r][0] = u.x, vw[r][1] = u.y;
             }
           }
 #pragma unroll
           for (int k = 0; k < Sh::VB / 4; ++k) {
             // bytes of two tokens side by side: a conversion makes a column's pair of tokens
-            const unsigned x[2] = {__byte_perm(w[0][k], w[1][k], 0x5140), __byte_perm(w[0][k], w[1][k], 0x7362)};
-            const unsigned y[2] = {__byte_perm(w[2][k], w[3][k], 0x5140), __byte_perm(w[2][k], w[3][k], 0x7362)};
+            const unsigned x[2] = {__byte_perm(vw[0][k], vw[1][k], 0x5140), __byte_perm(vw[0][k], vw[1][k], 0x7362)};
+            const unsigned y[2] = {__byte_perm(vw[2][k], vw[3][k], 0x5140), __byte_perm(vw[2][k], vw[3][k], 0x7362)};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const unsigned a0 = cvt_e4m3x2((unsigned short)x[h]), a1 = cvt_e4m3x2((unsigned short)(x[h] >> 16));
@@ -676,7 +678,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
             if (qi >= p.group) continue;
             const int qh = head * p.group + qi;
             T* out = reinterpret_cast<T*>(a.out) + at.b * a.ldo + (long long)qh * dim;
-            const float f = closing(m[nt][e], l[nt][e], mw[nt][e]);
+            const float f = closing(l[nt][e], w[nt][e]);
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) store_row(out, p.pairs, column<DP>(g, i), dim, o[nt][i][e] * f, o[nt][i][2 + e] * f);
             if (a.lse && g == 0) a.lse[(long long)at.b * a.q_heads + qh] = lse_of(m[nt][e], l[nt][e]);
@@ -697,7 +699,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
             for (int i = 0; i < DP / 16; ++i)
               *reinterpret_cast<float2*>(row + column<DP>(g, i)) = make_float2(o[nt][i][e], o[nt][i][2 + e]);
             if (g == 0)
-              *reinterpret_cast<float4*>(part + Sh::NQ * DP + 4 * (nt * 8 + 2 * j + e)) = make_float4(m[nt][e], l[nt][e], mw[nt][e], 0.f);
+              *reinterpret_cast<float4*>(part + Sh::NQ * DP + 4 * (nt * 8 + 2 * j + e)) = make_float4(m[nt][e], l[nt][e], w[nt][e], 0.f);
           }
         if (lane == 0) {
           part_of[2 * warp + which] = make_int2(at.b, 2 * at.unit + ends);
@@ -755,31 +757,32 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       }
       const int head = p.tiles_by.of(unit), qi = (unit - head * p.tiles) * Sh::NQ + q;
       if (qi >= p.group || (turns > 1 && nth++ % turns != turn)) continue;
-      const float4 v = mine ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, NONE, 0.f);
-      float m = v.x, mw = v.z;
+      const float4 v = mine ? *reinterpret_cast<const float4*>(part(lane) + Sh::NQ * DP + 4 * q) : make_float4(NONE, 0.f, 0.f, 0.f);
+      float m = v.x;
+#pragma unroll
+      for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+      const float less = ex2(v.x - m);
+      float l = v.y * less, w = v.z * less;
 #pragma unroll
       for (int k = 16; k; k >>= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-        mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, k));
+        l += __shfl_xor_sync(0xffffffffu, l, k);
+        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, k));
       }
-      const float by = ex2(v.z - mw);
-      float l = v.y * ex2(v.x - m);
-#pragma unroll
-      for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+      const float by = less * moved(top_exp(v.z), top_exp(w));
       const int qh = head * p.group + qi;
       T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * dim;
       float* to = ws + (2 * place + here) * Sh::PART;
       const bool done = here && ends;
-      const float f = done ? closing(m, l, mw) : 1.f;
+      const float f = done ? closing(l, w) : 1.f;
       for (int d = 4 * lane; d - 4 * lane < DP; d += 128) {
         const bool in = d < DP;
         float4 sum = make_float4(0, 0, 0, 0);
 #pragma unroll 4
         for (unsigned rest = all; rest; rest &= rest - 1) {
           const int r = __ffs(rest) - 1;
-          const float w = __shfl_sync(0xffffffffu, by, r);
+          const float f = __shfl_sync(0xffffffffu, by, r);
           const float4 x = in ? *reinterpret_cast<const float4*>(part(r) + q * DP + d) : make_float4(0, 0, 0, 0);
-          sum = make_float4(fmaf(x.x, w, sum.x), fmaf(x.y, w, sum.y), fmaf(x.z, w, sum.z), fmaf(x.w, w, sum.w));
+          sum = make_float4(fmaf(x.x, f, sum.x), fmaf(x.y, f, sum.y), fmaf(x.z, f, sum.z), fmaf(x.w, f, sum.w));
         }
         if (!in) continue;
         if (done) {
@@ -790,7 +793,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         }
       }
       if (lane == 0) {
-        if (!done) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, mw, 0.f);
+        if (!done) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, w, 0.f);
         else if (a.lse) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
       }
     }
@@ -812,7 +815,7 @@ template <class T, int DP, int NT, bool FEW>
 __global__ void __launch_bounds__(JOIN, FEW ? 1 : 3) k_kv_join(const __grid_constant__ KvCache c, const __grid_constant__ KvAttnArgs a,
                                                   const __grid_constant__ Plan p) {
   typedef Shape<T, DP, NT> Sh;
-  __shared__ float by[Sh::NQ][GRID_MAX], stat[Sh::NQ][3];   // factors; m, l, mw
+  __shared__ float by[Sh::NQ][GRID_MAX], stat[Sh::NQ][3];   // factors; m, l, w
   __shared__ float4 sums[JOIN];
   const int chunks = (min(Sh::NQ, p.group) + p.join_queries - 1) / p.join_queries;
   const int place = blockIdx.x / chunks, q0 = (blockIdx.x - place * chunks) * p.join_queries;
@@ -867,30 +870,32 @@ __global__ void __launch_bounds__(JOIN, FEW ? 1 : 3) k_kv_join(const __grid_cons
   }
   for (int q = warp; q < queries; q += JOIN / 32) {   // a warp to a query
     float4 v[GRID_MAX / 32];   // (all of them under way at once)
-    float m = NONE, mw = NONE, l = 0.f;
+    float m = NONE, w = 0.f, l = 0.f;
 #pragma unroll
     for (int e = 0; e < GRID_MAX / 32; ++e) {
-      v[e] = make_float4(NONE, 0.f, NONE, 0.f);
+      v[e] = make_float4(NONE, 0.f, 0.f, 0.f);
       if (lane + 32 * e < n) v[e] = *reinterpret_cast<const float4*>(part(lane + 32 * e) + Sh::NQ * DP + 4 * (q0 + q));
     }
 #pragma unroll
+    for (int e = 0; e < GRID_MAX / 32; ++e) m = fmaxf(m, v[e].x);
+#pragma unroll
+    for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+#pragma unroll
     for (int e = 0; e < GRID_MAX / 32; ++e) {
-      m = fmaxf(m, v[e].x);
-      mw = fmaxf(mw, v[e].z);
+      const float less = ex2(v[e].x - m);
+      l += v[e].y * less;
+      w = fmaxf(w, v[e].z * less);
+      v[e].x = less;
     }
 #pragma unroll
     for (int k = 16; k; k >>= 1) {
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-      mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, k));
+      l += __shfl_xor_sync(0xffffffffu, l, k);
+      w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, k));
     }
 #pragma unroll
-    for (int e = 0; e < GRID_MAX / 32; ++e) {
-      if (lane + 32 * e < n) by[q][lane + 32 * e] = ex2(v[e].z - mw);
-      l += v[e].y * ex2(v[e].x - m);
-    }
-#pragma unroll
-    for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
-    if (lane == 0) stat[q][0] = m, stat[q][1] = l, stat[q][2] = mw;
+    for (int e = 0; e < GRID_MAX / 32; ++e)
+      if (lane + 32 * e < n) by[q][lane + 32 * e] = v[e].x * moved(top_exp(v[e].z), top_exp(w));
+    if (lane == 0) stat[q][0] = m, stat[q][1] = l, stat[q][2] = w;
   }
   __syncthreads();
   const int width = queries * (DP / 4), lanes = JOIN / width, x = tid % width, k0 = tid / width;
@@ -916,7 +921,7 @@ __global__ void __launch_bounds__(JOIN, FEW ? 1 : 3) k_kv_join(const __grid_cons
   }
   const int qh = head * p.group + first + q0 + q;
   T* out = reinterpret_cast<T*>(a.out) + b * a.ldo + (long long)qh * c.head_dim;
-  const float f = closing(stat[q][0], stat[q][1], stat[q][2]);
+  const float f = closing(stat[q][1], stat[q][2]);
   store_row(out, p.pairs, d, c.head_dim, sum.x * f, sum.y * f);
   store_row(out, p.pairs, d + 2, c.head_dim, sum.z * f, sum.w * f);
   if (a.lse && d == 0) a.lse[(long long)b * a.q_heads + qh] = lse_of(stat[q][0], stat[q][1]);
