@@ -84,7 +84,7 @@ __device__ __forceinline__ Place place_of(const KvCache& c, const int* row_start
     back = row_start[b + 1] - (int)row;
     if (back <= 0) return {-1, 0, true};   // (starts that do not rise)
   }
-  const int t = kv_len(c, b) - back;
+  const int t = kv_len(c, c.lens[b]) - back;
   if (t < 0) return {-1, 0, false};
   const int n = page_size.of((unsigned)t), page = c.table[b * c.ld_table + n];
   return {(unsigned)page < (unsigned)c.pages ? page : -1, t - n * c.page_size, false};

@@ -63,10 +63,10 @@ struct Div {
   __device__ __forceinline__ int of(unsigned n) const { return (int)((__umulhi(m, n) + n) >> s); }
 };
 
-// Tokens of sequence b: what the table can hold at most.
-__device__ __forceinline__ int kv_len(const KvCache& c, int b) {
+// Tokens of a sequence, by its place in lens: what the table can hold at most.
+__device__ __forceinline__ int kv_len(const KvCache& c, int len) {
   const long long most = (long long)c.table_pages * c.page_size;
-  return (int)max(0ll, min((long long)c.lens[b], most));
+  return (int)max(0ll, min((long long)len, most));
 }
 
 // What a scale stands for: infinities and negative numbers are NaN (featfix_ops.h).

@@ -147,23 +147,37 @@ template <int DP> __device__ __forceinline__ int column(int g, int i) {
   return DP == 256 ? 128 * (i >> 3) + 16 * g + 2 * (i & 7) : DP / 8 * g + 2 * i;
 }
 
+// Lengths and page numbers may change while the kernel runs.  Results mean nothing then, but nothing may be
+// read or written out of range, nor lanes of a warp part.  So what a warp does by a length goes by lane 0's
+// load of it, a page number is one load, which the compiler may not repeat, and what either leads to is
+// bounded.  (4096 sequences of 32 tokens 114.4 -> 115.3 us.)
+__device__ __forceinline__ int shared_by_all(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ int once(const int* p) {
+  int v;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+
 // Tokens that sequence b's new token sees.
 struct Seen {
   int first, end;
 };
-__device__ __forceinline__ Seen seen(const KvCache& c, int window, int b) {
-  const int len = kv_len(c, b);
-  return {window && len > window ? len - window : 0, len};
-}
+__device__ __forceinline__ Seen seen_of(int len, int window) { return {window && len > window ? len - window : 0, len}; }
+__device__ __forceinline__ int len_of(const KvCache& c, int b) { return kv_len(c, c.lens[b]); }
+// (by a whole warp)
+__device__ __forceinline__ Seen seen(const KvCache& c, int window, int b) { return seen_of(shared_by_all(len_of(c, b)), window); }
 
 // Where a step of the line is: sequence, unit (as locate() finds it: group of units), step, and how
 // many steps the sequence has.
 struct Spot {
   int b, unit, step, steps;
 };
-template <int T> __device__ __forceinline__ int steps_seen(const KvCache& c, int window, int b) {
-  const Seen s = seen(c, window, b);
+template <int T> __device__ __forceinline__ int steps_of_lane(const KvCache& c, int window, int b) {
+  const Seen s = seen_of(len_of(c, b), window);
   return (s.end - s.first + T - 1) / T;
+}
+template <int T> __device__ __forceinline__ int steps_seen(const KvCache& c, int window, int b) {   // (by a whole warp)
+  return shared_by_all(steps_of_lane<T>(c, window, b));
 }
 
 // a / b for a >= 0, b > 0
@@ -185,7 +199,7 @@ template <int T> __device__ __forceinline__ Line line_up(const KvCache& c, int w
   long long n = 0;
 #pragma unroll 4
   for (int i = 0; i < per; ++i)
-    if (lane * per + i < c.seqs) n += steps_seen<T>(c, window, lane * per + i);
+    if (lane * per + i < c.seqs) n += steps_of_lane<T>(c, window, lane * per + i);
   n *= groups;
   long long sum = n;
 #pragma unroll
@@ -212,14 +226,16 @@ template <int T> __device__ __noinline__ Spot locate(const KvCache& c, int windo
 }
 
 // The warp's next unit that has steps: of the sequence's next group, or of the next sequence.
-template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, const Plan& p, int window, int u, Spot& s) {
+// `of` follows: what its sequence's new token sees.
+template <int T> __device__ __forceinline__ void next_unit(const KvCache& c, const Plan& p, int window, int u, Spot& s, Seen& of) {
   s.step = 0;
   s.unit += p.together;
   if (s.unit < c.heads * p.tiles) return;
   s.unit = u;
   do {
     if (s.b + 1 >= c.seqs) return;   // (as above: the line has an end before)
-    s.steps = steps_seen<T>(c, window, ++s.b);
+    of = seen(c, window, ++s.b);
+    s.steps = (of.end - of.first + T - 1) / T;
   } while (s.steps == 0);
 }
 
@@ -312,7 +328,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     auto page_of = [&](int t) { return p.page.of((unsigned)t); };
     auto look_up = [&] {
       const int t = token();
-      return t < in_seen.end ? c.table[in.b * c.ld_table + page_of(t)] : -1;
+      return (unsigned)t < (unsigned)in_seen.end ? once(c.table + in.b * c.ld_table + page_of(t)) : -1;
     };
     int entry = look_up();
     int stage_in = 0;
@@ -347,7 +363,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     auto issue_keys = [&] {
       if (to_issue > 0) {
         const int t = token();
-        const bool there = (unsigned)entry < (unsigned)c.pages && t < in_seen.end;
+        const bool there = (unsigned)entry < (unsigned)c.pages && (unsigned)t < (unsigned)in_seen.end;
         in_page = there ? entry : 0;
         in_slot = there ? t - page_of(t) * c.page_size : 0;
         in_mask = __ballot_sync(0xffffffffu, there);
@@ -374,8 +390,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         stage_in = stage_in + 1 == Sh::STAGES ? 0 : stage_in + 1;
         if (--to_issue > 0) {
           if (++in.step == in.steps) {
-            next_unit<Sh::T>(c, p, a.window, u, in);
-            in_seen = seen(c, a.window, in.b);
+            next_unit<Sh::T>(c, p, a.window, u, in, in_seen);
             heads_of(in.unit);
           }
           entry = look_up();
@@ -709,7 +724,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       begun = true;
       fresh = true;
       if (to_do > 0) {
-        next_unit<Sh::T>(c, p, a.window, u, at);
+        Seen of;
+        next_unit<Sh::T>(c, p, a.window, u, at, of);
         load_queries();
       }
     }
@@ -717,7 +733,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 
   // rows of sequences without tokens
   for (int b = blockIdx.x; b < c.seqs; b += gridDim.x) {
-    if (steps_seen<Sh::T>(c, a.window, b)) continue;
+    if (steps_of_lane<Sh::T>(c, a.window, b)) continue;
     T* out = reinterpret_cast<T*>(a.out) + b * a.ldo;
     for (int i = threadIdx.x; i < a.q_heads * dim; i += 32 * WARPS) out[i] = from_f<T>(0.f);
     if (a.lse)
@@ -752,7 +768,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
       const bool here = r0 & 1, ends = __ballot_sync(0xffffffffu, mine && (of.y & 1));
       if (warp == 0 && item == 0 && here && !ends && !p.whole) {
         // the block that has the group's last step: the last k with total * k / blocks < the steps up to it
-        goes_on = (int)(quot(part_upto[of_warp(r0)] * blocks + total - 1, total) - 1 - blockIdx.x);
+        goes_on = (int)(quot(part_upto[of_warp(r0)] * blocks + total - 1, max(1ll, total)) - 1 - blockIdx.x);
         if (lane == 0) meta[0] = b, meta[1] = unit;
       }
       const int head = p.tiles_by.of(unit), qi = (unit - head * p.tiles) * Sh::NQ + q;
@@ -788,13 +804,13 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
         if (done) {
           store_row(out, p.pairs, d, dim, sum.x * f, sum.y * f);
           store_row(out, p.pairs, d + 2, dim, sum.z * f, sum.w * f);
-        } else {
+        } else if (!p.whole) {   // (whole units are done, unless lengths changed meanwhile: they may have no workspace)
           *reinterpret_cast<float4*>(to + q * DP + d) = sum;
         }
       }
       if (lane == 0) {
-        if (!done) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, w, 0.f);
-        else if (a.lse) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
+        if (done && a.lse) a.lse[(long long)b * a.q_heads + qh] = lse_of(m, l);
+        if (!done && !p.whole) *reinterpret_cast<float4*>(to + Sh::NQ * DP + 4 * q) = make_float4(m, l, w, 0.f);
       }
     }
   }
