@@ -18,6 +18,8 @@ lengths and page tables are read on the device: a step that was captured in a gr
 once serves all later ones.
 """
 
+import operator
+
 import torch
 
 from . import featfix as ff
@@ -47,7 +49,14 @@ class KVCache8:
 
     def grow(self, counts):
         """Makes room for counts[b] more tokens of sequence b, as the next calls write them.  Raises
-        MemoryError, and changes nothing, where the pages or a sequence's row of the table run out."""
+        ValueError where counts are not one number from 0 on for each sequence, MemoryError where the pages or a
+        sequence's row of the table run out, and changes nothing then."""
+        try:
+            counts = [operator.index(n) for n in counts]
+        except TypeError:
+            raise ValueError("counts: expected a whole number for each sequence")
+        if len(counts) != len(self.used) or min(counts, default=0) < 0:
+            raise ValueError("counts: expected %d numbers from 0 on" % len(self.used))
         used = [u + n for u, n in zip(self.used, counts)]
         need = [-(-u // self.page_size) for u in used]
         if max(need, default=0) > self.width or sum(n - len(h) for n, h in zip(need, self.held)) > len(self.free):
