@@ -346,7 +346,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
     heads_of(in.unit);
     unsigned in_page = 0, in_slot = 0, in_mask = 0;
     float ks_in = 0.f, vs_in = 0.f;   // scales of this lane's token of the last step that was issued, and
-    char* scales_to = ring;           // where they go when they have come
+    // where they go when they have come (before the first: where no copy goes, whose order with these stores is open)
+    char* scales_to = ring + Sh::T * DP * 2 + 4 * lane;
     // Copies of a step's tokens from base + unit * (their offsets) to dst; `all`: no token of it is masked.
     auto copy = [&](auto all, uint32_t dst, const char* base, unsigned unit, unsigned at) {
       base += n_col ? col : 0;
