@@ -30,7 +30,11 @@ MATRICES = ("qkv", "proj", "fc1", "fc2")
 
 class KVCache8:
     """Pages of 8-bit keys and values of ``layers`` layers, and who has which: the same
-    page table and lengths serve every layer.  ``tokens``: the longest sequence."""
+    page table and lengths serve every layer.  ``tokens``: the longest sequence.
+
+    A step takes the last token of every sequence whose length is above ``settled``, its length before it
+    last grew; ``pending``: no step has run since.  All of them are on the GPU, where a captured step reads
+    and leaves them."""
 
     def __init__(self, layers, pages, page_size, heads, dim, seqs, tokens, device="cuda"):
         pad = (dim + 15) // 16 * 16
@@ -40,6 +44,8 @@ class KVCache8:
         self.page_size, self.width = page_size, -(-tokens // page_size)
         self.table = torch.full((seqs, self.width), -1, dtype=torch.int32, device=device)
         self.lens = torch.zeros(seqs, dtype=torch.int32, device=device)
+        self.settled = torch.zeros(seqs, dtype=torch.int32, device=device)
+        self.pending = torch.zeros((), dtype=torch.bool, device=device)
         self.free = list(range(pages - 1, -1, -1))
         self.held = [[] for _ in range(seqs)]
         self.used = [0] * seqs
@@ -67,13 +73,20 @@ class KVCache8:
                 self.held[b] += [self.free.pop() for _ in range(n - first)]
                 self.table[b, first:n] = torch.tensor(self.held[b][first:], dtype=torch.int32)
         self.used = used
+        # (what grew twice since the last step is new from its first growth on)
+        torch.where(self.pending, self.settled, self.lens, out=self.settled)
+        self.pending.fill_(True)
         self.lens.copy_(torch.tensor(used, dtype=torch.int32))
+
+    def written(self):
+        """A program wrote the tokens so far by itself: none of them is a step's new one."""
+        self.settled.copy_(self.lens)
 
     def drop(self, b):
         """Sequence b is over: its pages are free again."""
         self.free += reversed(self.held[b])
         self.held[b], self.used[b] = [], 0
-        self.lens[b] = 0
+        self.lens[b] = self.settled[b] = 0
         self.table[b] = -1
 
 
@@ -92,6 +105,8 @@ class Step8:
         empty = lambda w: torch.empty((n, w), dtype=torch.bfloat16, device=dev)
         self.qkv, self.o, self.d = empty((heads + 2 * k_heads) * self.dim), empty(heads * self.dim), empty(C)
         self.pos = torch.empty((1, n), dtype=torch.int32, device=dev)
+        # lengths of the sequences that have a new token, 0 of the others
+        self.new, self.lens = torch.empty(n, dtype=torch.bool, device=dev), torch.empty(n, dtype=torch.int32, device=dev)
         # 8-bit activations with their scales: of width C, of the heads, of width M
         self.a, self.p, self.h = ((torch.zeros((n, (w + 15) // 16 * 16), dtype=torch.uint8, device=dev)[:, :w],
                                    torch.empty(((w + 127) // 128, n), dtype=torch.float32, device=dev))
@@ -109,22 +124,26 @@ class Step8:
 
     def __call__(self, x):
         """The residual stream x (bf16 [sequences, C]) of the last of each sequence's cache.lens
-        tokens (0: of none, its row means nothing) is updated in place."""
+        tokens is updated in place.  A sequence that has no token, or none since the step before, is left out: its
+        row means nothing, and nothing of it is written to the cache."""
         w, dim, c = self.w, self.dim, self.cache
         split = [n * dim for n in (self.heads, self.k_heads, self.k_heads)]
         q, k, v = self.qkv.split(split, 1)
-        torch.sub(c.lens, 1, out=self.pos[0])
+        torch.gt(c.lens, c.settled, out=self.new)
+        torch.mul(c.lens, self.new, out=self.lens)
+        torch.sub(self.lens, 1, out=self.pos[0])
         ff.featfix_op_rms_norm("bf16", x, w[0]["norm1"], self.eps, q=self.a[0], q_scale=self.a[1])
         for i, wi in enumerate(w):
             self._linear(i, "qkv", self.a, out=self.qkv)
             ff.featfix_op_rope("bf16", self.pos, (dim,), dim, q=q, q_out=q, k=k, k_out=k, theta=self.theta,
                                q_weight=wi["q_norm"], k_weight=wi["k_norm"], eps=self.eps)
-            ff.featfix_op_kv_write("bf16", k, v, c.layer(i), c.table, c.lens)
-            ff.featfix_op_kv_attention("bf16", q, c.layer(i), c.table, c.lens, self.o, self.workspace, dim ** -0.5)
+            ff.featfix_op_kv_write("bf16", k, v, c.layer(i), c.table, self.lens)
+            ff.featfix_op_kv_attention("bf16", q, c.layer(i), c.table, self.lens, self.o, self.workspace, dim ** -0.5)
             ff.featfix_op_quant8("bf16", self.o, *self.p)
             self._linear(i, "proj", self.p, out=self.d)
             self._norms(x, wi["norm1_after"], wi["norm2"])
             self._linear(i, "fc1", self.a, act=1, q=self.h[0], q_scale=self.h[1])
             self._linear(i, "fc2", self.h, out=self.d)
             self._norms(x, wi["norm2_after"], w[i + 1]["norm1"] if i + 1 < len(w) else None)
+        c.pending.fill_(False)
         return x
