@@ -54,9 +54,9 @@ class KVCache8:
         return self.k8[i], self.k_scale[i], self.v8[i], self.v_scale[i]
 
     def grow(self, counts):
-        """Makes room for counts[b] more tokens of sequence b, as the next calls write them.  Raises
-        ValueError where counts are not one number from 0 on for each sequence, MemoryError where the pages or a
-        sequence's row of the table run out, and changes nothing then."""
+        """Makes room for counts[b] more tokens of sequence b, as the next calls write them; asynchronous on the
+        current stream, as the steps are.  Raises ValueError where counts are not one number from 0 on for each
+        sequence, MemoryError where the pages or a sequence's row of the table run out, and changes nothing then."""
         try:
             counts = [operator.index(n) for n in counts]
         except TypeError:
@@ -67,16 +67,24 @@ class KVCache8:
         need = [-(-u // self.page_size) for u in used]
         if max(need, default=0) > self.width or sum(n - len(h) for n, h in zip(need, self.held)) > len(self.free):
             raise MemoryError("no pages left for %d more tokens" % sum(counts))
+        at, pages = [], []   # what changes in the table
         for b, n in enumerate(need):
-            first = len(self.held[b])
-            if n > first:
-                self.held[b] += [self.free.pop() for _ in range(n - first)]
-                self.table[b, first:n] = torch.tensor(self.held[b][first:], dtype=torch.int32)
+            for i in range(len(self.held[b]), n):
+                self.held[b].append(self.free.pop())
+                at.append(b * self.width + i)
+                pages.append(self.held[b][i])
         self.used = used
+        # one copy from pinned memory: the host does not wait for the stream, as it would for pageable memory
+        sent = torch.tensor(used + at + pages, dtype=torch.int64)
+        if self.lens.is_cuda:
+            sent = sent.pin_memory().to(self.lens.device, non_blocking=True)
+        n, k = len(used), len(at)
+        if k:
+            self.table.view(-1)[sent[n:n + k]] = sent[n + k:].int()
         # (what grew twice since the last step is new from its first growth on)
         torch.where(self.pending, self.settled, self.lens, out=self.settled)
         self.pending.fill_(True)
-        self.lens.copy_(torch.tensor(used, dtype=torch.int32))
+        self.lens.copy_(sent[:n])
 
     def written(self):
         """A program wrote the tokens so far by itself: none of them is a step's new one."""
@@ -86,8 +94,9 @@ class KVCache8:
         """Sequence b is over: its pages are free again."""
         self.free += reversed(self.held[b])
         self.held[b], self.used[b] = [], 0
-        self.lens[b] = self.settled[b] = 0
-        self.table[b] = -1
+        self.lens[b].zero_()   # (an assignment would copy a number from the host, and wait)
+        self.settled[b].zero_()
+        self.table[b].fill_(-1)
 
 
 class Step8:

@@ -1,4 +1,4 @@
-"""What a step over the 8-bit cache leaves alone."""
+"""What a step over the 8-bit cache leaves alone, and what its growth waits for."""
 
 import pytest
 import torch
@@ -111,3 +111,20 @@ def test_tokens_that_the_program_wrote_itself(cuda):
     changed = (cache.layer(0)[0] != kept[0]).flatten(2).any(-1)
     where = {(cache.held[1][0], 0), (cache.held[2][0], 2)}
     assert {tuple(p) for p in changed.nonzero().tolist()} == where
+
+
+def test_growing_waits_for_nothing(cuda):
+    _, cache = model()
+    cache.grow([1, 2, 3])         # (pinned memory is there from now on)
+    cache.drop(0)
+    torch.cuda.synchronize()
+    mode = torch.cuda.get_sync_debug_mode()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        for i in range(20):
+            cache.grow([1, int(i < 9), 0])
+            if i == 9:
+                cache.drop(1)
+    finally:
+        torch.cuda.set_sync_debug_mode(mode)
+    assert cache.lens.tolist() == [20, 0, 3] and cache.table[0].tolist() == cache.held[0] + [-1] * (cache.width - 5)
