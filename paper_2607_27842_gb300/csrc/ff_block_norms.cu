@@ -556,14 +556,12 @@ template <class T, bool Q8> cudaError_t norms(long long rows, int C, const Block
   if (few || C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
     return norms_any<T, Q8>(rows, C, a, s);
   const int pieces = (C + 255) / 256;
-  // Warps to a row: four pieces to a warp (three where they leave fewer lanes idle), fewer while the rows
-  // alone leave the SMs without 8 warps each.  14566 x 2048 with modulation and 8-bit output 35.8 us with four, 38.9
-  // with eight (one block to an SM), before the factors' present form 38.0 and 45.8 with two; fp32 85.3, with two
-  // 84.5, centered 79.5 and 86.5.
+  // Warps to a row: four pieces to a warp, fewer while the rows alone leave the SMs without 8 warps each.
+  // 14566 x 2048 with modulation and 8-bit output 35.8 us with four, 38.9 with eight (one block to an SM), before the
+  // factors' present form 38.0 and 45.8 with two; fp32 85.3, with two 84.5, centered 79.5 and 86.5.
   constexpr int PREF = 4;
   int W = 1;
   while (W < 8 && (pieces > PREF * W || (rows * W < 152 * 8 && pieces > W))) W *= 2;
-  if (W > 1 && pieces <= 3 * (W / 2) && rows * (W / 2) >= 152 * 8) W /= 2;
   const int nb = (pieces + W - 1) / W;
   return nb <= 1 ? norms_nb<T, 1, Q8>(W, rows, C, a, s) : nb <= 2 ? norms_nb<T, 2, Q8>(W, rows, C, a, s)
          : nb <= 3 ? norms_nb<T, 3, Q8>(W, rows, C, a, s) : nb <= 4 ? norms_nb<T, 4, Q8>(W, rows, C, a, s)
