@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(256, NORMS_BLOCKS<T, NB>)
 // Rows on any boundary and of any width, element by element: NB adjacent 128-column blocks to a warp,
 // adjacent rows one after the other.  With KEEP the factors stay in registers until the sample changes.
 // Bound by the latency of single elements' loads and of the norms' meetings: 1333 x 1001 in fp32, centered
-// and modulated, 8.4 us, 1.9 TB/s; 14566 x 1001 in bf16 55 us; 1 x 2048 with 8-bit output 3.3 us, the call's own time.
+// and modulated, 8.4 us, 2.5 TB/s; 14566 x 1001 in bf16 55 us.
 template <class T, int NB, bool Q8, bool KEEP>
 __global__ void __launch_bounds__(256, KEEP ? 2 : 1) k_block_norms_any(long long rows, int C, int W, long long per,
                                                                    const __grid_constant__ BlockNormsArgs a) {
@@ -551,9 +551,9 @@ template <class T, int NB, bool Q8> cudaError_t norms_nb(int W, long long rows, 
 }
 template <class T, bool Q8> cudaError_t norms(long long rows, int C, const BlockNormsArgs& a, cudaStream_t s) {
   const auto al = [](const void* p, long long ld) { return !((uintptr_t)p & 15) && ld % (16 / (int)sizeof(T)) == 0; };
-  // (a row to a slot, and weights alone: nothing to reuse from shared memory, 1 x 2048 3.3 instead of 3.65 us)
-  const bool few = rows <= 2 * 152 && C <= 2048 && !a.gate && !a.scale && !a.shift;
-  if (few || C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
+  // (few rows with weights alone too: 1, 152 and 304 rows of 2048 in bf16 with 8-bit output 2.4, 2.6 and 2.9 us, element
+  // by element 3.0, 3.5 and 3.7; of 512 columns 2.15, 2.42 and 2.40, and 2.04, 2.40 and 2.64)
+  if (C % 8 || !al(a.y, a.ldy) || (a.x && !al(a.x, a.ldx)) || (a.sum && !al(a.sum, a.ldsum)) || (a.out && !al(a.out, a.ldo)))
     return norms_any<T, Q8>(rows, C, a, s);
   const int pieces = (C + 255) / 256;
   // Warps to a row: four pieces to a warp, fewer while the rows alone leave the SMs without 8 warps each.
