@@ -268,7 +268,8 @@ FEATFIX_API featfix_status featfix_op_kv_read(int dtype, const featfix_kv_cache*
                                   void* stream);
 
 /* Scratch bytes that featfix_op_kv_attention needs for up to `seqs` sequences in caches of up to
- * `tokens` tokens to each (table_pages * page_size), on any GPU; 0 where it needs none. */
+ * `tokens` tokens to each (table_pages * page_size), on any GPU; 0 where it needs none, and for
+ * arguments that the operator refuses. */
 FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int k_heads, int head_dim,
                                          long long tokens);
 
@@ -279,9 +280,12 @@ FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int 
  *   lse[b, j] = log sum_t exp(x_t)
  * for the heads j of q [seqs, q_heads * head_dim], q_heads a multiple of the cache's heads;
  * out as q (and may be q), dev_lse [seqs, q_heads] nullable.  A row without tokens has
- * out 0 and lse -infinity.  fp32 sums and statistics; q as two fp16 terms with a power of two
- * apart where dtype is f32 and as one where it is bf16, probabilities the same: relative
- * errors of 2^-22 and 2^-11, below dtype's own rounding.  The workspace (16-byte aligned) may
+ * out 0 and lse -infinity.  Scores, sums and statistics are fp32.  q (f32) and the weights
+ * exp(x_t) v_scale (both dtypes) enter the products as two fp16 terms with a power of two
+ * apart: off by 2^-22 of themselves, four times fp32's rounding and far below bf16's, or by
+ * 2^-39 of the head's largest, whichever is more; q in bf16 as one, off by the latter alone.
+ * Weights below 2^-126 of the largest exp(x_t) are 0.  Results are finite for finite q, k and v
+ * with head_dim |scale| max|q| max|k| below 2^126.  The workspace (16-byte aligned) may
  * hold anything; calls that may run at the same time need one each.  The same inputs
  * give the same bits.  The largest power of two that divides the page's and the slot's stride
  * times 2^32 must pass the last place's offset (FEATFIX_ERR_UNSUPPORTED: pools from 64 GB on,

@@ -26,6 +26,14 @@
 // largest still have 11 bits.  w is kept relative to m, as l is: a sum x + log2(scale_v) would lose the
 // scale in the rounding of large x (from 2^24 on more than a factor of two, past fp16's largest number).
 //
+// Bits.  Scores, m, l, w and all sums are fp32.  e4m3 is exact in fp16, and so are bf16 queries (but for elements
+// 2^-29 below the largest of a head): one term.  fp32 queries and all weights are two fp16 terms, 22 bits: errors
+// against 64 bits are 7.0e-7 in fp32 (48 x 700 tokens), and third terms leave them there (7.1e-7, and 13% more
+// time for the queries'), as they come from the exponential and from the products' sums.  Weights in one term
+// (11 bits) made 5% of bf16 results round the other way than fp32 weights do, where two make 0.1%: 64 x 8192
+// tokens 192.4 and 190.8 us, 64 ragged 103.7 and 104.2, 1 x 257 7.07 and 7.25, 4096 x 32 115 and 119, heads of 64 and
+// 256 3% more.
+//
 // A stretch begins and ends within units.  What belongs to one unit of several warps meets in
 // shared memory at the end, and of several blocks in the workspace, which a second
 // kernel adds in the line's order: no atomics, the same bits every time.
@@ -262,7 +270,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
                                                                  const __grid_constant__ KvAttnArgs a,
                                                                  const __grid_constant__ Plan p) {
   typedef Shape<T, DP, NT> Sh;
-  constexpr int WARPS = Sh::WARPS, TERMS = sizeof(T) == 4 ? 2 : 1;   // fp16 terms of queries and of weights
+  constexpr int WARPS = Sh::WARPS, TERMS = sizeof(T) == 4 ? 2 : 1;   // fp16 terms of queries
   extern __shared__ __align__(16) char smem[];
   // partial results of the block's units, in the line's order: what a warp has of a unit that began
   // before its stretch, then of one that goes on behind it
@@ -613,26 +621,19 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
             for (int e = 0; e < 4; ++e) o[nt][i][e] *= f[e & 1];
         }
       }
-      unsigned pb[Sh::MT][NT][TERMS][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float up[2] = {raised(to[nt][0]), raised(to[nt][1])};
+      for (int mt = 0; mt < Sh::MT; ++mt) {
+        unsigned pb[NT][2][2];   // two fp16 terms of weights
 #pragma unroll
-        for (int mt = 0; mt < Sh::MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const float u = s[mt][nt][2 * r] * up[0], v = s[mt][nt][2 * r + 1] * up[1];
+            const float u = s[mt][nt][2 * r] * raised(to[nt][0]), v = s[mt][nt][2 * r + 1] * raised(to[nt][1]);
             const unsigned hi = half2_bits(u, v);
-            pb[mt][nt][0][r] = transposed8x8(hi);
-            if constexpr (TERMS == 2) {
-              const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              pb[mt][nt][1][r] = transposed8x8(half2_bits(u - h.x, v - h.y));
-            }
+            pb[nt][0][r] = transposed8x8(hi);
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            pb[nt][1][r] = transposed8x8(half2_bits(u - h.x, v - h.y));
           }
-      }
-
-#pragma unroll
-      for (int mt = 0; mt < Sh::MT; ++mt)
 #pragma unroll
         for (int i = 0; i < Sh::NV; ++i) {
           unsigned vw[4][Sh::VB / 4];   // tokens 2j, 2j + 1, 2j + 8, 2j + 9: VB adjacent columns
@@ -653,18 +654,22 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
             // bytes of two tokens side by side: a conversion makes a column's pair of tokens
             const unsigned x[2] = {__byte_perm(vw[0][k], vw[1][k], 0x5140), __byte_perm(vw[0][k], vw[1][k], 0x7362)};
             const unsigned y[2] = {__byte_perm(vw[2][k], vw[3][k], 0x5140), __byte_perm(vw[2][k], vw[3][k], 0x7362)};
+            unsigned a[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const unsigned a0 = cvt_e4m3x2((unsigned short)x[h]), a1 = cvt_e4m3x2((unsigned short)(x[h] >> 16));
-              const unsigned a2 = cvt_e4m3x2((unsigned short)y[h]), a3 = cvt_e4m3x2((unsigned short)(y[h] >> 16));
+              a[h][0] = cvt_e4m3x2((unsigned short)x[h]), a[h][1] = cvt_e4m3x2((unsigned short)(x[h] >> 16));
+              a[h][2] = cvt_e4m3x2((unsigned short)y[h]), a[h][3] = cvt_e4m3x2((unsigned short)(y[h] >> 16));
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-                  mma16816(o[nt][i * (Sh::VB / 2) + 2 * k + h], a0, a1, a2, a3, pb[mt][nt][t][0], pb[mt][nt][t][1]);
-            }
+                for (int h = 0; h < 2; ++h)
+                  mma16816(o[nt][i * (Sh::VB / 2) + 2 * k + h], a[h][0], a[h][1], a[h][2], a[h][3], pb[nt][t][0], pb[nt][t][1]);
           }
         }
+      }
       __syncwarp();   // the stage's values and their scales have been read
       }
       issue_values();

@@ -104,3 +104,19 @@ def test_queries_and_keys_of_1500(cuda):
     top = torch.stack([c.values(b, 0, 300)[1].abs().amax(0) for b in range(32)])
     tol = A * (2.0 ** -20 + 364 * 2.0 ** -24 + 2.0 ** -11) + 2.0 ** -25 * top + want.abs() * U["bf16"] * 1.01
     assert ((got - want[:, :, None]).abs() <= tol[:, :, None]).all()
+
+
+@pytest.mark.parametrize("seqs,tokens,heads,group,dim", [(16, 40, 4, 4, 128), (8, 150, 2, 8, 64), (4, 150, 2, 12, 96), (1, 3000, 2, 4, 128),
+                                                         (4, 70, 2, 3, 256)])
+def test_bf16_results_are_those_of_fp32_weights(cuda, seqs, tokens, heads, group, dim):
+    """Exact scores again, so that weights are the values' scales: a result is the rounding of a number within
+    fp32's error, not bf16's, of the formula's."""
+    steps = torch.zeros(tokens, device="cuda")
+    c, q, u = rows(seqs, tokens, heads, group, dim, "bf16", 3, steps, 1.0, 7)
+    out, _ = attend(c, q, heads * group, dim ** -0.5)
+    got = out.view(seqs, heads, group, dim)
+    for b in range(seqs):
+        _, v = c.values(b, 0, tokens)
+        want, A, top = v.mean(0)[:, None], v.abs().mean(0)[:, None], v.abs().amax(0)[:, None]
+        e = A * (2.0 ** -20 + (tokens + 64) * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -36 * top
+        assert ((got[b] >= (want - e).bfloat16()) & (got[b] <= (want + e).bfloat16())).all()
