@@ -294,7 +294,8 @@ featfix_status featfix_op_kv_read(int dtype, const featfix_kv_cache* cache, long
 }
 
 size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int k_heads, int head_dim, long long tokens) {
-  if (seqs <= 0 || q_heads <= 0 || k_heads <= 0 || q_heads % k_heads || head_dim <= 0 || head_dim > KV_DIM_MAX || tokens <= 0)
+  if (seqs <= 0 || q_heads <= 0 || q_heads > 65535 || k_heads <= 0 || q_heads % k_heads || head_dim <= 0 ||
+      head_dim % 8 || head_dim > KV_DIM_MAX || tokens <= 0 || tokens > DIM_MAX)
     return 0;
   return kv_attention_workspace(seqs, q_heads, k_heads, head_dim, tokens);
 }
