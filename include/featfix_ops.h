@@ -216,8 +216,9 @@ FEATFIX_API featfix_status featfix_op_rope(int dtype, long long rows, int head_d
 /* ---------------------------------------------------------------------------
  * An 8-bit cache of keys and values in pages, and the attention of one new token
  * of each sequence over it.  A program that makes tokens one after another, or a
- * clip piece by piece, keeps what later tokens attend to in it.  (The paper has no
- * counterpart.)
+ * clip piece by piece, keeps what later tokens attend to in it.  Several new tokens of
+ * one sequence attend as several sequences, with the same pages and each token's own
+ * length; every one of them reads the cache.  (The paper has no counterpart.)
  *
  * A place of the cache holds a head of one token: head_dim e4m3 values and one
  * scale, by the rule above with the head as the block:
@@ -279,8 +280,8 @@ FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int 
  *   x_t = scale * q[b, j] . k_t[h],   out[b, j] = sum_t exp(x_t) v_t[h] / sum_t exp(x_t),
  *   lse[b, j] = log sum_t exp(x_t)
  * for the heads j of q [seqs, q_heads * head_dim], q_heads a multiple of the cache's heads;
- * out as q (and may be q), dev_lse [seqs, q_heads] nullable.  A row without tokens has
- * out 0 and lse -infinity.  Scores, sums and statistics are fp32.  q (f32) and the weights
+ * out as q (and may be q, with its row stride), dev_lse [seqs, q_heads] nullable.  A row without
+ * tokens has out 0 and lse -infinity.  Scores, sums and statistics are fp32.  q (f32) and weights
  * exp(x_t) v_scale (both dtypes) enter the products as two fp16 terms with a power of two
  * apart: off by 2^-22 of themselves, four times fp32's rounding and far below bf16's, or by
  * 2^-39 of the head's largest, whichever is more; q in bf16 as one, off by the latter alone.

@@ -32,7 +32,7 @@ class KVCache8:
     """Pages of 8-bit keys and values of ``layers`` layers, and who has which: the same
     page table and lengths serve every layer.  ``tokens``: the longest sequence.
 
-    A step takes the last token of every sequence whose length is above ``settled``, its length before it
+    A step takes the last token of every sequence whose length is another than ``settled``, its length before it
     last grew; ``pending``: no step has run since.  All of them are on the GPU, where a captured step reads
     and leaves them."""
 
@@ -138,7 +138,7 @@ class Step8:
         w, dim, c = self.w, self.dim, self.cache
         split = [n * dim for n in (self.heads, self.k_heads, self.k_heads)]
         q, k, v = self.qkv.split(split, 1)
-        torch.gt(c.lens, c.settled, out=self.new)
+        torch.ne(c.lens, c.settled, out=self.new)
         torch.mul(c.lens, self.new, out=self.lens)
         torch.sub(self.lens, 1, out=self.pos[0])
         ff.featfix_op_rms_norm("bf16", x, w[0]["norm1"], self.eps, q=self.a[0], q_scale=self.a[1])
