@@ -1,6 +1,7 @@
 // Attention of one new token of each sequence over the 8-bit key-value cache
-// (formulas: featfix_op_kv_attention).  Bound by memory: every cached byte that a token
-// sees is read once for all query heads of its key head.
+// (formulas: featfix_op_kv_attention).  Bound by memory: every cached byte that a token sees is read
+// once for up to 16 query heads of its key head (8 of more than 128 columns).  More are units of their
+// own, which read it again: 64 x 8192 tokens, 8 key heads of 128 with 16 query heads each 266 us, with 32 486.
 //
 // The work is a line of steps: a unit is one key head of one sequence with up to 8 or 16 of
 // its query heads, a step T of its tokens.  Units of a sequence whose number divides the
@@ -28,8 +29,8 @@
 //
 // Bits.  Scores, m, l, w and all sums are fp32.  e4m3 is exact in fp16, and so are bf16 queries (but for elements
 // 2^-29 below the largest of a head): one term.  fp32 queries and all weights are two fp16 terms, 22 bits: errors
-// against 64 bits are 7.0e-7 in fp32 (48 x 700 tokens), and third terms leave them there (7.1e-7, and 13% more
-// time for the queries'), as they come from the exponential and from the products' sums.  Weights in one term
+// against 64 bits are 7.0e-7 in fp32 (48 x 700 tokens), and third terms leave them there (7.1e-7, and 16 to 20% more
+// time for the queries'), as they come from the exponential, the scores' rounding and the products' sums.  Weights in one term
 // (11 bits) made 5% of bf16 results round the other way than fp32 weights do, where two make 0.1%: 64 x 8192
 // tokens 192.4 and 190.8 us, 64 ragged 103.7 and 104.2, 1 x 257 7.07 and 7.25, 4096 x 32 115 and 119, heads of 64 and
 // 256 3% more.
@@ -38,10 +39,10 @@
 // shared memory at the end, and of several blocks in the workspace, which a second
 // kernel adds in the line's order: no atomics, the same bits every time.
 //
-// Measured, heads of 128 in bf16: 64 sequences of 8192 tokens, 32 + 8 heads, 182 us, 6.1 TB/s (6.4 of
-// HBM's while the kernel runs); 64 of 4096 with fp32 queries 109 us, 5.1 TB/s, where the two terms double
-// the products; 1 x 131072, 16 + 4 heads, 33 us, of which the loop takes 21 (6.7 TB/s) and start, the
-// joins of warps and the second kernel 12; 1 x 257 7 us, a chain of waits.
+// Measured, heads of 128 in bf16: 64 sequences of 8192 tokens, 32 + 8 heads, 185 us, 6.0 TB/s; 64 of 4096
+// with fp32 queries 108 us, 5.1 TB/s, where the queries' two terms double the first product; 1 x 131072, 16 + 4
+// heads, 34 us, of which the loop takes 21 (6.7 TB/s) and start, the joins of warps and the second kernel 13;
+// 1 x 257 7 us, a chain of waits.
 #include "ff_kv8.cuh"
 #include "ff_host.h"
 
@@ -59,7 +60,8 @@ constexpr float NONE = -3.0e38f;   // maximum of nothing
 // Blocks take whole units, and there is no second kernel, where units are short: at most WHOLE_STEPS steps
 // (1 x 1000 tokens of 16 + 4 heads 11.1 us so and 13.6 shared out, 1 x 2000 17.3 and 14.0), and a block's
 // fit its warps (200 x 1000 tokens of 32 + 8 heads 73 and 86 us) or have WHOLE_SUM steps in all (256 x 256
-// tokens 36.3 and 41.6, 256 x 1000 106 and 104, 4096 x 32 130 and 115).
+// tokens 36.3 and 41.6, 256 x 1000 106 and 104, 4096 x 32 130 and 115).  The 152 are this rule's, not the call's GPU's: a
+// workspace is asked for without one, and both sides have to agree.
 constexpr int WHOLE_STEPS = 32, WHOLE_SUM = 160, SMS = 152;
 bool whole_units(long long units, long long steps, int warps) {
   return steps <= WHOLE_STEPS && (units <= (long long)SMS * warps || units * steps <= SMS * WHOLE_SUM);
@@ -70,7 +72,7 @@ template <class E, int DP, int NT> struct Shape {
   // warps of a block: as many as have the registers for their sums and queries.  A spilled register
   // in the loop goes through the 20 KB of L1 that the rings leave: 64 x 8192 tokens took 221 us with
   // 16 warps of 128 registers (80 bytes spilled), 189 with 12 of 168, 206 with 8; 64 x 4096 in fp32 123 with
-  // 8 and 109 with 12, though 88 bytes spill.
+  // 8 and 109 with 12, though 92 bytes spill.
   static constexpr int WARPS = NT > 1 || DP == 256 ? 8 : DP == 64 && sizeof(E) == 2 ? 16 : 12;
   static constexpr int MT = DP == 256 ? 1 : 2;                 // groups of 16 tokens in a step
   static constexpr int T = 16 * MT;
@@ -830,7 +832,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::WARPS, 1) k_kv_attentio
 // latency of its loads in turn: 2 us behind 1 x 131072 tokens of 16 + 4 heads (2.5 MB of parts).
 //
 // FEW: every block has an SM to itself.  Then a thread's first AHEAD parts are under way while the factors are
-// found (114 registers): 1 x 131072 tokens 32.7 us, 35.3 without.  Else three blocks share one: 64 ragged sequences
+// found (107 registers): 1 x 131072 tokens 32.7 us, 35.3 without.  Else three blocks share one: 64 ragged sequences
 // of 32 + 8 heads 104 us with, 99 without.
 constexpr int JOIN = 512;
 template <class T, int DP, int NT, bool FEW>
