@@ -286,7 +286,7 @@ FEATFIX_API size_t featfix_op_kv_attention_workspace(int seqs, int q_heads, int 
  * apart: off by 2^-22 of themselves, four times fp32's rounding and far below bf16's, or by
  * 2^-39 of the head's largest, whichever is more; q in bf16 as one, off by the latter alone.
  * Weights below 2^-126 of the largest exp(x_t) are 0.  Results are finite for finite q, k and v
- * with head_dim |scale| max|q| max|k| below 2^126.  The workspace (16-byte aligned) may
+ * with |scale| and head_dim |scale| max|q| max|k| below 2^126.  The workspace (16-byte aligned) may
  * hold anything; calls that may run at the same time need one each.  The same inputs
  * give the same bits.  The largest power of two that divides the page's and the slot's stride
  * times 2^32 must pass the last place's offset (FEATFIX_ERR_UNSUPPORTED: pools from 64 GB on,

@@ -143,8 +143,11 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
         x[kv][i].zero();
         if (in && i < n) x[kv][i].load(from[kv] + head * c.head_dim + 8 * i);
       }
-    if (h0 == first) p = place_of(c, r.row_start, row, page_size);
-    if (p.page < 0) return;
+    if (h0 == first) {
+      p = place_of(c, r.row_start, row, page_size);
+      // (one place for all lanes, unless lengths or table change meanwhile: then too the warp goes on together)
+      if (!__any_sync(0xffffffffu, p.page >= 0)) return;
+    }
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       float v[16];
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ KvCach
       float m = amax16<T, VEC>(x[kv], v);
 #pragma unroll
       for (int o = L / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (!in) continue;
+      if (!in || p.page < 0) continue;
       const float s = q8_scale(__float_as_uint(m)), inv = q8_inv(s);
       uint8_t* q = reinterpret_cast<uint8_t*>(kv ? c.v : c.k) + place_at(kv ? c.v_stride : c.k_stride, p, head) + col;
       const f32x2 i2 = f2u(inv, inv);

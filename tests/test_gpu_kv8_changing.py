@@ -1,14 +1,14 @@
-"""Lengths that another stream changes while the attention over the 8-bit cache runs: the
-results of those sequences mean nothing, but nothing outside of them is written, whether
-the call has a workspace or needs none, and later calls are as ever."""
+"""Lengths that another stream changes while the 8-bit cache's operators run: the results of
+those sequences mean nothing, but nothing outside of them is written, whether the attention
+has a workspace or needs none, and later calls are as ever."""
 
 import pytest
 import torch
 
 from paper_2607_27842_gb300 import featfix as ff
 
-from .kv_helpers import Cache, TD
-from .test_gpu_kv8 import attend, randn, work
+from .kv_helpers import Cache, NAN8, TD
+from .test_gpu_kv8 import attend, randn, starts, work
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,41 @@ def test_lengths_that_change_during_calls(cuda, dtype, seqs, most, heads, group,
     c.lens.copy_(torch.tensor(lens, dtype=torch.int32))
     call()
     assert (out == want).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_lengths_that_change_during_writes_and_reads(cuda, dtype, ragged):
+    seqs, heads, dim, page = 60, 5, 72, 16
+    counts = [(7 * b) % 23 for b in range(seqs)] if ragged else [1] * seqs
+    lens = [n + 3 * b for b, n in enumerate(counts)]
+    c = Cache(sum(-(-n // page) for n in lens) + 1, page, heads, dim, seqs, -(-max(lens) // page))
+    c.place(lens)
+    free = set(range(c.pages)) - {int(p) for b, n in enumerate(lens) for p in c.table[b, :-(-n // page)]}
+    c.table[c.table == 1 << 30] = min(free)      # (for a while sequences are longer than their pages)
+    k = randn((sum(counts), heads * dim), 3).to(TD[dtype])
+    rs = starts(counts) if ragged else None
+    back = torch.full((2, k.shape[0] + 2, k.shape[1] + 8), 3.0, device="cuda").to(TD[dtype])
+    kb, vb = (t[1:-1, :k.shape[1]] for t in back)
+    write = lambda: ff.featfix_op_kv_write(dtype, k, -k, c.parts, c.table, c.lens, row_start=rs)
+    read = lambda: ff.featfix_op_kv_read(dtype, c.parts, c.table, c.lens, kb, vb, row_start=rs)
+    states = [torch.tensor(s, dtype=torch.int32).cuda() for s in ([0] * seqs, lens, [1 << 30] * seqs, lens[::-1], [-5] * seqs)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(300):
+        with torch.cuda.stream(side):
+            for s in states:
+                c.lens.copy_(s)
+        for _ in range(3):
+            write()
+            read()
+    torch.cuda.synchronize()
+    assert (back[:, 0] == 3).all() and (back[:, -1] == 3).all() and (back[:, :, k.shape[1]:] == 3).all()
+    base = c.k8._base
+    while base._base is not None:
+        base = base._base
+    assert (base[..., dim:] == NAN8).all()
+    c.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    write()
+    read()
+    assert (kb == -vb).all() and ((kb - k).abs().amax(-1) <= k.abs().amax(-1) / 16).all()
